@@ -488,6 +488,115 @@ int mok_ep_expert_bwd(const mok_ep_bwd_args* args);
 int mok_ep_bwd_combine(const mok_ep_bwd_combine_args* args);
 
 /*
+ * Routing from given logits (Section 2.1 uses softmax scores; sigmoid scores, a balance bias and expert groups are what
+ * layers of this kind were extended with since).  Per token, in fp32:
+ *     s = softmax(logits) or sigmoid(logits);   c = s + bias          (bias: selection only; NULL = none)
+ *     the E experts form n_groups groups of consecutive ids; a group's value is its largest c (group_top = 1) or the sum of
+ *     its two largest (2); the topk_groups groups of largest value stay (n_groups = topk_groups = 1: no groups)
+ *     topk_idx = the k largest c among them, descending; all ties go to the lowest id
+ *     topk_w   = scale * s_i / sum_j s_j over the chosen (renormalise != 0; 0 where that sum is 0), or scale * s_i
+ * Without a bias, and unless sums of two scores are compared, the logits themselves are compared.  Logits of -inf are
+ * experts that a token may not use (a token whose logits are all -inf gets weights of 0); NaN logits rank below -inf
+ * and reach their own token's weights only.  The ids are always k distinct ones in 0 .. E-1.
+ * Limits: E <= 512, k <= 32, n_groups <= 32 and a divisor of E, k <= topk_groups * E / n_groups.
+ */
+enum { MOK_TYPE_BF16 = 0, MOK_TYPE_F16 = 1, MOK_TYPE_F32 = 2 };
+enum { MOK_SCORE_SOFTMAX = 0, MOK_SCORE_SIGMOID = 1 };
+typedef struct mok_gate_args {
+    const void* logits;                      /* [T, E] of logits_type, rows logits_stride elements apart */
+    const float* bias;                       /* fp32 [E] or NULL */
+    int64_t logits_stride;
+    int32_t T, E, k;
+    int32_t logits_type;                     /* MOK_TYPE_* */
+    int32_t score;                           /* MOK_SCORE_* */
+    int32_t n_groups, topk_groups, group_top;
+    int32_t renormalise;
+    float scale;
+    int32_t* topk_idx;                       /* out: int32 [T, k] */
+    float* topk_w;                           /* out: fp32 [T, k] */
+    void* stream;
+} mok_gate_args;
+int mok_gate(const mok_gate_args* args);
+
+/* dL/dlogits of mok_gate from dL/dtopk_w (mok_moe_backward's dw) and the chosen ids: the chain rule of the weights above;
+ * the selection and the bias have no gradient.  topk_idx: distinct ids per token; ids outside 0 .. E-1 have no part.
+ * dlogits is written completely, in logits_type. */
+typedef struct mok_gate_bwd_args {
+    const void* logits;
+    const int32_t* topk_idx;                 /* int32 [T, k] */
+    const float* dw;                         /* fp32 [T, k] */
+    int64_t logits_stride, dlogits_stride;
+    int32_t T, E, k;
+    int32_t logits_type, score, renormalise;
+    float scale;
+    void* dlogits;                           /* out: [T, E] of logits_type */
+    void* stream;
+} mok_gate_bwd_args;
+int mok_gate_backward(const mok_gate_bwd_args* args);
+
+/*
+ * Products in 8-bit integers, one scale per token and one per output channel (the paper's low-precision mode is MXFP8,
+ * Section 3.4; this is the form that weight-and-activation quantised checkpoints come in).
+ *   codes   : int8 in -127 .. 127, rows of `stride` bytes (a multiple of 16 for the products; bytes past K are not read)
+ *   quantise: scale = amax / 127, code = round(127 x / amax) in fp32, ties to even; a row of zeros has scale 0, a row with
+ *             an infinity or a NaN has that as its scale and codes 0, so that its products are NaN and no other row's
+ *   product : out[m, n] = x_scale[m] * W_scale[n] * sum_k x_code[m, k] W_code[n, k] (+ bias[n]); the sums are exact 32-bit
+ *             integers (K <= 131072), the scaling is fp32, one rounding to out_type
+ * Any M, N, K and any row strides of x and out; the fast paths want 16-byte aligned rows.
+ * mok_i8_linear with x quantises the rows into the workspace and multiplies; with x = NULL it takes x_codes / x_scales.
+ */
+int mok_i8_quantize(const void* x, int type, long long rows, int K, long long x_stride, int8_t* codes, long long codes_stride,
+                    float* scales, void* stream);
+typedef struct mok_i8_linear_args {
+    const void* x;                           /* [M, K] of x_type, rows x_stride elements apart; or NULL */
+    const int8_t* x_codes;                   /* [M, K], rows codes_stride bytes apart (x = NULL) */
+    const float* x_scales;                   /* fp32 [M] (x = NULL) */
+    const int8_t* W_codes;                   /* [N, K], rows w_stride bytes apart */
+    const float* W_scales;                   /* fp32 [N] */
+    const float* bias;                       /* fp32 [N] or NULL */
+    int64_t x_stride, codes_stride, w_stride, out_stride;
+    int32_t M, K, N, x_type, out_type;
+    void* out;                               /* [M, N] of out_type, rows out_stride elements apart */
+    void* workspace;                         /* mok_i8_linear_workspace_bytes(M, K), 256-byte aligned (x given) */
+    size_t workspace_bytes;
+    void* stream;
+} mok_i8_linear_args;
+size_t mok_i8_linear_workspace_bytes(int M, int K);
+int mok_i8_linear(const mok_i8_linear_args* args);
+
+/*
+ * The routed experts of the layer on 8-bit operands, from given routes:
+ *     out[t] = add[t] + sum_s topk_w[t, s] f_{topk_idx[t, s]}(x[t]),   f_e(x) = W_down_e (silu(W_gate_e x) .* (W_up_e x))
+ * x and the gated activation are quantised per token row as above.  Slots whose id is outside 0 .. E-1 are not routed (a
+ * device that holds some of the experts passes ids relative to its first one).  Deterministic: fixed slot order, no atomics.
+ * H and I multiples of 8, I <= 16384; limits of the layer otherwise.
+ */
+typedef struct mok_i8_experts_args {
+    const void* x;                           /* [T, H] of type, rows x_stride elements apart */
+    const int32_t* topk_idx;                 /* int32 [T, k] */
+    const float* topk_w;                     /* fp32 [T, k] */
+    const int8_t* gate_up_codes;             /* [E, 2I, H]: gate rows, then up rows; rows gate_up_stride bytes apart */
+    const float* gate_up_scales;             /* fp32 [E, 2I] */
+    const int8_t* down_codes;                /* [E, H, I], rows down_stride bytes apart */
+    const float* down_scales;                /* fp32 [E, H] */
+    const float* down_max;                   /* fp32 [E]: the largest down_scales of each expert */
+    const void* add;                         /* [T, H] of type (a shared expert's output), or NULL */
+    int64_t x_stride, gate_up_stride, down_stride, add_stride, out_stride;
+    int32_t T, H, I, E, k;
+    int32_t type;                            /* of x, add and out: MOK_TYPE_BF16 or MOK_TYPE_F16 */
+    void* out;                               /* [T, H], rows out_stride elements apart */
+    void* workspace;                         /* mok_i8_experts_workspace_bytes(...), 256-byte aligned */
+    size_t workspace_bytes;
+    void* stream;
+} mok_i8_experts_args;
+size_t mok_i8_experts_workspace_bytes(int T, int H, int I, int E, int k);
+int mok_i8_experts(const mok_i8_experts_args* args);
+
+/* Status word of the 8-bit products on the current device (one for all of them, kept until it is read): synchronises
+ * `stream`, returns MOK_OK or MOK_ERR_TIMEOUT (a bounded wait ran out) and clears it. */
+int mok_i8_status(void* stream);
+
+/*
  * Reads the device-side status word of a workspace after synchronising `stream` -- the only call besides
  * mok_moe_forward_host that blocks the host.  Returns MOK_OK, MOK_ERR_TIMEOUT or MOK_ERR_SCHEDULE
  * (or MOK_ERR_CUDA if the stream itself is in error).

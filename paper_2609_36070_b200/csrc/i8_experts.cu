@@ -1,0 +1,372 @@
+// Routed expert FFNs in 8-bit integers: out[t] = add[t] + sum_s w[t, s] f_{idx[t, s]}(x[t]), every product with exact
+// integer sums and one scale per row and per channel.
+//   1. token rows -> codes (once per token, not once per route)
+//   2. dispatch schedule (the layer's own kernels)
+//   3. gate/up product over gathered rows, h = silu(g) u in fp32
+//   4. rows of h -> codes; the row's factor for step 6
+//   5. down product, fp16 in the unit of the row
+//   6. combine: slot order, fp32, no atomics, so the bits do not depend on the launch
+#include "i8_common.cuh"
+#include <string.h>
+
+namespace mok {
+namespace i8 {
+
+constexpr int THREADS = 256;
+
+// Rows of h (fp32, padded row space) -> codes.  factor = scale * b_max / y_unit: what the combine multiplies a row by.
+// Pad rows are left alone.
+template <int TPR, int NV>
+__global__ void __launch_bounds__(THREADS)
+quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ codes, int ldc, float* __restrict__ factor,
+                       const float* __restrict__ b_max, float inv_unit, const WsHeader* __restrict__ hdr,
+                       const int32_t* __restrict__ tile_expert, const int32_t* __restrict__ pad_offsets,
+                       const int32_t* __restrict__ counts) {
+    __shared__ uint32_t s_max[THREADS / 32];
+    pdl_enter();
+    constexpr int ROWS = THREADS / TPR;
+    const int sub = threadIdx.x % TPR, pieces = I >> 2;
+    const int rows = hdr->n_mtiles * TILE_M;
+    for (int p0 = blockIdx.x * ROWS; p0 < rows; p0 += gridDim.x * ROWS) {
+        const int p = p0 + threadIdx.x / TPR;
+        int e = 0;
+        bool live = p < rows;
+        if (live) {
+            e = __ldg(tile_expert + p / TILE_M);
+            live = p - __ldg(pad_offsets + e) < __ldg(counts + e);
+        }
+        const float4* src = reinterpret_cast<const float4*>(h + (size_t)p * I);
+        float4 v[NV];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = sub + i * TPR;
+            v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (live && c < pieces) v[i] = __ldcs(src + c);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+            m = max(max(m, max(abs_bits(v[i].x), abs_bits(v[i].y))), max(abs_bits(v[i].z), abs_bits(v[i].w)));
+        m = __reduce_max_sync(0xffffffffu, m);
+        if (TPR > 32) {
+            const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+            __syncthreads();
+            if (lane == 0) s_max[warp] = m;
+            __syncthreads();
+            m = __reduce_max_sync(0xffffffffu, lane < THREADS / 32 ? s_max[lane] : 0u);
+        }
+        if (!live) continue;
+        const float amax = __uint_as_float(m);
+        const bool codable = m > 0 && finite_bits(m);
+        const RowRule rule = row_rule(amax);
+        int8_t* dst = codes + (size_t)p * ldc;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = sub + i * TPR;
+            if (c >= pieces) break;
+            uint32_t o = 0u;
+            if (codable)
+                o = pack4(code_bits(v[i].x, rule), code_bits(v[i].y, rule), code_bits(v[i].z, rule), code_bits(v[i].w, rule));
+            *reinterpret_cast<uint32_t*>(dst + c * 4) = o;
+        }
+        if (sub == 0) factor[p] = amax / 127.f * (b_max[e] * inv_unit);
+    }
+}
+
+template <class T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
+
+// One block per token.  Slots whose expert id is outside 0 .. E-1 are not routed.
+template <class T>
+__global__ void __launch_bounds__(128)
+combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ factor, const int32_t* __restrict__ idx,
+                    const float* __restrict__ w, const int32_t* __restrict__ pos, const T* __restrict__ add, long long ld_add,
+                    int H, int E, int k, T* __restrict__ out, long long ld_out) {
+    __shared__ int32_t s_pos[MAX_K];
+    __shared__ float s_w[MAX_K];
+    pdl_enter();
+    const size_t t = blockIdx.x;
+    if (threadIdx.x < k) {
+        const size_t j = t * k + threadIdx.x;
+        const bool routed = (unsigned)idx[j] < (unsigned)E;
+        const int p = routed ? pos[j] : -1;
+        s_pos[threadIdx.x] = p;
+        s_w[threadIdx.x] = routed ? w[j] * factor[p] : 0.f;
+    }
+    __syncthreads();
+    const int chunks = H >> 3;
+    for (int c = threadIdx.x; c < chunks; c += 128) {
+        float acc[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+        if (add) {
+            const uint4 raw = __ldg(reinterpret_cast<const uint4*>(add + t * ld_add + c * 8));
+            const T* v = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] = to_f(v[i]);
+        }
+#pragma unroll 4
+        for (int s = 0; s < k; ++s) {
+            if (s_pos[s] < 0) continue;
+            const uint4 raw = __ldg(reinterpret_cast<const uint4*>(y + (size_t)s_pos[s] * H + c * 8));
+            const __half2* v = reinterpret_cast<const __half2*>(&raw);
+            const float f = s_w[s];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 q = __half22float2(v[i]);
+                acc[2 * i] = fmaf(f, q.x, acc[2 * i]);
+                acc[2 * i + 1] = fmaf(f, q.y, acc[2 * i + 1]);
+            }
+        }
+        uint4 o;
+        T* v = reinterpret_cast<T*>(&o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = from_f<T>(acc[i]);
+        *reinterpret_cast<uint4*>(out + t * ld_out + c * 8) = o;
+    }
+}
+
+static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+// Workspace of the routed experts: the schedule's tables (a WsLayout of which only those are set) and the activations.
+struct ExpertsLayout {
+    WsLayout L;
+    size_t xq, xs, h, hq, factor, y, total;
+    int pitch_h, pitch_i;
+    long long max_tiles;         // upper bound of 256-row tiles
+};
+
+static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) {
+    if (T < 0 || H < 8 || I < 8 || (H % 8) || (I % 8) || E < 1 || E > MAX_E || k < 1 || k > MAX_K || k > E) return false;
+    if (H > MAX_CONTRACTION || I > 16384 || (long long)T * k >= (1ll << 31) / 256) return false;
+    memset(X, 0, sizeof(*X));
+    WsLayout& L = X->L;
+    const long long R = (long long)T * k, nonempty = R < E ? R : E;
+    const long long rpad = (R + nonempty * (TILE_M - 1) + TILE_M - 1) / TILE_M * TILE_M;
+    L.R = (int32_t)R;
+    L.Rpad = (int32_t)(rpad > TILE_M ? rpad : TILE_M);
+    L.max_mt = L.Rpad / TILE_M;
+    L.n_blk = (int32_t)((R + SCHED_CHUNK - 1) / SCHED_CHUNK);
+    if (L.n_blk < 1) L.n_blk = 1;
+    X->max_tiles = R / (2 * TILE_M) + nonempty;
+    X->pitch_h = pitch_of(H);
+    X->pitch_i = pitch_of(I);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; };
+    const size_t r1 = sizeof(int32_t) * (size_t)(R > 0 ? R : 1);
+    L.header = take(sizeof(WsHeader));
+    L.counts = take(sizeof(int32_t) * E);
+    L.offsets = take(sizeof(int32_t) * (E + 1));
+    L.pad_offsets = take(sizeof(int32_t) * (E + 1));
+    L.mt_start = take(sizeof(int32_t) * (E + 1));
+    L.tile_expert = take(sizeof(int32_t) * (size_t)L.max_mt);
+    L.mt_start2 = take(sizeof(int32_t) * (E + 1));
+    L.tile_expert2 = take(sizeof(int32_t) * (size_t)L.max_mt);
+    L.perm = take(r1);
+    L.inv = take(r1);
+    L.pos = take(r1);
+    L.blk_hist = take(sizeof(int32_t) * (size_t)L.n_blk * E);
+    L.row_token = take(sizeof(int32_t) * (size_t)L.Rpad);
+    X->xq = take((size_t)(T > 0 ? T : 1) * X->pitch_h);
+    X->xs = take(sizeof(float) * (size_t)(T > 0 ? T : 1));
+    X->h = take(sizeof(float) * (size_t)L.Rpad * I);
+    X->hq = take((size_t)L.Rpad * X->pitch_i);
+    X->factor = take(sizeof(float) * (size_t)L.Rpad);
+    X->y = take(2 * (size_t)L.Rpad * H);
+    X->total = off;
+    return true;
+}
+
+template <class T>
+static cudaError_t launch_combine_half(const mok_i8_experts_args* a, const ExpertsLayout& X, char* ws, cudaStream_t s) {
+    return launch_pdl(combine_half_kernel<T>, dim3((unsigned)a->T), dim3(128), 0, s, reinterpret_cast<const __half*>(ws + X.y),
+                      reinterpret_cast<const float*>(ws + X.factor), a->topk_idx, a->topk_w,
+                      reinterpret_cast<const int32_t*>(ws + X.L.pos), reinterpret_cast<const T*>(a->add),
+                      (long long)a->add_stride, a->H, a->E, a->k, reinterpret_cast<T*>(a->out), (long long)a->out_stride);
+}
+
+}  // namespace i8
+}  // namespace mok
+
+using namespace mok;
+
+extern "C" {
+
+int mok_i8_quantize(const void* x, int type, long long rows, int K, long long x_stride, int8_t* codes, long long codes_stride,
+                    float* scales, void* stream) {
+    if (!i8::type_ok(type) || rows < 0 || K < 1 || K > i8::MAX_CONTRACTION) return MOK_ERR_SHAPE;
+    if (rows > 1 && (x_stride < K || codes_stride < K)) return MOK_ERR_SHAPE;
+    if (rows == 0) return MOK_OK;
+    if (!x || !codes || !scales) return MOK_ERR_NULL;
+    if (!i8::aligned(x, i8::type_bytes(type)) || !i8::aligned(scales, 4)) return MOK_ERR_ALIGN;
+    g_pdl = true;
+    const cudaError_t e = i8::launch_quantize(x, type, rows, K, x_stride, codes, codes_stride > K ? codes_stride : K, scales,
+                                              reinterpret_cast<cudaStream_t>(stream));
+    return e == cudaSuccess ? MOK_OK : cuda_fail(e);
+}
+
+size_t mok_i8_linear_workspace_bytes(int M, int K) {
+    if (M < 0 || K < 1 || K > i8::MAX_CONTRACTION) return 0;
+    const size_t m = M > 0 ? M : 1;
+    return align_up(m * i8::pitch_of(K), 256) + align_up(m * sizeof(float), 256);
+}
+
+int mok_i8_linear(const mok_i8_linear_args* a) {
+    if (!a) return MOK_ERR_NULL;
+    const bool coded = a->x == nullptr && a->x_codes != nullptr;
+    if (a->M < 0 || a->K < 1 || a->K > i8::MAX_CONTRACTION || a->N < 1 || !i8::type_ok(a->out_type) ||
+        (!coded && !i8::type_ok(a->x_type)))
+        return MOK_ERR_SHAPE;
+    if ((a->M > 1 && ((coded ? a->codes_stride : a->x_stride) < a->K || a->out_stride < a->N)) || a->w_stride < a->K)
+        return MOK_ERR_SHAPE;
+    if (a->M == 0) return MOK_OK;
+    if ((!a->x && !a->x_codes) || (coded && !a->x_scales) || !a->W_codes || !a->W_scales || !a->out) return MOK_ERR_NULL;
+    if (!i8::aligned(a->W_codes, 16) || (a->w_stride % 16) || !i8::aligned(a->W_scales, 4) || !i8::aligned(a->bias, 4) ||
+        !i8::aligned(a->out, i8::type_bytes(a->out_type)))
+        return MOK_ERR_ALIGN;
+    if (coded ? !i8::aligned(a->x_codes, 16) || (a->codes_stride % 16) || !i8::aligned(a->x_scales, 4)
+              : !i8::aligned(a->x, i8::type_bytes(a->x_type)))
+        return MOK_ERR_ALIGN;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
+    g_pdl = true;
+    i8::ProductArgs g = {};
+    cudaError_t e = i8::status_header(&g.header);
+    if (e != cudaSuccess) return cuda_fail(e);
+    if (coded) {
+        g.A = a->x_codes;
+        g.lda = a->codes_stride;
+        g.a_scale = a->x_scales;
+    } else {
+        if (!a->workspace || !i8::aligned(a->workspace, 256) || a->workspace_bytes < mok_i8_linear_workspace_bytes(a->M, a->K))
+            return MOK_ERR_WORKSPACE;
+        char* ws = reinterpret_cast<char*>(a->workspace);
+        int8_t* codes = reinterpret_cast<int8_t*>(ws);
+        const int pitch = i8::pitch_of(a->K);
+        float* scales = reinterpret_cast<float*>(ws + align_up((size_t)a->M * pitch, 256));
+        e = i8::launch_quantize(a->x, a->x_type, a->M, a->K, a->x_stride, codes, pitch, scales, s);
+        if (e != cudaSuccess) return cuda_fail(e);
+        g.A = codes;
+        g.lda = pitch;
+        g.a_scale = scales;
+    }
+    g.a_rows = a->M;
+    g.B = a->W_codes;
+    g.ldb = a->w_stride;
+    g.b_scale = a->W_scales;
+    g.bias = a->bias;
+    g.K = a->K; g.N = a->N; g.E = 1;
+    g.C = a->out;
+    g.ldc = a->M > 1 ? a->out_stride : a->N;
+    g.c_type = a->out_type;
+    g.dense_rows = a->M;
+    g.max_mt = (a->M + 2 * TILE_M - 1) / (2 * TILE_M);
+    e = i8::launch_product(g, i8::EPI_PLAIN, s);
+    return e == cudaSuccess ? MOK_OK : cuda_fail(e);
+}
+
+size_t mok_i8_experts_workspace_bytes(int T, int H, int I, int E, int k) {
+    i8::ExpertsLayout X;
+    return i8::experts_layout(T, H, I, E, k, &X) ? X.total : 0;
+}
+
+int mok_i8_experts(const mok_i8_experts_args* a) {
+    if (!a) return MOK_ERR_NULL;
+    i8::ExpertsLayout X;
+    if (!i8::experts_layout(a->T, a->H, a->I, a->E, a->k, &X) || (a->type != MOK_TYPE_BF16 && a->type != MOK_TYPE_F16))
+        return MOK_ERR_SHAPE;
+    if (a->gate_up_stride < a->H || a->down_stride < a->I ||
+        (a->T > 1 && (a->x_stride < a->H || a->out_stride < a->H || (a->add && a->add_stride < a->H))))
+        return MOK_ERR_SHAPE;
+    if (a->T == 0) return MOK_OK;
+    if (!a->x || !a->topk_idx || !a->topk_w || !a->gate_up_codes || !a->gate_up_scales || !a->down_codes || !a->down_scales ||
+        !a->down_max || !a->out)
+        return MOK_ERR_NULL;
+    if (!i8::aligned(a->x, 2) || !i8::aligned(a->out, 16) || !i8::aligned(a->add, 16) || !i8::aligned(a->gate_up_codes, 16) ||
+        !i8::aligned(a->down_codes, 16) || (a->gate_up_stride % 16) || (a->down_stride % 16) || (a->out_stride % 8) ||
+        (a->add && a->add_stride % 8) || !i8::aligned(a->topk_idx, 4) || !i8::aligned(a->topk_w, 4))
+        return MOK_ERR_ALIGN;
+    if (!a->workspace || !i8::aligned(a->workspace, 256) || a->workspace_bytes < X.total) return MOK_ERR_WORKSPACE;
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
+    char* ws = reinterpret_cast<char*>(a->workspace);
+    WsHeader* hdr = reinterpret_cast<WsHeader*>(ws + X.L.header);
+    g_pdl = true;
+    i8::ProductArgs g = {};
+    cudaError_t e = i8::status_header(&g.header);
+    if (e != cudaSuccess) return cuda_fail(e);
+    e = i8::launch_quantize(a->x, a->type, a->T, a->H, a->x_stride, reinterpret_cast<int8_t*>(ws + X.xq), X.pitch_h,
+                            reinterpret_cast<float*>(ws + X.xs), s);
+    if (e != cudaSuccess) return cuda_fail(e);
+    e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
+    if (e != cudaSuccess) return cuda_fail(e);
+    g.E = a->E;
+    g.counts = reinterpret_cast<const int32_t*>(ws + X.L.counts);
+    g.pad_offsets = reinterpret_cast<const int32_t*>(ws + X.L.pad_offsets);
+    g.n_mtiles = &hdr->n_mtiles2;
+    g.tile_expert = reinterpret_cast<const int32_t*>(ws + X.L.tile_expert2);
+    g.mt_start = reinterpret_cast<const int32_t*>(ws + X.L.mt_start2);
+    g.max_mt = (int32_t)X.max_tiles;
+    g.A = reinterpret_cast<const int8_t*>(ws + X.xq);
+    g.lda = X.pitch_h;
+    g.a_rows = a->T;
+    g.a_scale = reinterpret_cast<const float*>(ws + X.xs);
+    g.row_token = reinterpret_cast<const int32_t*>(ws + X.L.row_token);
+    g.B = a->gate_up_codes;
+    g.ldb = a->gate_up_stride;
+    g.b_scale = a->gate_up_scales;
+    g.K = a->H; g.N = a->I;
+    g.C = ws + X.h;
+    g.ldc = a->I;
+    e = i8::launch_product(g, i8::EPI_GATED, s);
+    if (e != cudaSuccess) return cuda_fail(e);
+    float unit = 1.f;                                // |sum| * unit <= 65504
+    while (127.0 * 127.0 * a->I * unit > 65504.0) unit *= 0.5f;
+    {
+        const float* h = reinterpret_cast<const float*>(ws + X.h);
+        int8_t* hq = reinterpret_cast<int8_t*>(ws + X.hq);
+        float* factor = reinterpret_cast<float*>(ws + X.factor);
+        const int32_t* te = reinterpret_cast<const int32_t*>(ws + X.L.tile_expert);
+        const long long rows = X.L.Rpad, most = 148 * 16;
+        const bool warp_rows = a->I <= 1024;
+        const long long blocks = warp_rows ? (rows + 7) / 8 : rows;
+        const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(i8::THREADS);
+        e = warp_rows ? launch_pdl(i8::quantize_hidden_kernel<32, 8>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor, a->down_max,
+                                   1.f / unit, hdr, te, g.pad_offsets, g.counts)
+            : a->I <= 8192 ? launch_pdl(i8::quantize_hidden_kernel<256, 8>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor,
+                                        a->down_max, 1.f / unit, hdr, te, g.pad_offsets, g.counts)
+                           : launch_pdl(i8::quantize_hidden_kernel<256, 16>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor,
+                                        a->down_max, 1.f / unit, hdr, te, g.pad_offsets, g.counts);
+        if (e != cudaSuccess) return cuda_fail(e);
+    }
+    g.A = reinterpret_cast<const int8_t*>(ws + X.hq);
+    g.lda = X.pitch_i;
+    g.a_rows = X.L.Rpad;
+    g.a_scale = nullptr;
+    g.row_token = nullptr;
+    g.B = a->down_codes;
+    g.ldb = a->down_stride;
+    g.b_scale = a->down_scales;
+    g.b_max = a->down_max;
+    g.y_unit = unit;
+    g.K = a->I; g.N = a->H;
+    g.C = ws + X.y;
+    g.ldc = a->H;
+    e = i8::launch_product(g, i8::EPI_HALF, s);
+    if (e != cudaSuccess) return cuda_fail(e);
+    e = a->type == MOK_TYPE_BF16 ? i8::launch_combine_half<__nv_bfloat16>(a, X, ws, s) : i8::launch_combine_half<__half>(a, X, ws, s);
+    return e == cudaSuccess ? MOK_OK : cuda_fail(e);
+}
+
+int mok_i8_status(void* stream) {
+    WsHeader* hdr = nullptr;
+    cudaError_t e = i8::status_header(&hdr);
+    if (e != cudaSuccess) return cuda_fail(e);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    int32_t status = 0;
+    if ((e = cudaMemcpyAsync(&status, &hdr->status, sizeof(status), cudaMemcpyDeviceToHost, s)) != cudaSuccess ||
+        (e = cudaMemsetAsync(&hdr->status, 0, sizeof(status), s)) != cudaSuccess || (e = cudaStreamSynchronize(s)) != cudaSuccess)
+        return cuda_fail(e);
+    return status;
+}
+
+}  // extern "C"

@@ -5,6 +5,7 @@ device memory and streams.  Importing this module fails loudly if the library ha
 (`python -m paper_2609_36070_b200.build`); there is no CPU or PyTorch fallback.
 """
 import ctypes
+import functools
 import os
 
 import torch
@@ -27,13 +28,17 @@ EXPORTS = ["mok_moe_forward", "mok_workspace_bytes", "mok_workspace_bytes_ring",
            "mok_mx_scale_bytes", "mok_mx_quantize_weights", "mok_mx_quantize_rows", "mok_mx_workspace_bytes",
            "mok_ep_mx_workspace_bytes", "mok_bwd_workspace_bytes", "mok_moe_backward", "mok_ep_bwd_workspace_bytes",
            "mok_ep_expert_bwd", "mok_ep_bwd_combine", "mok_selftest_per_device",
-           "mok_router_prepared_bytes", "mok_router_prepare"]
+           "mok_router_prepared_bytes", "mok_router_prepare", "mok_gate", "mok_gate_backward", "mok_i8_quantize",
+           "mok_i8_linear_workspace_bytes", "mok_i8_linear", "mok_i8_experts_workspace_bytes", "mok_i8_experts",
+           "mok_i8_status"]
 MOK_PRECISION_BF16, MOK_PRECISION_MXFP8 = 0, 1
 MOK_H_RING_MIN_TILES = 24
 MOK_MAX_RANKS = 16
 MOK_NOALLOC_MAX_ROUTES = 32768
 MOK_DEBUG_STARVE = 2
 MOK_DEBUG_NO_ARRIVALS = 3
+MOK_TYPE_BF16, MOK_TYPE_F16, MOK_TYPE_F32 = 0, 1, 2
+MOK_SCORE_SOFTMAX, MOK_SCORE_SIGMOID = 0, 1
 STAGES = ["router", "schedule", "gather", "gemm1", "gemm2", "shared_gemm1", "shared_gemm2", "combine"]
 
 
@@ -126,6 +131,59 @@ class mok_bwd_args(ctypes.Structure):
                 ("config", ctypes.POINTER(mok_config)), ("stream", ctypes.c_void_p)]
 
 
+class mok_gate_args(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("logits_stride", ctypes.c_int64),
+                ("T", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("logits_type", ctypes.c_int32),
+                ("score", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("topk_groups", ctypes.c_int32),
+                ("group_top", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
+
+
+class mok_gate_bwd_args(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("topk_idx", ctypes.c_void_p), ("dw", ctypes.c_void_p),
+                ("logits_stride", ctypes.c_int64), ("dlogits_stride", ctypes.c_int64),
+                ("T", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("logits_type", ctypes.c_int32),
+                ("score", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("dlogits", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
+
+
+class mok_i8_linear_args(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_codes", ctypes.c_void_p), ("x_scales", ctypes.c_void_p),
+                ("W_codes", ctypes.c_void_p), ("W_scales", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("codes_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("M", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32),
+                ("x_type", ctypes.c_int32), ("out_type", ctypes.c_int32), ("out", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+class mok_i8_experts_args(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p),
+                ("gate_up_codes", ctypes.c_void_p), ("gate_up_scales", ctypes.c_void_p),
+                ("down_codes", ctypes.c_void_p), ("down_scales", ctypes.c_void_p), ("down_max", ctypes.c_void_p),
+                ("add", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("gate_up_stride", ctypes.c_int64),
+                ("down_stride", ctypes.c_int64), ("add_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("I", ctypes.c_int32), ("E", ctypes.c_int32),
+                ("k", ctypes.c_int32), ("type", ctypes.c_int32), ("out", ctypes.c_void_p),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
+
+
+_lib.mok_gate.restype = ctypes.c_int
+_lib.mok_gate.argtypes = [ctypes.POINTER(mok_gate_args)]
+_lib.mok_gate_backward.restype = ctypes.c_int
+_lib.mok_gate_backward.argtypes = [ctypes.POINTER(mok_gate_bwd_args)]
+_lib.mok_i8_quantize.restype = ctypes.c_int
+_lib.mok_i8_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong,
+                                 ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p]
+_lib.mok_i8_linear_workspace_bytes.restype = ctypes.c_size_t
+_lib.mok_i8_linear_workspace_bytes.argtypes = [ctypes.c_int] * 2
+_lib.mok_i8_linear.restype = ctypes.c_int
+_lib.mok_i8_linear.argtypes = [ctypes.POINTER(mok_i8_linear_args)]
+_lib.mok_i8_experts_workspace_bytes.restype = ctypes.c_size_t
+_lib.mok_i8_experts_workspace_bytes.argtypes = [ctypes.c_int] * 5
+_lib.mok_i8_experts.restype = ctypes.c_int
+_lib.mok_i8_experts.argtypes = [ctypes.POINTER(mok_i8_experts_args)]
+_lib.mok_i8_status.restype = ctypes.c_int
+_lib.mok_i8_status.argtypes = [ctypes.c_void_p]
 _lib.mok_bwd_workspace_bytes.restype = ctypes.c_size_t
 _lib.mok_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 6
 _lib.mok_moe_backward.restype = ctypes.c_int
@@ -655,6 +713,203 @@ def mok_moe_backward(x, W_gate_up, W_down, W_shared_gate_up, W_shared_down, topk
     _check(_lib.mok_moe_backward(ctypes.byref(a)))
     res["workspace"] = workspace
     return res
+
+
+_TYPES = {torch.bfloat16: MOK_TYPE_BF16, torch.float16: MOK_TYPE_F16, torch.float32: MOK_TYPE_F32}
+_SCORES = {"softmax": MOK_SCORE_SOFTMAX, "sigmoid": MOK_SCORE_SIGMOID}
+
+
+def _on_stream(call):
+    """For the entry points below: runs the call on the device of its first tensor and, with stream=, on that stream, so that
+    outputs and scratch that it allocates belong to the stream that writes them."""
+    @functools.wraps(call)
+    def wrapped(first, *args, stream=None, **kwargs):
+        device = first.device
+        if device.type != "cuda":
+            raise ValueError(f"{call.__name__}: tensors have to be on a CUDA device, got {device}")
+        if stream is None and device.index == torch.cuda.current_device():
+            return call(first, *args, raw_stream=torch.cuda.current_stream().cuda_stream, **kwargs)
+        with torch.cuda.device(device):
+            if stream is None:
+                stream = torch.cuda.current_stream()
+            with torch.cuda.stream(stream):
+                return call(first, *args, raw_stream=stream.cuda_stream, **kwargs)
+    return wrapped
+
+
+def _rows(name, t, width, device, *dtypes):
+    """Checks a matrix argument [rows, width] whose last index is contiguous; returns the elements between its rows."""
+    if t.dim() != 2 or t.shape[1] < width or t.dtype not in dtypes or t.device != device or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name}: expected rows of {width} contiguous elements of {dtypes} on {device}, got shape "
+                         f"{tuple(t.shape)}, strides {t.stride()}, {t.dtype} on {t.device}")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _packed(name, t, shape, device, dtype):
+    """Checks an argument that has to be contiguous; returns its address."""
+    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}, got shape {tuple(t.shape)}, "
+                         f"strides {t.stride()}, {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+@_on_stream
+def mok_gate(logits, k, bias=None, score="softmax", n_groups=1, topk_groups=1, group_top=2, renormalise=True, scale=1.0, *,
+             raw_stream):
+    """Routing from logits [T, E] (bf16, fp16 or fp32): returns (topk_idx int32 [T, k], topk_w fp32 [T, k]).  score:
+    "softmax" or "sigmoid"; bias fp32 [E] takes part in the selection only; see include/mok.h for groups and weights."""
+    T, E = logits.shape
+    a = mok_gate_args()
+    a.logits_stride = _rows("logits", logits, E, logits.device, *_TYPES)
+    a.logits, a.logits_type = logits.data_ptr(), _TYPES[logits.dtype]
+    if bias is not None:
+        a.bias = _packed("bias", bias, (E,), logits.device, torch.float32)
+    a.T, a.E, a.k, a.score, a.n_groups, a.topk_groups, a.group_top = T, E, k, _SCORES[score], n_groups, topk_groups, group_top
+    a.renormalise, a.scale, a.stream = bool(renormalise), scale, raw_stream
+    idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
+    w = torch.empty((T, k), dtype=torch.float32, device=logits.device)
+    a.topk_idx, a.topk_w = idx.data_ptr(), w.data_ptr()
+    _check(_lib.mok_gate(a))
+    return idx, w
+
+
+@_on_stream
+def mok_gate_backward(logits, topk_idx, dw, score="softmax", renormalise=True, scale=1.0, *, raw_stream):
+    """dL/dlogits [T, E] (in the logits' type) from dL/dtopk_w (dw) and the chosen experts of mok_gate."""
+    T, E = logits.shape
+    k = topk_idx.shape[1]
+    a = mok_gate_bwd_args()
+    a.logits_stride = _rows("logits", logits, E, logits.device, *_TYPES)
+    a.logits, a.logits_type = logits.data_ptr(), _TYPES[logits.dtype]
+    a.topk_idx = _packed("topk_idx", topk_idx, (T, k), logits.device, torch.int32)
+    a.dw = _packed("dw", dw, (T, k), logits.device, torch.float32)
+    a.T, a.E, a.k, a.score, a.renormalise, a.scale = T, E, k, _SCORES[score], bool(renormalise), scale
+    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
+    a.dlogits, a.dlogits_stride, a.stream = out.data_ptr(), E, raw_stream
+    _check(_lib.mok_gate_backward(a))
+    return out
+
+
+@_on_stream
+def mok_i8_quantize(x, *, raw_stream):
+    """Rows of x [..., K] (bf16, fp16 or fp32) -> (codes int8 [..., K rounded up to 16], scales fp32 [...])."""
+    K = x.shape[-1]
+    rows = x if x.dim() == 2 else x.reshape(-1, K)
+    ldx = _rows("x", rows, K, x.device, *_TYPES)
+    pitch = (K + 15) // 16 * 16
+    codes = torch.empty((*x.shape[:-1], pitch), dtype=torch.int8, device=x.device)
+    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    _check(_lib.mok_i8_quantize(rows.data_ptr(), _TYPES[x.dtype], rows.shape[0], K, ldx, codes.data_ptr(), pitch,
+                                scales.data_ptr(), raw_stream))
+    return codes, scales
+
+
+class I8Weights:
+    """8-bit weights with a scale for each output channel: codes int8 [N, K] or [E, N, K] (rows of a multiple of 16 bytes;
+    columns past the activations' K are not read), scales fp32 [N] or [E, N], and max, the largest scale of each matrix
+    (found here if it is not given)."""
+    __slots__ = ("codes", "scales", "max")
+
+    def __init__(self, codes, scales, max=None):
+        self.codes, self.scales = codes, scales
+        self.max = scales.amax(-1) if max is None else max
+
+    @classmethod
+    def quantize(cls, W, stream=None):
+        """From floating-point weights [N, K] or [E, N, K]."""
+        return cls(*mok_i8_quantize(W, stream=stream))
+
+
+def _i8_product(a, weights, N, K, bias, out_dtype, device, raw_stream):
+    a.w_stride = _rows("weights.codes", weights.codes, K, device, torch.int8)
+    a.W_codes = weights.codes.data_ptr()
+    a.W_scales = _packed("weights.scales", weights.scales, (N,), device, torch.float32)
+    if bias is not None:
+        a.bias = _packed("bias", bias, (N,), device, torch.float32)
+    out = torch.empty((a.M, N), dtype=out_dtype, device=device)
+    a.K, a.N, a.out_type = K, N, _TYPES[out_dtype]
+    a.out, a.out_stride, a.stream = out.data_ptr(), N, raw_stream
+    _check(_lib.mok_i8_linear(a))
+    return out
+
+
+@_on_stream
+def mok_i8_linear(x, weights, bias=None, out_dtype=None, workspace=None, *, raw_stream):
+    """out [M, N] = quantise(x [M, K]) W8^T (+ bias): the rows of x are quantised in the call.  weights: I8Weights [N, K];
+    out_dtype defaults to x's.  workspace: a uint8 tensor of mok_i8_linear_workspace_bytes(M, K) + 256 (None: allocated)."""
+    M, K = x.shape
+    a = mok_i8_linear_args()
+    a.x_stride = _rows("x", x, K, x.device, *_TYPES)
+    a.x, a.x_type, a.M = x.data_ptr(), _TYPES[x.dtype], M
+    if workspace is None:
+        workspace = torch.empty(_lib.mok_i8_linear_workspace_bytes(M, K) + 256, dtype=torch.uint8, device=x.device)
+    a.workspace, a.workspace_bytes = _aligned_ws(workspace)
+    return _i8_product(a, weights, weights.codes.shape[0], K, bias, out_dtype or x.dtype, x.device, raw_stream)
+
+
+@_on_stream
+def mok_i8_matmul(codes, scales, weights, K=None, bias=None, out_dtype=torch.bfloat16, *, raw_stream):
+    """out [M, N] from rows that are 8-bit already (mok_i8_quantize): codes int8 [M, >= K], scales fp32 [M]."""
+    M = codes.shape[0]
+    K = weights.codes.shape[1] if K is None else K
+    a = mok_i8_linear_args()
+    a.codes_stride = _rows("codes", codes, K, codes.device, torch.int8)
+    a.x_codes, a.M = codes.data_ptr(), M
+    a.x_scales = _packed("scales", scales, (M,), codes.device, torch.float32)
+    return _i8_product(a, weights, weights.codes.shape[0], K, bias, out_dtype, codes.device, raw_stream)
+
+
+def alloc_i8_workspace(T, H, I, E, k, device="cuda"):
+    """A torch uint8 buffer large enough for mok_i8_experts."""
+    n = int(_lib.mok_i8_experts_workspace_bytes(T, H, I, E, k))
+    if n == 0:
+        raise MokError(MOK_ERR_SHAPE)
+    return torch.empty(n + 256, dtype=torch.uint8, device=device)
+
+
+@_on_stream
+def mok_i8_experts(x, topk_idx, topk_w, gate_up, down, add=None, workspace=None, *, raw_stream):
+    """out [T, H] = add + sum_s topk_w[:, s] f_{topk_idx[:, s]}(x) on 8-bit operands; gate_up: I8Weights [E, 2I, H], down:
+    I8Weights [E, H, I].  Ids outside 0 .. E-1 are not routed."""
+    T, H = x.shape
+    k, E, I, device = topk_idx.shape[1], gate_up.codes.shape[0], gate_up.codes.shape[1] // 2, x.device
+    a = mok_i8_experts_args()
+    a.x_stride = _rows("x", x, H, device, torch.bfloat16, torch.float16)
+    a.x, a.type = x.data_ptr(), _TYPES[x.dtype]
+    a.topk_idx = _packed("topk_idx", topk_idx, (T, k), device, torch.int32)
+    a.topk_w = _packed("topk_w", topk_w, (T, k), device, torch.float32)
+    for name, w, n, width in (("gate_up", gate_up, 2 * I, H), ("down", down, H, I)):
+        if w.codes.dim() != 3 or w.codes.shape[2] < width:
+            raise ValueError(f"{name}.codes: expected [{E}, {n}, >= {width}], got {tuple(w.codes.shape)}")
+        setattr(a, name + "_codes", _packed(name + ".codes", w.codes, (E, n, w.codes.shape[2]), device, torch.int8))
+        setattr(a, name + "_scales", _packed(name + ".scales", w.scales, (E, n), device, torch.float32))
+        setattr(a, name + "_stride", w.codes.shape[2])
+    a.down_max = _packed("down.max", down.max, (E,), device, torch.float32)
+    if add is not None:
+        a.add_stride, a.add = _rows("add", add, H, device, x.dtype), add.data_ptr()
+        if add.shape != x.shape:
+            raise ValueError(f"add: expected {tuple(x.shape)}, got {tuple(add.shape)}")
+    a.T, a.H, a.I, a.E, a.k = T, H, I, E, k
+    if workspace is None:
+        workspace = alloc_i8_workspace(T, H, I, E, k, device)
+    a.workspace, a.workspace_bytes = _aligned_ws(workspace)
+    out = torch.empty((T, H), dtype=x.dtype, device=device)
+    a.out, a.out_stride, a.stream = out.data_ptr(), H, raw_stream
+    _check(_lib.mok_i8_experts(a))
+    return out
+
+
+def mok_i8_linear_workspace_bytes(M, K):
+    return int(_lib.mok_i8_linear_workspace_bytes(M, K))
+
+
+def mok_i8_experts_workspace_bytes(T, H, I, E, k):
+    return int(_lib.mok_i8_experts_workspace_bytes(T, H, I, E, k))
+
+
+def mok_i8_status(stream=None):
+    """Status of the 8-bit products on the current device since it was last read (synchronises the stream)."""
+    return int(_lib.mok_i8_status(_stream(stream)))
 
 
 DEBUG_COUNTERS = ["mma_wait_operands", "mma_wait_peer_operands", "mma_wait_accumulator", "mma_total", "k_blocks",
