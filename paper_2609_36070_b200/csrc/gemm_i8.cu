@@ -5,10 +5,9 @@
 // issued by the even CTA.  Each CTA stages its own 128 rows of A and half of the 256 rows of B (128 bytes of K per stage, 32 KB,
 // six stages), so an SM pulls 32 KB for 256 cycles of MMA; a 128 x 256 tile of one CTA would pull 48 KB for them, and one-byte
 // operands are bound by that rate.
-//   warp 0       TMA producer : B tile and, without a gather, the A tile (128-byte swizzle)
+//   warp 0       TMA producer : A and B tiles (128-byte swizzle)
 //   warp 1       MMA issuer (even CTA)
 //   warps 2..9   epilogue     : warp w drains TMEM lane quadrant w % 4 and one half of the tile's columns
-//   warp 10      gather       : routed rows (GATHER): each lane fetches four token rows with one gathering TMA load
 // Two 256-column accumulators: a tile's epilogue runs beside the next tile's products.
 //
 //   EPI_PLAIN : C = scaled sums (+ bias) as bf16, fp16 or fp32, one rounding
@@ -59,15 +58,13 @@ __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t adesc, uint64_t bd
         "tcgen05.mma.cta_group::2.kind::i8 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
 }
-// Four rows r[0..3] of the tensor, 128 bytes each from byte column c0, to 512 consecutive (swizzled) bytes; completes on the
-// even CTA's barrier.
-__device__ __forceinline__ void tma_gather4_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, const int (&r)[4]) {
-    asm volatile(
-        "{\n\t.reg .b32 rb;\n\t"
-        "mapa.shared::cluster.u32 rb, %2, 0;\n\t"
-        "cp.async.bulk.tensor.2d.shared::cluster.global.tile::gather4.mbarrier::complete_tx::bytes.cta_group::2 "
-        "[%0], [%1, {%3, %4, %5, %6, %7}], [rb];\n\t}"
-        ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+__device__ __forceinline__ void st_shared_f32(uint32_t addr, float v) {
+    asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
+    float4 v;
+    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+    return v;
 }
 
 struct PairTile { int row0, n, e, valid; };     // valid: rows of the segment from row0 on
@@ -148,8 +145,8 @@ __device__ __forceinline__ void store_block(const float (&v)[32], uint32_t slab,
 // 11-bit tanh would move in one case of fifty.
 __device__ __forceinline__ float gated(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
 
-template <int EPI, bool GATHER>
-__global__ void __launch_bounds__(THREADS + (GATHER ? 32 : 0), 1)
+template <int EPI>
+__global__ void __launch_bounds__(THREADS, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
                     const __grid_constant__ ProductArgs a, const int n_nt, const int k_blocks) {
     constexpr bool GATED = EPI == EPI_GATED;
@@ -205,9 +202,9 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                     if (!ok) break;
                     const uint32_t full = smem_u32(&ctrl->full[s]);
                     const uint32_t sa = base + s * STAGE_BYTES, sb = sa + A_BYTES;
-                    // the even CTA's barrier collects the bytes of both CTAs of the pair, gathered rows included
+                    // the even CTA's barrier collects the bytes of both CTAs of the pair
                     if (rank == 0) mbar_expect_tx(full, 2 * STAGE_BYTES);
-                    if (!GATHER) tma_load_2d_peer(sa, &tmapA, full, kb * BKB, t.row0 + rank * BM);
+                    tma_load_2d_peer(sa, &tmapA, full, kb * BKB, t.row0 + rank * BM);
                     tma_load_2d_peer(sb, &tmapB, full, kb * BKB, brow);
                     if (++s == STAGES) { s = 0; ph ^= 1u; }
                 }
@@ -244,29 +241,6 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             }
         }
         __syncwarp();
-    } else if (GATHER && warp == 2 + EPI_WARPS) {
-        // ------------------------------------------------------------------ gather: lane l owns rows 4 l .. 4 l + 3
-        int s = 0;
-        uint32_t ph = 0;
-        for (int L = unit; L < total; L += n_units) {
-            const PairTile t = pair_tile(a, L, n_nt, n_mt);
-            const int tok0 = __ldg(a.row_token + t.row0);
-            int rows[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {        // rows past the segment re-read its first row; they are never stored
-                const int r = rank * BM + lane * 4 + i;
-                rows[i] = r < t.valid ? __ldg(a.row_token + t.row0 + r) : tok0;
-            }
-            bool ok = true;
-            for (int kb = 0; kb < k_blocks; ++kb) {
-                ok = mbar_wait(smem_u32(&ctrl->empty[s]), ph ^ 1u, abort_flag, a.header, 5);
-                ok = __all_sync(0xffffffffu, ok);
-                if (!ok) break;
-                tma_gather4_pair(base + s * STAGE_BYTES + lane * 512, &tmapA, smem_u32(&ctrl->full[s]), kb * BKB, rows);
-                if (++s == STAGES) { s = 0; ph ^= 1u; }
-            }
-            if (!ok) break;
-        }
     } else {
         // ------------------------------------------------------------------ epilogue
         const int quad = warp & 3, half = (warp - 2) >> 2;
@@ -280,58 +254,86 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             const int r0 = rank * BM + quad * 32;                    // first of the warp's rows inside the tile
             const int n_rows = min(32, t.valid - r0);
             float rs = 0.f;
-            if (EPI != EPI_HALF && lane < n_rows) {
-                const int r = t.row0 + r0 + lane;
-                rs = __ldg(a.a_scale + (GATHER ? __ldg(a.row_token + r) : r));
+            if (EPI != EPI_HALF && lane < n_rows) rs = __ldg(a.a_scale + t.row0 + r0 + lane);
+            // the warp's column scales, one column of each piece per lane, on their way while the products finish
+            constexpr int CHUNKS = GATED ? 2 : 4;                    // 32-column pieces of this warp
+            const int first = t.n * (GATED ? BN / 2 : BN) + half * 32 * CHUNKS;
+            const float* bs = a.b_scale + (size_t)t.e * (GATED ? 2 : 1) * a.N;
+            float unit_n = 1.f;
+            if constexpr (EPI == EPI_HALF) {
+                const float top = __ldg(a.b_max + t.e);
+                unit_n = top > 0.f ? a.y_unit / top : 0.f;
+            }
+            float s0[CHUNKS], s1[CHUNKS];                            // s1: up scales, or the bias
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) {
+                const int n = first + c * 32 + lane;
+                s0[c] = n < a.N ? __ldg(bs + n) : 0.f;
+                s1[c] = 0.f;
+                if (GATED && n < a.N) s1[c] = __ldg(bs + a.N + n);
+                if (EPI == EPI_PLAIN && a.bias && n < a.N) s1[c] = __ldg(a.bias + n);
+                if (EPI == EPI_HALF) s0[c] *= unit_n;
             }
             bool ok = mbar_wait(smem_u32(&ctrl->tfull[buf]), aph, abort_flag, a.header, 4);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + (uint32_t)(buf * BN) + ((uint32_t)(quad * 32) << 16);
-            constexpr int CHUNKS = GATED ? 2 : 4;                    // 32-column pieces of this warp
-#pragma unroll 1
+#pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 uint32_t acc[32], up[GATED ? 32 : 1];
-                const int col = GATED ? half * 64 + c * 32 : half * 128 + c * 32;
+                const int col = half * 32 * CHUNKS + c * 32;
                 tc_ld32(taddr + col, acc);
                 if constexpr (GATED) tc_ld32(taddr + BN / 2 + col, up);
+                __syncwarp();                                        // the slab's previous block has been read
+                st_shared_f32(slab + lane * 4, s0[c]);
+                st_shared_f32(slab + 128 + lane * 4, s1[c]);
+                __syncwarp();
                 tc_wait_ld();
                 if (c == CHUNKS - 1) {                               // the accumulator goes back before the last arithmetic
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(smem_u32(&ctrl->tempty[buf]), 0);
                 }
-                if (n_rows <= 0) continue;
-                const int n0 = t.n * (GATED ? BN / 2 : BN) + col;    // first output column of the piece
-                const int n_cols = a.N - n0;
-                if (n_cols <= 0) continue;
-                const float* bs = a.b_scale + (size_t)t.e * (GATED ? 2 : 1) * a.N + n0;
+                const int n0 = first + c * 32, n_cols = a.N - n0;    // first output column of the piece, and how many exist
+                if (n_rows <= 0 || n_cols <= 0) continue;
                 float v[32];
-                if constexpr (EPI == EPI_PLAIN) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int n = i < n_cols ? i : 0;
-                        v[i] = (float)(int)acc[i] * rs * __ldg(bs + n);
-                        if (a.bias) v[i] += __ldg(a.bias + n0 + n);
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 f = ld_shared_f4(slab + i * 4);
+                    if constexpr (EPI == EPI_HALF) {
+                        v[i] = (float)(int)acc[i] * f.x;
+                        v[i + 1] = (float)(int)acc[i + 1] * f.y;
+                        v[i + 2] = (float)(int)acc[i + 2] * f.z;
+                        v[i + 3] = (float)(int)acc[i + 3] * f.w;
+                    } else {
+                        const float4 q = ld_shared_f4(slab + 128 + i * 4);
+                        v[i] = (float)(int)acc[i] * rs * f.x;
+                        v[i + 1] = (float)(int)acc[i + 1] * rs * f.y;
+                        v[i + 2] = (float)(int)acc[i + 2] * rs * f.z;
+                        v[i + 3] = (float)(int)acc[i + 3] * rs * f.w;
+                        if constexpr (GATED) {
+                            v[i] = gated(v[i], (float)(int)up[i] * rs * q.x);
+                            v[i + 1] = gated(v[i + 1], (float)(int)up[i + 1] * rs * q.y);
+                            v[i + 2] = gated(v[i + 2], (float)(int)up[i + 2] * rs * q.z);
+                            v[i + 3] = gated(v[i + 3], (float)(int)up[i + 3] * rs * q.w);
+                        } else {
+                            v[i] += q.x;
+                            v[i + 1] += q.y;
+                            v[i + 2] += q.z;
+                            v[i + 3] += q.w;
+                        }
                     }
-                    const long long at = (long long)(t.row0 + r0) * a.ldc + n0;
+                }
+                const long long at = (long long)(t.row0 + r0) * a.ldc + n0;
+                if constexpr (GATED) {
+                    store_block(v, slab, reinterpret_cast<float*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
+                } else if constexpr (EPI == EPI_HALF) {
+                    store_block(v, slab, reinterpret_cast<__half*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
+                } else {
                     if (a.c_type == MOK_TYPE_F32) store_block(v, slab, reinterpret_cast<float*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
                     else if (a.c_type == MOK_TYPE_F16) store_block(v, slab, reinterpret_cast<__half*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
                     else store_block(v, slab, reinterpret_cast<__nv_bfloat16*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
-                } else if constexpr (GATED) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int n = i < n_cols ? i : 0;
-                        v[i] = gated((float)(int)acc[i] * rs * __ldg(bs + n), (float)(int)up[i] * rs * __ldg(bs + a.N + n));
-                    }
-                    store_block(v, slab, reinterpret_cast<float*>(a.C) + (long long)(t.row0 + r0) * a.ldc + n0, a.ldc, n_rows, n_cols, vec, lane);
-                } else {
-                    const float top = __ldg(a.b_max + t.e);
-                    const float unit_n = top > 0.f ? a.y_unit / top : 0.f;
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = (float)(int)acc[i] * (__ldg(bs + (i < n_cols ? i : 0)) * unit_n);
-                    store_block(v, slab, reinterpret_cast<__half*>(a.C) + (long long)(t.row0 + r0) * a.ldc + n0, a.ldc, n_rows, n_cols, vec, lane);
                 }
             }
             if (++buf == 2) { buf = 0; aph ^= 1u; }
@@ -376,11 +378,11 @@ static bool byte_map(CUtensorMap* m, const void* ptr, long long rows, int cols, 
                            CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
-template <int EPI, bool GATHER>
+template <int EPI>
 static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, const ProductArgs& a, int n_nt, int k_blocks,
                                long long tiles, cudaStream_t s) {
     static PerDevice configured;                 // per device: CTA pairs that run at once
-    auto kernel = product_pair_kernel<EPI, GATHER>;
+    auto kernel = product_pair_kernel<EPI>;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -389,7 +391,7 @@ static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, con
     attr[0].val.clusterDim.z = 1;
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.blockDim = dim3(THREADS + (GATHER ? 32 : 0));
+    cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = SMEM_BYTES;
     cfg.stream = s;
     cfg.attrs = attr;
@@ -415,20 +417,18 @@ static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, con
 }
 
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s) {
-    const bool gated = epi == EPI_GATED, gather = a.row_token != nullptr;
+    const bool gated = epi == EPI_GATED;
     CUtensorMap mA, mB;
-    // a gathering load addresses single rows: its box is one row high
-    if (!byte_map(&mA, a.A, a.a_rows, a.K, a.lda, gather ? 1 : BM) ||
+    if (!byte_map(&mA, a.A, a.a_rows, a.K, a.lda, BM) ||
         !byte_map(&mB, a.B, (long long)a.E * (gated ? 2 : 1) * a.N, a.K, a.ldb, BN / 2))
         return cudaErrorInvalidValue;
     const int n_nt = gated ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + BN - 1) / BN;
     const int k_blocks = (a.K + BKB - 1) / BKB;
     const long long tiles = (a.dense_rows > 0 ? (a.dense_rows + 2 * BM - 1) / (2 * BM) : a.max_mt) * (long long)n_nt;
     if (tiles <= 0 || tiles > 0x7fffffffll) return cudaErrorInvalidValue;
-    if (epi == EPI_PLAIN && !gather) return launch_pair<EPI_PLAIN, false>(mA, mB, a, n_nt, k_blocks, tiles, s);
-    if (gated && gather) return launch_pair<EPI_GATED, true>(mA, mB, a, n_nt, k_blocks, tiles, s);
-    if (epi == EPI_HALF && !gather) return launch_pair<EPI_HALF, false>(mA, mB, a, n_nt, k_blocks, tiles, s);
-    return cudaErrorInvalidValue;
+    if (epi == EPI_PLAIN) return launch_pair<EPI_PLAIN>(mA, mB, a, n_nt, k_blocks, tiles, s);
+    if (gated) return launch_pair<EPI_GATED>(mA, mB, a, n_nt, k_blocks, tiles, s);
+    return launch_pair<EPI_HALF>(mA, mB, a, n_nt, k_blocks, tiles, s);
 }
 
 }  // namespace i8

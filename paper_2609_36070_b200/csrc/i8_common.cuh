@@ -41,7 +41,7 @@ inline int pitch_of(int K) { return (K + 15) / 16 * 16; }
 
 // One product launch.  Rows live in the padded space of the schedule (grouped) or are 0 .. dense_rows - 1.
 struct ProductArgs {
-    const int8_t* A;             // codes [a_rows, K], lda bytes apart; with row_token set, gathered through it
+    const int8_t* A;             // codes [a_rows, K], lda bytes apart
     const int8_t* B;             // codes [E * (swiglu ? 2 : 1) * N, K], ldb bytes apart
     long long lda, ldb, a_rows;
     int32_t K, N, E;
@@ -54,7 +54,6 @@ struct ProductArgs {
     float y_unit;                // EPI_HALF: power of two that brings |sum| <= 127 * 127 * K below 65504
     const float* bias;           // [N] or NULL (plain)
     int32_t dense_rows;          // > 0: dense
-    const int32_t* row_token;
     const int32_t* counts;
     const int32_t* pad_offsets;
     const int32_t* n_mtiles;     // 256-row tile table
@@ -65,8 +64,14 @@ struct ProductArgs {
 };
 enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
 
+// Where a token's codes go when its rows are wanted in expert order: row pos[t * k + s] for every routed slot s.
+struct RouteArgs {
+    const int32_t* idx;
+    const int32_t* pos;
+    int32_t E, k;
+};
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
-                            float* scales, cudaStream_t s);
+                            float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s);
 cudaError_t status_header(WsHeader** out);
 

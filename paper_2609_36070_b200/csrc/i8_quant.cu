@@ -21,11 +21,30 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* s_max) {
     return v;
 }
 
+// The rows that a quantised row is written to: itself, or with ROUTED one per routed slot of the token.
+template <bool ROUTED>
+struct Targets {
+    long long first;
+    const int32_t *idx, *pos;
+    int E, n;
+    __device__ __forceinline__ Targets(long long r, const RouteArgs& q) : first(r), idx(nullptr), pos(nullptr), E(q.E), n(1) {
+        if (ROUTED) {
+            n = q.k;
+            idx = q.idx + r * q.k;
+            pos = q.pos + r * q.k;
+        }
+    }
+    __device__ __forceinline__ long long row(int s) const {          // -1: the slot is not routed
+        if (!ROUTED) return first;
+        return (unsigned)__ldg(idx + s) < (unsigned)E ? (long long)__ldg(pos + s) : -1;
+    }
+};
+
 // Rows of whole 16-byte pieces that fit into the registers of their threads: one pass over memory.
-template <class T, int TPR>
+template <class T, int TPR, bool ROUTED>
 __global__ void __launch_bounds__(THREADS)
 quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ldx, int8_t* __restrict__ codes, long long ldc,
-                    float* __restrict__ scales) {
+                    float* __restrict__ scales, const RouteArgs routes) {
     constexpr int PER = 16 / sizeof(T);
     __shared__ uint32_t s_max[THREADS / 32];
     pdl_enter();
@@ -54,33 +73,41 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
         const float amax = __uint_as_float(m);
         const bool codable = m > 0 && finite_bits(m);
         const RowRule rule = row_rule(amax);
-        int8_t* dst = codes + r * ldc;
+        uint32_t o[VEC_PER_THREAD][PER / 4];
 #pragma unroll
         for (int i = 0; i < VEC_PER_THREAD; ++i) {
-            const int c = sub + i * TPR;
-            if (c >= pieces) break;
             const T* v = reinterpret_cast<const T*>(&raw[i]);
-            uint32_t o[PER / 4];
 #pragma unroll
             for (int q = 0; q < PER / 4; ++q) {
-                o[q] = 0u;
-                if (codable)
-                    o[q] = pack4(code_bits(to_f(v[4 * q]), rule), code_bits(to_f(v[4 * q + 1]), rule),
-                                 code_bits(to_f(v[4 * q + 2]), rule), code_bits(to_f(v[4 * q + 3]), rule));
+                o[i][q] = 0u;
+                if (codable && sub + i * TPR < pieces)
+                    o[i][q] = pack4(code_bits(to_f(v[4 * q]), rule), code_bits(to_f(v[4 * q + 1]), rule),
+                                    code_bits(to_f(v[4 * q + 2]), rule), code_bits(to_f(v[4 * q + 3]), rule));
             }
-            if (PER == 8) *reinterpret_cast<uint2*>(dst + c * 8) = make_uint2(o[0], o[PER / 4 - 1]);
-            else *reinterpret_cast<uint32_t*>(dst + c * 4) = o[0];
         }
-        if (sub == 0) scales[r] = amax / 127.f;
-        for (int c = K + sub; c < ldc && c < K + 16; c += TPR) dst[c] = 0;     // the pitch's tail
+        const Targets<ROUTED> to(r, routes);
+        for (int s = 0; s < to.n; ++s) {
+            const long long row = to.row(s);
+            if (row < 0) continue;
+            int8_t* dst = codes + row * ldc;
+#pragma unroll
+            for (int i = 0; i < VEC_PER_THREAD; ++i) {
+                const int c = sub + i * TPR;
+                if (c >= pieces) break;
+                if (PER == 8) *reinterpret_cast<uint2*>(dst + c * 8) = make_uint2(o[i][0], o[i][PER / 4 - 1]);
+                else *reinterpret_cast<uint32_t*>(dst + c * 4) = o[i][0];
+            }
+            if (sub == 0) scales[row] = amax / 127.f;
+            for (int c = K + sub; c < ldc && c < K + 16; c += TPR) dst[c] = 0;     // the pitch's tail
+        }
     }
 }
 
 // Any length, stride and alignment: one block per row, two passes (the second one hits the caches).
-template <class T>
+template <class T, bool ROUTED>
 __global__ void __launch_bounds__(THREADS)
 quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ldx, int8_t* __restrict__ codes, long long ldc,
-                    float* __restrict__ scales) {
+                    float* __restrict__ scales, const RouteArgs routes) {
     __shared__ uint32_t s_max[THREADS / 32];
     pdl_enter();
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
@@ -91,37 +118,49 @@ quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ld
         const float amax = __uint_as_float(m);
         const bool codable = m > 0 && finite_bits(m);
         const RowRule rule = row_rule(amax);
-        int8_t* dst = codes + r * ldc;
-        for (int c = threadIdx.x; c < K; c += THREADS)
-            dst[c] = codable ? (int8_t)(code_bits(to_f(src[c]), rule) & 0xffu) : (int8_t)0;
-        if (threadIdx.x == 0) scales[r] = amax / 127.f;
-        for (int c = K + threadIdx.x; c < ldc && c < K + 16; c += THREADS) dst[c] = 0;
+        const Targets<ROUTED> to(r, routes);
+        for (int s = 0; s < to.n; ++s) {
+            const long long row = to.row(s);
+            if (row < 0) continue;
+            int8_t* dst = codes + row * ldc;
+            for (int c = threadIdx.x; c < K; c += THREADS)
+                dst[c] = codable ? (int8_t)(code_bits(to_f(src[c]), rule) & 0xffu) : (int8_t)0;
+            if (threadIdx.x == 0) scales[row] = amax / 127.f;
+            for (int c = K + threadIdx.x; c < ldc && c < K + 16; c += THREADS) dst[c] = 0;
+        }
     }
 }
 
-template <class T>
-static cudaError_t launch_typed(const T* x, long long rows, int K, long long ldx, int8_t* codes, long long ldc, float* scales,
-                                cudaStream_t s) {
+template <class T, bool ROUTED>
+static cudaError_t launch_typed(const void* xv, long long rows, int K, long long ldx, int8_t* codes, long long ldc, float* scales,
+                                const RouteArgs& routes, cudaStream_t s) {
     constexpr int PER = 16 / sizeof(T);
+    const T* x = reinterpret_cast<const T*>(xv);
+    const bool one = rows == 1 && !ROUTED;
     const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && K % PER == 0 && (ldx % PER == 0 || rows == 1) &&
-                     (reinterpret_cast<uintptr_t>(codes) & 15u) == 0 && (ldc % 16 == 0 || rows == 1);
+                     (reinterpret_cast<uintptr_t>(codes) & 15u) == 0 && (ldc % 16 == 0 || one);
     const long long most = 148 * 16;
     if (vec && K <= 32 * VEC_PER_THREAD * PER && rows >= 148 * 8) {      // enough rows for a warp each
-        long long blocks = (rows + 7) / 8;
-        return launch_pdl(quantize_vec_kernel<T, 32>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0, s, x,
-                          rows, K, ldx, codes, ldc, scales);
+        const long long blocks = (rows + 7) / 8;
+        return launch_pdl(quantize_vec_kernel<T, 32, ROUTED>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0, s,
+                          x, rows, K, ldx, codes, ldc, scales, routes);
     }
     const dim3 grid((unsigned)(rows < most ? rows : most));
     if (vec && K <= THREADS * VEC_PER_THREAD * PER)
-        return launch_pdl(quantize_vec_kernel<T, THREADS>, grid, dim3(THREADS), 0, s, x, rows, K, ldx, codes, ldc, scales);
-    return launch_pdl(quantize_any_kernel<T>, grid, dim3(THREADS), 0, s, x, rows, K, ldx, codes, ldc, scales);
+        return launch_pdl(quantize_vec_kernel<T, THREADS, ROUTED>, grid, dim3(THREADS), 0, s, x, rows, K, ldx, codes, ldc, scales,
+                          routes);
+    return launch_pdl(quantize_any_kernel<T, ROUTED>, grid, dim3(THREADS), 0, s, x, rows, K, ldx, codes, ldc, scales, routes);
 }
 
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
-                            float* scales, cudaStream_t s) {
-    if (type == MOK_TYPE_F32) return launch_typed(reinterpret_cast<const float*>(x), rows, K, ldx, codes, ldc, scales, s);
-    if (type == MOK_TYPE_F16) return launch_typed(reinterpret_cast<const __half*>(x), rows, K, ldx, codes, ldc, scales, s);
-    return launch_typed(reinterpret_cast<const __nv_bfloat16*>(x), rows, K, ldx, codes, ldc, scales, s);
+                            float* scales, cudaStream_t s, const RouteArgs* routes) {
+    if (routes)          // (16-bit activations only)
+        return type == MOK_TYPE_F16 ? launch_typed<__half, true>(x, rows, K, ldx, codes, ldc, scales, *routes, s)
+                                    : launch_typed<__nv_bfloat16, true>(x, rows, K, ldx, codes, ldc, scales, *routes, s);
+    const RouteArgs none = {};
+    if (type == MOK_TYPE_F32) return launch_typed<float, false>(x, rows, K, ldx, codes, ldc, scales, none, s);
+    if (type == MOK_TYPE_F16) return launch_typed<__half, false>(x, rows, K, ldx, codes, ldc, scales, none, s);
+    return launch_typed<__nv_bfloat16, false>(x, rows, K, ldx, codes, ldc, scales, none, s);
 }
 
 }  // namespace i8

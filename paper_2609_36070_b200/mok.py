@@ -6,6 +6,7 @@ device memory and streams.  Importing this module fails loudly if the library ha
 """
 import ctypes
 import functools
+import inspect
 import os
 
 import torch
@@ -716,7 +717,12 @@ def mok_moe_backward(x, W_gate_up, W_down, W_shared_gate_up, W_shared_down, topk
 
 
 _TYPES = {torch.bfloat16: MOK_TYPE_BF16, torch.float16: MOK_TYPE_F16, torch.float32: MOK_TYPE_F32}
+_HALVES, _INT8 = (torch.bfloat16, torch.float16), (torch.int8,)
 _SCORES = {"softmax": MOK_SCORE_SOFTMAX, "sigmoid": MOK_SCORE_SIGMOID}
+
+
+_current_device = torch._C._cuda_getDevice                 # (torch.cuda.current_device / current_stream without their checks:
+_raw_stream = torch._C._cuda_getCurrentRawStream           #  a third of the host time of a small call)
 
 
 def _on_stream(call):
@@ -724,25 +730,31 @@ def _on_stream(call):
     outputs and scratch that it allocates belong to the stream that writes them."""
     @functools.wraps(call)
     def wrapped(first, *args, stream=None, **kwargs):
-        device = first.device
-        if device.type != "cuda":
-            raise ValueError(f"{call.__name__}: tensors have to be on a CUDA device, got {device}")
-        if stream is None and device.index == torch.cuda.current_device():
-            return call(first, *args, raw_stream=torch.cuda.current_stream().cuda_stream, **kwargs)
+        device = first.get_device()
+        if device < 0:
+            raise ValueError(f"{call.__name__}: tensors have to be on a CUDA device, got {first.device}")
+        if stream is None and device == _current_device():
+            return call(_raw_stream(device), first, *args, **kwargs)
         with torch.cuda.device(device):
             if stream is None:
-                stream = torch.cuda.current_stream()
+                return call(_raw_stream(device), first, *args, **kwargs)
             with torch.cuda.stream(stream):
-                return call(first, *args, raw_stream=stream.cuda_stream, **kwargs)
+                return call(stream.cuda_stream, first, *args, **kwargs)
+    sig = inspect.signature(call)                          # what a caller sees: the tensor first, stream= last
+    first, *rest = list(sig.parameters.values())[1:]
+    wrapped.__signature__ = sig.replace(parameters=[
+        first.replace(kind=inspect.Parameter.POSITIONAL_ONLY), *rest,
+        inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
     return wrapped
 
 
-def _rows(name, t, width, device, *dtypes):
+def _rows(name, t, width, device, dtypes):
     """Checks a matrix argument [rows, width] whose last index is contiguous; returns the elements between its rows."""
-    if t.dim() != 2 or t.shape[1] < width or t.dtype not in dtypes or t.device != device or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name}: expected rows of {width} contiguous elements of {dtypes} on {device}, got shape "
-                         f"{tuple(t.shape)}, strides {t.stride()}, {t.dtype} on {t.device}")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or shape[1] < width or t.dtype not in dtypes or t.device != device or (strides[1] != 1 and shape[1] > 1):
+        raise ValueError(f"{name}: expected rows of {width} contiguous elements of {tuple(dtypes)} on {device}, got shape "
+                         f"{tuple(shape)}, strides {strides}, {t.dtype} on {t.device}")
+    return strides[0] if shape[0] > 1 else shape[1]
 
 
 def _packed(name, t, shape, device, dtype):
@@ -754,48 +766,40 @@ def _packed(name, t, shape, device, dtype):
 
 
 @_on_stream
-def mok_gate(logits, k, bias=None, score="softmax", n_groups=1, topk_groups=1, group_top=2, renormalise=True, scale=1.0, *,
-             raw_stream):
+def mok_gate(raw_stream, logits, k, bias=None, score="softmax", n_groups=1, topk_groups=1, group_top=2, renormalise=True, scale=1.0):
     """Routing from logits [T, E] (bf16, fp16 or fp32): returns (topk_idx int32 [T, k], topk_w fp32 [T, k]).  score:
     "softmax" or "sigmoid"; bias fp32 [E] takes part in the selection only; see include/mok.h for groups and weights."""
-    T, E = logits.shape
-    a = mok_gate_args()
-    a.logits_stride = _rows("logits", logits, E, logits.device, *_TYPES)
-    a.logits, a.logits_type = logits.data_ptr(), _TYPES[logits.dtype]
-    if bias is not None:
-        a.bias = _packed("bias", bias, (E,), logits.device, torch.float32)
-    a.T, a.E, a.k, a.score, a.n_groups, a.topk_groups, a.group_top = T, E, k, _SCORES[score], n_groups, topk_groups, group_top
-    a.renormalise, a.scale, a.stream = bool(renormalise), scale, raw_stream
-    idx = torch.empty((T, k), dtype=torch.int32, device=logits.device)
-    w = torch.empty((T, k), dtype=torch.float32, device=logits.device)
-    a.topk_idx, a.topk_w = idx.data_ptr(), w.data_ptr()
-    _check(_lib.mok_gate(a))
+    (T, E), device = logits.shape, logits.device
+    ld = _rows("logits", logits, E, device, _TYPES)
+    idx = torch.empty((T, k), dtype=torch.int32, device=device)
+    w = torch.empty((T, k), dtype=torch.float32, device=device)
+    _check(_lib.mok_gate(mok_gate_args(
+        logits.data_ptr(), None if bias is None else _packed("bias", bias, (E,), device, torch.float32), ld, T, E, k,
+        _TYPES[logits.dtype], _SCORES[score], n_groups, topk_groups, group_top, bool(renormalise), scale, idx.data_ptr(),
+        w.data_ptr(), raw_stream)))
     return idx, w
 
 
 @_on_stream
-def mok_gate_backward(logits, topk_idx, dw, score="softmax", renormalise=True, scale=1.0, *, raw_stream):
+def mok_gate_backward(raw_stream, logits, topk_idx, dw, score="softmax", renormalise=True, scale=1.0):
     """dL/dlogits [T, E] (in the logits' type) from dL/dtopk_w (dw) and the chosen experts of mok_gate."""
-    T, E = logits.shape
-    k = topk_idx.shape[1]
-    a = mok_gate_bwd_args()
-    a.logits_stride = _rows("logits", logits, E, logits.device, *_TYPES)
-    a.logits, a.logits_type = logits.data_ptr(), _TYPES[logits.dtype]
-    a.topk_idx = _packed("topk_idx", topk_idx, (T, k), logits.device, torch.int32)
-    a.dw = _packed("dw", dw, (T, k), logits.device, torch.float32)
-    a.T, a.E, a.k, a.score, a.renormalise, a.scale = T, E, k, _SCORES[score], bool(renormalise), scale
-    out = torch.empty((T, E), dtype=logits.dtype, device=logits.device)
-    a.dlogits, a.dlogits_stride, a.stream = out.data_ptr(), E, raw_stream
-    _check(_lib.mok_gate_backward(a))
+    (T, E), device = logits.shape, logits.device
+    k = topk_idx.shape[-1]
+    ld = _rows("logits", logits, E, device, _TYPES)
+    out = torch.empty((T, E), dtype=logits.dtype, device=device)
+    _check(_lib.mok_gate_backward(mok_gate_bwd_args(
+        logits.data_ptr(), _packed("topk_idx", topk_idx, (T, k), device, torch.int32),
+        _packed("dw", dw, (T, k), device, torch.float32), ld, E, T, E, k, _TYPES[logits.dtype], _SCORES[score],
+        bool(renormalise), scale, out.data_ptr(), raw_stream)))
     return out
 
 
 @_on_stream
-def mok_i8_quantize(x, *, raw_stream):
+def mok_i8_quantize(raw_stream, x):
     """Rows of x [..., K] (bf16, fp16 or fp32) -> (codes int8 [..., K rounded up to 16], scales fp32 [...])."""
     K = x.shape[-1]
     rows = x if x.dim() == 2 else x.reshape(-1, K)
-    ldx = _rows("x", rows, K, x.device, *_TYPES)
+    ldx = _rows("x", rows, K, x.device, _TYPES)
     pitch = (K + 15) // 16 * 16
     codes = torch.empty((*x.shape[:-1], pitch), dtype=torch.int8, device=x.device)
     scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
@@ -812,7 +816,7 @@ class I8Weights:
 
     def __init__(self, codes, scales, max=None):
         self.codes, self.scales = codes, scales
-        self.max = scales.amax(-1) if max is None else max
+        self.max = scales.amax(-1) if max is None and codes.dim() == 3 else max
 
     @classmethod
     def quantize(cls, W, stream=None):
@@ -820,43 +824,40 @@ class I8Weights:
         return cls(*mok_i8_quantize(W, stream=stream))
 
 
-def _i8_product(a, weights, N, K, bias, out_dtype, device, raw_stream):
-    a.w_stride = _rows("weights.codes", weights.codes, K, device, torch.int8)
-    a.W_codes = weights.codes.data_ptr()
-    a.W_scales = _packed("weights.scales", weights.scales, (N,), device, torch.float32)
-    if bias is not None:
-        a.bias = _packed("bias", bias, (N,), device, torch.float32)
-    out = torch.empty((a.M, N), dtype=out_dtype, device=device)
-    a.K, a.N, a.out_type = K, N, _TYPES[out_dtype]
-    a.out, a.out_stride, a.stream = out.data_ptr(), N, raw_stream
-    _check(_lib.mok_i8_linear(a))
+def _i8_product(x, x_codes, x_scales, x_stride, codes_stride, M, K, x_type, weights, bias, out_dtype, workspace,
+                workspace_bytes, device, raw_stream):
+    W = weights.codes
+    N = W.shape[0]
+    w_stride = _rows("weights.codes", W, K, device, _INT8)
+    out = torch.empty((M, N), dtype=out_dtype, device=device)
+    _check(_lib.mok_i8_linear(mok_i8_linear_args(
+        x, x_codes, x_scales, W.data_ptr(), _packed("weights.scales", weights.scales, (N,), device, torch.float32),
+        None if bias is None else _packed("bias", bias, (N,), device, torch.float32), x_stride, codes_stride, w_stride, N,
+        M, K, N, x_type, _TYPES[out_dtype], out.data_ptr(), workspace, workspace_bytes, raw_stream)))
     return out
 
 
 @_on_stream
-def mok_i8_linear(x, weights, bias=None, out_dtype=None, workspace=None, *, raw_stream):
+def mok_i8_linear(raw_stream, x, weights, bias=None, out_dtype=None, workspace=None):
     """out [M, N] = quantise(x [M, K]) W8^T (+ bias): the rows of x are quantised in the call.  weights: I8Weights [N, K];
     out_dtype defaults to x's.  workspace: a uint8 tensor of mok_i8_linear_workspace_bytes(M, K) + 256 (None: allocated)."""
-    M, K = x.shape
-    a = mok_i8_linear_args()
-    a.x_stride = _rows("x", x, K, x.device, *_TYPES)
-    a.x, a.x_type, a.M = x.data_ptr(), _TYPES[x.dtype], M
+    (M, K), device, dtype = x.shape, x.device, x.dtype
+    ldx = _rows("x", x, K, device, _TYPES)
     if workspace is None:
-        workspace = torch.empty(_lib.mok_i8_linear_workspace_bytes(M, K) + 256, dtype=torch.uint8, device=x.device)
-    a.workspace, a.workspace_bytes = _aligned_ws(workspace)
-    return _i8_product(a, weights, weights.codes.shape[0], K, bias, out_dtype or x.dtype, x.device, raw_stream)
+        workspace = torch.empty(_lib.mok_i8_linear_workspace_bytes(M, K), dtype=torch.uint8, device=device)
+    ws, ws_bytes = _aligned_ws(workspace)
+    return _i8_product(x.data_ptr(), None, None, ldx, 0, M, K, _TYPES[dtype], weights, bias, out_dtype or dtype, ws, ws_bytes,
+                       device, raw_stream)
 
 
 @_on_stream
-def mok_i8_matmul(codes, scales, weights, K=None, bias=None, out_dtype=torch.bfloat16, *, raw_stream):
+def mok_i8_matmul(raw_stream, codes, scales, weights, K=None, bias=None, out_dtype=torch.bfloat16):
     """out [M, N] from rows that are 8-bit already (mok_i8_quantize): codes int8 [M, >= K], scales fp32 [M]."""
-    M = codes.shape[0]
+    M, device = codes.shape[0], codes.device
     K = weights.codes.shape[1] if K is None else K
-    a = mok_i8_linear_args()
-    a.codes_stride = _rows("codes", codes, K, codes.device, torch.int8)
-    a.x_codes, a.M = codes.data_ptr(), M
-    a.x_scales = _packed("scales", scales, (M,), codes.device, torch.float32)
-    return _i8_product(a, weights, weights.codes.shape[0], K, bias, out_dtype, codes.device, raw_stream)
+    ldc = _rows("codes", codes, K, device, _INT8)
+    return _i8_product(None, codes.data_ptr(), _packed("scales", scales, (M,), device, torch.float32), 0, ldc, M, K, 0, weights,
+                       bias, out_dtype, None, 0, device, raw_stream)
 
 
 def alloc_i8_workspace(T, H, I, E, k, device="cuda"):
@@ -867,35 +868,38 @@ def alloc_i8_workspace(T, H, I, E, k, device="cuda"):
     return torch.empty(n + 256, dtype=torch.uint8, device=device)
 
 
+def _expert_weights(name, w, E, n, width, device):
+    """Addresses of a stack of 8-bit matrices [E, n, >= width] and of its scales, and its row pitch."""
+    pitch = w.codes.shape[-1]
+    if pitch < width:
+        raise ValueError(f"{name}.codes: expected [{E}, {n}, >= {width}], got {tuple(w.codes.shape)}")
+    return (_packed(name + ".codes", w.codes, (E, n, pitch), device, torch.int8),
+            _packed(name + ".scales", w.scales, (E, n), device, torch.float32), pitch)
+
+
 @_on_stream
-def mok_i8_experts(x, topk_idx, topk_w, gate_up, down, add=None, workspace=None, *, raw_stream):
+def mok_i8_experts(raw_stream, x, topk_idx, topk_w, gate_up, down, add=None, workspace=None):
     """out [T, H] = add + sum_s topk_w[:, s] f_{topk_idx[:, s]}(x) on 8-bit operands; gate_up: I8Weights [E, 2I, H], down:
-    I8Weights [E, H, I].  Ids outside 0 .. E-1 are not routed."""
-    T, H = x.shape
-    k, E, I, device = topk_idx.shape[1], gate_up.codes.shape[0], gate_up.codes.shape[1] // 2, x.device
-    a = mok_i8_experts_args()
-    a.x_stride = _rows("x", x, H, device, torch.bfloat16, torch.float16)
-    a.x, a.type = x.data_ptr(), _TYPES[x.dtype]
-    a.topk_idx = _packed("topk_idx", topk_idx, (T, k), device, torch.int32)
-    a.topk_w = _packed("topk_w", topk_w, (T, k), device, torch.float32)
-    for name, w, n, width in (("gate_up", gate_up, 2 * I, H), ("down", down, H, I)):
-        if w.codes.dim() != 3 or w.codes.shape[2] < width:
-            raise ValueError(f"{name}.codes: expected [{E}, {n}, >= {width}], got {tuple(w.codes.shape)}")
-        setattr(a, name + "_codes", _packed(name + ".codes", w.codes, (E, n, w.codes.shape[2]), device, torch.int8))
-        setattr(a, name + "_scales", _packed(name + ".scales", w.scales, (E, n), device, torch.float32))
-        setattr(a, name + "_stride", w.codes.shape[2])
-    a.down_max = _packed("down.max", down.max, (E,), device, torch.float32)
+    I8Weights [E, H, I].  Ids outside 0 .. E-1 are not routed.  workspace: from alloc_i8_workspace (None: allocated)."""
+    (T, H), device, dtype = x.shape, x.device, x.dtype
+    k, E, I = topk_idx.shape[-1], gate_up.codes.shape[0], gate_up.codes.shape[-2] // 2
+    ldx = _rows("x", x, H, device, _HALVES)
+    gu, gu_scales, gu_pitch = _expert_weights("gate_up", gate_up, E, 2 * I, H, device)
+    dn, dn_scales, dn_pitch = _expert_weights("down", down, E, H, I, device)
+    ld_add = 0
     if add is not None:
-        a.add_stride, a.add = _rows("add", add, H, device, x.dtype), add.data_ptr()
+        ld_add = _rows("add", add, H, device, (dtype,))
         if add.shape != x.shape:
             raise ValueError(f"add: expected {tuple(x.shape)}, got {tuple(add.shape)}")
-    a.T, a.H, a.I, a.E, a.k = T, H, I, E, k
     if workspace is None:
-        workspace = alloc_i8_workspace(T, H, I, E, k, device)
-    a.workspace, a.workspace_bytes = _aligned_ws(workspace)
-    out = torch.empty((T, H), dtype=x.dtype, device=device)
-    a.out, a.out_stride, a.stream = out.data_ptr(), H, raw_stream
-    _check(_lib.mok_i8_experts(a))
+        workspace = torch.empty(_lib.mok_i8_experts_workspace_bytes(T, H, I, E, k), dtype=torch.uint8, device=device)
+    ws, ws_bytes = _aligned_ws(workspace)
+    out = torch.empty((T, H), dtype=dtype, device=device)
+    _check(_lib.mok_i8_experts(mok_i8_experts_args(
+        x.data_ptr(), _packed("topk_idx", topk_idx, (T, k), device, torch.int32),
+        _packed("topk_w", topk_w, (T, k), device, torch.float32), gu, gu_scales, dn, dn_scales,
+        _packed("down.max", down.max, (E,), device, torch.float32), None if add is None else add.data_ptr(),
+        ldx, gu_pitch, dn_pitch, ld_add, H, T, H, I, E, k, _TYPES[dtype], out.data_ptr(), ws, ws_bytes, raw_stream)))
     return out
 
 
