@@ -32,10 +32,11 @@ constexpr int BM = 128, BN = 256, BKB = 128;
 constexpr int A_BYTES = BM * BKB, B_BYTES = BN / 2 * BKB, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr int STAGES = 6;
 constexpr int EPI_WARPS = 8;
-constexpr int SLAB_BYTES = 4096;                 // per epilogue warp: 32 rows x 32 columns of up to four bytes
+constexpr int SLAB_BYTES = 2048;                 // 32 rows of 64 bytes; two per epilogue warp
 constexpr int SLAB_REGION = STAGES * STAGE_BYTES;
-constexpr int CTRL_REGION = SLAB_REGION + EPI_WARPS * SLAB_BYTES;
-constexpr int SMEM_BYTES = CTRL_REGION + 256 + 1024;
+constexpr int SCALE_REGION = SLAB_REGION + EPI_WARPS * 2 * SLAB_BYTES;      // per epilogue warp: 2 x 32 column factors
+constexpr int CTRL_REGION = SCALE_REGION + EPI_WARPS * 256;
+constexpr int SMEM_BYTES = CTRL_REGION + 256;
 constexpr int TMEM_COLS = 512;
 constexpr int THREADS = 64 + 32 * EPI_WARPS;     // + one gather warp
 constexpr int GROUP_ROWS = 2048;
@@ -71,72 +72,102 @@ struct PairTile { int row0, n, e, valid; };     // valid: rows of the segment fr
 
 __device__ __forceinline__ PairTile pair_tile(const ProductArgs& a, int L, int n_nt, int n_mt) {
     PairTile t;
-    int mt0 = 0, m_cnt = n_mt, pad0 = 0, rows = a.dense_rows;
-    t.e = 0;
     if (a.dense_rows <= 0) {
-        t.e = __ldg(a.tile_expert + L / n_nt);
-        mt0 = __ldg(a.mt_start + t.e);
-        m_cnt = __ldg(a.mt_start + t.e + 1) - mt0;
-        pad0 = __ldg(a.pad_offsets + t.e);
-        rows = __ldg(a.counts + t.e);
+        // one load from the tile list: a chain of look-ups (expert, first tile, offset) costs as much as a short tile's products
+        const int q = L / n_nt;
+        const int4 d = __ldg(a.tiles + q);
+        t.row0 = d.x; t.valid = d.y; t.e = d.z;
+        t.n = L - q * n_nt;
+        return t;
     }
     // row tiles in groups of GROUP_ROWS rows, fastest inside a group: its rows stay in L2 while the weight tiles stream
     constexpr int group_m = GROUP_ROWS / (2 * BM);
-    const int r = L - n_nt * mt0;
-    const int g = r / (group_m * n_nt);
-    const int rem = r - g * group_m * n_nt;
-    const int in_group = min(group_m, m_cnt - g * group_m);
+    const int g = L / (group_m * n_nt);
+    const int rem = L - g * group_m * n_nt;
+    const int in_group = min(group_m, n_mt - g * group_m);
+    t.e = 0;
     t.n = rem / in_group;
-    const int m = g * group_m + (rem - t.n * in_group);
-    t.row0 = pad0 + m * 2 * BM;
-    t.valid = rows - m * 2 * BM;
+    t.row0 = (g * group_m + rem - t.n * in_group) * 2 * BM;
+    t.valid = a.dense_rows - t.row0;
     return t;
 }
 
 template <class T> struct Pack;
 template <> struct Pack<__nv_bfloat16> {
     static __device__ __forceinline__ uint32_t two(float a, float b) { return pack_bf16(a, b); }
+    static __device__ __forceinline__ __nv_bfloat16 one(float a) { return __float2bfloat16_rn(a); }
+};
+template <> struct Pack<float> {
+    static __device__ __forceinline__ float one(float a) { return a; }
 };
 template <> struct Pack<__half> {
     static __device__ __forceinline__ uint32_t two(float a, float b) {
         const __half2 h = __floats2half2_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
+    static __device__ __forceinline__ __half one(float a) { return __float2half_rn(a); }
 };
 
-// Writes a warp's 32 rows x 32 columns (lane = row, v = its columns) to C through the warp's slab, so that a store
-// instruction covers whole row segments.  n_rows, n_cols: how many of them exist.
+// Puts 32 rows (lane = row) of 64 bytes into a slab, in the 64-byte swizzle of the tensor map that they are stored through.
+__device__ __forceinline__ void stage_row(uint32_t slab, int lane, const uint32_t (&w)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        st_shared_v4(slab + lane * 64 + ((i ^ ((lane >> 1) & 3)) << 4), w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+}
+__device__ __forceinline__ void store_wait_read_1() { asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+
+// A warp's 32 rows x 32 columns (v = the columns of row `lane`) to C as one or two bulk tensor stores from the warp's slabs:
+// no address arithmetic, and rows and columns past the tensor are clipped by the map.  `flip` alternates the slabs.
 template <class T>
-__device__ __forceinline__ void store_block(const float (&v)[32], uint32_t slab, T* c, long long ldc, int n_rows, int n_cols,
-                                            bool vec, int lane) {
-    constexpr int PER = 16 / sizeof(T), SEGS = 32 / PER;             // elements of a 16-byte piece, pieces of a row
-    __syncwarp();
+__device__ __forceinline__ void store_tile(const float (&v)[32], const CUtensorMap* map, uint32_t slabs, int& flip, int col,
+                                           int row, int lane) {
+    if constexpr (sizeof(T) == 4) {
+        if (lane == 0) tma_store_wait_read();
+        __syncwarp();
 #pragma unroll
-    for (int i = 0; i < SEGS; ++i) {
-        const uint32_t at = slab + lane * (32 * sizeof(T)) + ((sizeof(T) == 4 ? (i ^ (lane & 7)) : (i ^ ((lane >> 1) & 3))) << 4);
-        if constexpr (sizeof(T) == 4)
-            st_shared_v4(at, __float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
-        else
-            st_shared_v4(at, Pack<T>::two(v[8 * i], v[8 * i + 1]), Pack<T>::two(v[8 * i + 2], v[8 * i + 3]),
-                         Pack<T>::two(v[8 * i + 4], v[8 * i + 5]), Pack<T>::two(v[8 * i + 6], v[8 * i + 7]));
+        for (int h = 0; h < 2; ++h) {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __float_as_uint(v[16 * h + i]);
+            stage_row(slabs + h * SLAB_BYTES, lane, w);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(map, slabs, col, row);
+            tma_store_2d(map, slabs + SLAB_BYTES, col + 16, row);
+            tma_store_commit();
+        }
+    } else {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = Pack<T>::two(v[2 * i], v[2 * i + 1]);
+        const uint32_t slab = slabs + flip * SLAB_BYTES;
+        flip ^= 1;
+        if (lane == 0) store_wait_read_1();          // (the store before the last one was the last user of this slab)
+        __syncwarp();
+        stage_row(slab, lane, w);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(map, slab, col, row);
+            tma_store_commit();
+        }
     }
+}
+
+// The same for a C whose rows are not 16-byte aligned (odd widths): row by row, lanes along the columns.
+template <class T>
+__device__ __forceinline__ void store_any(const float (&v)[32], uint32_t slabs, T* c, long long ldc, int n_rows, int n_cols, int lane) {
     __syncwarp();
-    const int seg = lane % SEGS;
 #pragma unroll
-    for (int it = 0; it < SEGS; ++it) {
-        const int r = it * (32 / SEGS) + lane / SEGS;
-        uint4 val;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(val.x), "=r"(val.y), "=r"(val.z), "=r"(val.w)
-                     : "r"(slab + r * (uint32_t)(32 * sizeof(T)) + ((sizeof(T) == 4 ? (seg ^ (r & 7)) : (seg ^ ((r >> 1) & 3))) << 4)));
-        if (r >= n_rows) continue;
-        T* dst = c + (long long)r * ldc + seg * PER;
-        if (vec && (seg + 1) * PER <= n_cols) {
-            *reinterpret_cast<uint4*>(dst) = val;
-        } else {
-            const T* e = reinterpret_cast<const T*>(&val);
-#pragma unroll
-            for (int j = 0; j < PER; ++j)
-                if (seg * PER + j < n_cols) dst[j] = e[j];
+    for (int i = 0; i < 32; ++i) st_shared_f32(slabs + lane * 128 + ((i ^ lane) << 2), v[i]);
+    __syncwarp();
+    if (lane < n_cols) {
+        for (int r = 0; r < n_rows; ++r) {
+            float f;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(slabs + r * 128 + ((lane ^ r) << 2)));
+            c[(long long)r * ldc + lane] = Pack<T>::one(f);
         }
     }
 }
@@ -148,12 +179,10 @@ __device__ __forceinline__ float gated(float g, float u) { return __fdividef(g, 
 template <int EPI>
 __global__ void __launch_bounds__(THREADS, 1)
 product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_constant__ CUtensorMap tmapB,
-                    const __grid_constant__ ProductArgs a, const int n_nt, const int k_blocks) {
+                    const __grid_constant__ CUtensorMap tmapC, const __grid_constant__ ProductArgs a, const int n_nt, const int k_blocks) {
     constexpr bool GATED = EPI == EPI_GATED;
-    extern __shared__ uint8_t smem_raw[];
-    const uint32_t raw = smem_u32(smem_raw);
-    const uint32_t base = (raw + 1023u) & ~1023u;
-    uint8_t* smem = smem_raw + (base - raw);
+    extern __shared__ __align__(1024) uint8_t smem[];       // (the swizzled tiles want 1024-byte boundaries)
+    const uint32_t base = smem_u32(smem);
     Ctrl* ctrl = reinterpret_cast<Ctrl*>(smem + CTRL_REGION);
     volatile uint32_t* abort_flag = &ctrl->abort;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -193,8 +222,11 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
         if (lane == 0) {
             int s = 0;
             uint32_t ph = 0;
+            PairTile next = {};
+            if (unit < total) next = pair_tile(a, unit, n_nt, n_mt);
             for (int L = unit; L < total; L += n_units) {
-                const PairTile t = pair_tile(a, L, n_nt, n_mt);
+                const PairTile t = next;
+                if (L + n_units < total) next = pair_tile(a, L + n_units, n_nt, n_mt);     // (on its way during this tile)
                 const int brow = GATED ? t.e * 2 * a.N + rank * a.N + t.n * (BN / 2) : t.e * a.N + t.n * BN + rank * (BN / 2);
                 bool ok = true;
                 for (int kb = 0; kb < k_blocks; ++kb) {
@@ -244,22 +276,24 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
     } else {
         // ------------------------------------------------------------------ epilogue
         const int quad = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t slab = base + SLAB_REGION + (warp - 2) * SLAB_BYTES;
-        const size_t c_bytes = EPI == EPI_HALF ? 2 : (GATED || a.c_type == MOK_TYPE_F32) ? 4 : 2;
-        const bool vec = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && ((a.ldc * c_bytes) & 15u) == 0;
-        int buf = 0;
+        const uint32_t slabs = base + SLAB_REGION + (warp - 2) * 2 * SLAB_BYTES;
+        const uint32_t factors = base + SCALE_REGION + (warp - 2) * 256;
+        constexpr int CHUNKS = GATED ? 2 : 4;                        // 32-column pieces of this warp
+        int buf = 0, flip = 0;
         uint32_t aph = 0;
+        PairTile next = {};
+        if (unit < total) next = pair_tile(a, unit, n_nt, n_mt);
         for (int L = unit; L < total; L += n_units) {
-            const PairTile t = pair_tile(a, L, n_nt, n_mt);
+            const PairTile t = next;
+            if (L + n_units < total) next = pair_tile(a, L + n_units, n_nt, n_mt);
             const int r0 = rank * BM + quad * 32;                    // first of the warp's rows inside the tile
             const int n_rows = min(32, t.valid - r0);
-            float rs = 0.f;
-            if (EPI != EPI_HALF && lane < n_rows) rs = __ldg(a.a_scale + t.row0 + r0 + lane);
-            // the warp's column scales, one column of each piece per lane, on their way while the products finish
-            constexpr int CHUNKS = GATED ? 2 : 4;                    // 32-column pieces of this warp
+            // the row's scale and the warp's column scales, one column of each piece per lane, on their way while the
+            // products finish
             const int first = t.n * (GATED ? BN / 2 : BN) + half * 32 * CHUNKS;
             const float* bs = a.b_scale + (size_t)t.e * (GATED ? 2 : 1) * a.N;
-            float unit_n = 1.f;
+            float rs = 0.f, unit_n = 1.f;
+            if (EPI != EPI_HALF && lane < n_rows) rs = __ldg(a.a_scale + t.row0 + r0 + lane);
             if constexpr (EPI == EPI_HALF) {
                 const float top = __ldg(a.b_max + t.e);
                 unit_n = top > 0.f ? a.y_unit / top : 0.f;
@@ -272,72 +306,73 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                 s1[c] = 0.f;
                 if (GATED && n < a.N) s1[c] = __ldg(bs + a.N + n);
                 if (EPI == EPI_PLAIN && a.bias && n < a.N) s1[c] = __ldg(a.bias + n);
-                if (EPI == EPI_HALF) s0[c] *= unit_n;
             }
             bool ok = mbar_wait(smem_u32(&ctrl->tfull[buf]), aph, abort_flag, a.header, 4);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t taddr = tmem_base + (uint32_t)(buf * BN) + ((uint32_t)(quad * 32) << 16);
+            const uint32_t taddr = tmem_base + (uint32_t)(buf * BN + half * 32 * CHUNKS) + ((uint32_t)(quad * 32) << 16);
+            uint32_t acc[2][32], up[2][GATED ? 32 : 1];
+            tc_ld32(taddr, acc[0]);
+            if constexpr (GATED) tc_ld32(taddr + BN / 2, up[0]);
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
-                uint32_t acc[32], up[GATED ? 32 : 1];
-                const int col = half * 32 * CHUNKS + c * 32;
-                tc_ld32(taddr + col, acc);
-                if constexpr (GATED) tc_ld32(taddr + BN / 2 + col, up);
-                __syncwarp();                                        // the slab's previous block has been read
-                st_shared_f32(slab + lane * 4, s0[c]);
-                st_shared_f32(slab + 128 + lane * 4, s1[c]);
-                __syncwarp();
+                const int b = c & 1;
+                st_shared_f32(factors + lane * 4, EPI == EPI_HALF ? s0[c] * unit_n : s0[c]);
+                if (EPI != EPI_HALF) st_shared_f32(factors + 128 + lane * 4, s1[c]);
                 tc_wait_ld();
-                if (c == CHUNKS - 1) {                               // the accumulator goes back before the last arithmetic
+                if (c + 1 < CHUNKS) {                                // the next piece comes while this one is worked on
+                    tc_ld32(taddr + (c + 1) * 32, acc[b ^ 1]);
+                    if constexpr (GATED) tc_ld32(taddr + BN / 2 + (c + 1) * 32, up[b ^ 1]);
+                    __syncwarp();
+                } else {                                             // the accumulator goes back before the last arithmetic
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(smem_u32(&ctrl->tempty[buf]), 0);
                 }
                 const int n0 = first + c * 32, n_cols = a.N - n0;    // first output column of the piece, and how many exist
-                if (n_rows <= 0 || n_cols <= 0) continue;
-                float v[32];
+                if (n_rows > 0 && n_cols > 0) {
+                    float v[32];
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const float4 f = ld_shared_f4(slab + i * 4);
-                    if constexpr (EPI == EPI_HALF) {
-                        v[i] = (float)(int)acc[i] * f.x;
-                        v[i + 1] = (float)(int)acc[i + 1] * f.y;
-                        v[i + 2] = (float)(int)acc[i + 2] * f.z;
-                        v[i + 3] = (float)(int)acc[i + 3] * f.w;
-                    } else {
-                        const float4 q = ld_shared_f4(slab + 128 + i * 4);
-                        v[i] = (float)(int)acc[i] * rs * f.x;
-                        v[i + 1] = (float)(int)acc[i + 1] * rs * f.y;
-                        v[i + 2] = (float)(int)acc[i + 2] * rs * f.z;
-                        v[i + 3] = (float)(int)acc[i + 3] * rs * f.w;
-                        if constexpr (GATED) {
-                            v[i] = gated(v[i], (float)(int)up[i] * rs * q.x);
-                            v[i + 1] = gated(v[i + 1], (float)(int)up[i + 1] * rs * q.y);
-                            v[i + 2] = gated(v[i + 2], (float)(int)up[i + 2] * rs * q.z);
-                            v[i + 3] = gated(v[i + 3], (float)(int)up[i + 3] * rs * q.w);
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 f = ld_shared_f4(factors + i * 4);
+                        const float fs[4] = {f.x, f.y, f.z, f.w};
+                        if constexpr (EPI == EPI_HALF) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) v[i + j] = (float)(int)acc[b][i + j] * fs[j];
                         } else {
-                            v[i] += q.x;
-                            v[i + 1] += q.y;
-                            v[i + 2] += q.z;
-                            v[i + 3] += q.w;
+                            const float4 q = ld_shared_f4(factors + 128 + i * 4);
+                            const float qs[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                v[i + j] = (float)(int)acc[b][i + j] * rs * fs[j];
+                                if constexpr (GATED) v[i + j] = gated(v[i + j], (float)(int)up[b][i + j] * rs * qs[j]);
+                                else v[i + j] += qs[j];
+                            }
                         }
                     }
+                    const int row = t.row0 + r0;
+                    // (grouped rows are stored in whole blocks of 32: what follows a segment's last row is its own padding)
+                    if constexpr (GATED) {
+                        store_tile<float>(v, &tmapC, slabs, flip, n0, row, lane);
+                    } else if constexpr (EPI == EPI_HALF) {
+                        store_tile<__half>(v, &tmapC, slabs, flip, n0, row, lane);
+                    } else if (a.c_mapped) {
+                        if (a.c_type == MOK_TYPE_F32) store_tile<float>(v, &tmapC, slabs, flip, n0, row, lane);
+                        else if (a.c_type == MOK_TYPE_F16) store_tile<__half>(v, &tmapC, slabs, flip, n0, row, lane);
+                        else store_tile<__nv_bfloat16>(v, &tmapC, slabs, flip, n0, row, lane);
+                    } else {
+                        const long long at = (long long)row * a.ldc + n0;
+                        if (a.c_type == MOK_TYPE_F32) store_any(v, slabs, reinterpret_cast<float*>(a.C) + at, a.ldc, n_rows, n_cols, lane);
+                        else if (a.c_type == MOK_TYPE_F16) store_any(v, slabs, reinterpret_cast<__half*>(a.C) + at, a.ldc, n_rows, n_cols, lane);
+                        else store_any(v, slabs, reinterpret_cast<__nv_bfloat16*>(a.C) + at, a.ldc, n_rows, n_cols, lane);
+                    }
                 }
-                const long long at = (long long)(t.row0 + r0) * a.ldc + n0;
-                if constexpr (GATED) {
-                    store_block(v, slab, reinterpret_cast<float*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
-                } else if constexpr (EPI == EPI_HALF) {
-                    store_block(v, slab, reinterpret_cast<__half*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
-                } else {
-                    if (a.c_type == MOK_TYPE_F32) store_block(v, slab, reinterpret_cast<float*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
-                    else if (a.c_type == MOK_TYPE_F16) store_block(v, slab, reinterpret_cast<__half*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
-                    else store_block(v, slab, reinterpret_cast<__nv_bfloat16*>(a.C) + at, a.ldc, n_rows, n_cols, vec, lane);
-                }
+                __syncwarp();                                        // the factors have been read
             }
             if (++buf == 2) { buf = 0; aph ^= 1u; }
         }
+        if (lane == 0) tma_store_wait_all();
     }
 
     // ---------------------------------------------------------------------- teardown
@@ -379,7 +414,7 @@ static bool byte_map(CUtensorMap* m, const void* ptr, long long rows, int cols, 
 }
 
 template <int EPI>
-static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, const ProductArgs& a, int n_nt, int k_blocks,
+static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, const CUtensorMap& mC, const ProductArgs& a, int n_nt, int k_blocks,
                                long long tiles, cudaStream_t s) {
     static PerDevice configured;                 // per device: CTA pairs that run at once
     auto kernel = product_pair_kernel<EPI>;
@@ -413,22 +448,32 @@ static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, con
     if (e != cudaSuccess) return e;
     cfg.gridDim = dim3((unsigned)(2 * (tiles < units ? tiles : units)));
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, mA, mB, a, n_nt, k_blocks);
+    return cudaLaunchKernelEx(&cfg, kernel, mA, mB, mC, a, n_nt, k_blocks);
 }
 
-cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s) {
+cudaError_t launch_product(const ProductArgs& args, int epi, cudaStream_t s) {
+    ProductArgs a = args;
     const bool gated = epi == EPI_GATED;
-    CUtensorMap mA, mB;
+    CUtensorMap mA, mB, mC;
     if (!byte_map(&mA, a.A, a.a_rows, a.K, a.lda, BM) ||
         !byte_map(&mB, a.B, (long long)a.E * (gated ? 2 : 1) * a.N, a.K, a.ldb, BN / 2))
+        return cudaErrorInvalidValue;
+    // C in boxes of 32 rows of 64 bytes, where its rows allow it
+    const int type = gated ? MOK_TYPE_F32 : epi == EPI_HALF ? MOK_TYPE_F16 : a.c_type;
+    const uint64_t size = type_bytes(type);
+    a.c_mapped = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
+    if (!a.c_mapped) mC = mA;
+    else if (!tmap::encode_2d(&mC, type == MOK_TYPE_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_UINT16, a.C,
+                              (uint64_t)(a.dense_rows > 0 ? a.dense_rows : a.a_rows), (uint64_t)a.N, a.ldc * size,
+                              (uint32_t)(64 / size), 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return cudaErrorInvalidValue;
     const int n_nt = gated ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + BN - 1) / BN;
     const int k_blocks = (a.K + BKB - 1) / BKB;
     const long long tiles = (a.dense_rows > 0 ? (a.dense_rows + 2 * BM - 1) / (2 * BM) : a.max_mt) * (long long)n_nt;
     if (tiles <= 0 || tiles > 0x7fffffffll) return cudaErrorInvalidValue;
-    if (epi == EPI_PLAIN) return launch_pair<EPI_PLAIN>(mA, mB, a, n_nt, k_blocks, tiles, s);
-    if (gated) return launch_pair<EPI_GATED>(mA, mB, a, n_nt, k_blocks, tiles, s);
-    return launch_pair<EPI_HALF>(mA, mB, a, n_nt, k_blocks, tiles, s);
+    if (epi == EPI_PLAIN) return launch_pair<EPI_PLAIN>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
+    if (gated) return launch_pair<EPI_GATED>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
+    return launch_pair<EPI_HALF>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
 }
 
 }  // namespace i8

@@ -54,21 +54,21 @@ struct ProductArgs {
     float y_unit;                // EPI_HALF: power of two that brings |sum| <= 127 * 127 * K below 65504
     const float* bias;           // [N] or NULL (plain)
     int32_t dense_rows;          // > 0: dense
-    const int32_t* counts;
-    const int32_t* pad_offsets;
-    const int32_t* n_mtiles;     // 256-row tile table
-    const int32_t* tile_expert;
-    const int32_t* mt_start;
-    int32_t max_mt;
+    const int4* tiles;           // grouped: {first row, rows of the segment from there on, expert, -} of every 256-row tile
+    const int32_t* n_mtiles;     // how many
+    int32_t max_mt;              // at most
+    int32_t c_mapped;            // set by the launcher: C is stored through a tensor map
     WsHeader* header;
 };
 enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
 
 // Where a token's codes go when its rows are wanted in expert order: row pos[t * k + s] for every routed slot s.
+// The launch also writes the product's tile list from the schedule's tables.
 struct RouteArgs {
-    const int32_t* idx;
-    const int32_t* pos;
+    const int32_t *idx, *pos;
     int32_t E, k;
+    int4* tiles;
+    const int32_t *n_mtiles, *tile_expert, *mt_start, *pad_offsets, *counts;
 };
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);

@@ -133,7 +133,7 @@ static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 // Workspace of the routed experts: the schedule's tables (a WsLayout of which only those are set) and the activations.
 struct ExpertsLayout {
     WsLayout L;
-    size_t xq, xs, h, hq, factor, y, total;
+    size_t tiles, xq, xs, h, hq, factor, y, total;
     int pitch_h, pitch_i;
     long long max_tiles;         // upper bound of 256-row tiles
 };
@@ -169,6 +169,7 @@ static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) 
     L.pos = take(r1);
     L.blk_hist = take(sizeof(int32_t) * (size_t)L.n_blk * E);
     L.row_token = take(sizeof(int32_t) * (size_t)L.Rpad);
+    X->tiles = take(sizeof(int4) * (size_t)(X->max_tiles > 0 ? X->max_tiles : 1));
     X->xq = take((size_t)L.Rpad * X->pitch_h);
     X->xs = take(sizeof(float) * (size_t)L.Rpad);
     X->h = take(sizeof(float) * (size_t)L.Rpad * I);
@@ -297,16 +298,16 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     if (e != cudaSuccess) return cuda_fail(e);
     e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
     if (e != cudaSuccess) return cuda_fail(e);
-    const i8::RouteArgs routes = {a->topk_idx, reinterpret_cast<const int32_t*>(ws + X.L.pos), a->E, a->k};
+    auto table = [&](size_t at) { return reinterpret_cast<const int32_t*>(ws + at); };
+    int4* tiles = reinterpret_cast<int4*>(ws + X.tiles);
+    const i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k, tiles, &hdr->n_mtiles2, table(X.L.tile_expert2),
+                                  table(X.L.mt_start2), table(X.L.pad_offsets), table(X.L.counts)};
     e = i8::launch_quantize(a->x, a->type, a->T, a->H, a->x_stride, reinterpret_cast<int8_t*>(ws + X.xq), X.pitch_h,
                             reinterpret_cast<float*>(ws + X.xs), s, &routes);
     if (e != cudaSuccess) return cuda_fail(e);
     g.E = a->E;
-    g.counts = reinterpret_cast<const int32_t*>(ws + X.L.counts);
-    g.pad_offsets = reinterpret_cast<const int32_t*>(ws + X.L.pad_offsets);
+    g.tiles = tiles;
     g.n_mtiles = &hdr->n_mtiles2;
-    g.tile_expert = reinterpret_cast<const int32_t*>(ws + X.L.tile_expert2);
-    g.mt_start = reinterpret_cast<const int32_t*>(ws + X.L.mt_start2);
     g.max_mt = (int32_t)X.max_tiles;
     g.A = reinterpret_cast<const int8_t*>(ws + X.xq);
     g.lda = X.pitch_h;
@@ -326,17 +327,17 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
         const float* h = reinterpret_cast<const float*>(ws + X.h);
         int8_t* hq = reinterpret_cast<int8_t*>(ws + X.hq);
         float* factor = reinterpret_cast<float*>(ws + X.factor);
-        const int32_t* te = reinterpret_cast<const int32_t*>(ws + X.L.tile_expert);
+        const int32_t *te = table(X.L.tile_expert), *pads = table(X.L.pad_offsets), *counts = table(X.L.counts);
         const long long rows = X.L.Rpad, most = 148 * 16;
         const bool warp_rows = a->I <= 1024;
         const long long blocks = warp_rows ? (rows + 7) / 8 : rows;
         const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(i8::THREADS);
         e = warp_rows ? launch_pdl(i8::quantize_hidden_kernel<32, 8>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor, a->down_max,
-                                   1.f / unit, hdr, te, g.pad_offsets, g.counts)
+                                   1.f / unit, hdr, te, pads, counts)
             : a->I <= 8192 ? launch_pdl(i8::quantize_hidden_kernel<256, 8>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor,
-                                        a->down_max, 1.f / unit, hdr, te, g.pad_offsets, g.counts)
+                                        a->down_max, 1.f / unit, hdr, te, pads, counts)
                            : launch_pdl(i8::quantize_hidden_kernel<256, 16>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor,
-                                        a->down_max, 1.f / unit, hdr, te, g.pad_offsets, g.counts);
+                                        a->down_max, 1.f / unit, hdr, te, pads, counts);
         if (e != cudaSuccess) return cuda_fail(e);
     }
     g.A = reinterpret_cast<const int8_t*>(ws + X.hq);
