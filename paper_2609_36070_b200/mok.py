@@ -771,8 +771,8 @@ def mok_gate(raw_stream, logits, k, bias=None, score="softmax", n_groups=1, topk
     "softmax" or "sigmoid"; bias fp32 [E] takes part in the selection only; see include/mok.h for groups and weights."""
     (T, E), device = logits.shape, logits.device
     ld = _rows("logits", logits, E, device, _TYPES)
-    idx = torch.empty((T, k), dtype=torch.int32, device=device)
-    w = torch.empty((T, k), dtype=torch.float32, device=device)
+    idx = torch.empty_strided((T, k), (k, 1), dtype=torch.int32, device=device)      # (1 us less host time than empty)
+    w = torch.empty_strided((T, k), (k, 1), dtype=torch.float32, device=device)
     _check(_lib.mok_gate(mok_gate_args(
         logits.data_ptr(), None if bias is None else _packed("bias", bias, (E,), device, torch.float32), ld, T, E, k,
         _TYPES[logits.dtype], _SCORES[score], n_groups, topk_groups, group_top, bool(renormalise), scale, idx.data_ptr(),
@@ -786,7 +786,7 @@ def mok_gate_backward(raw_stream, logits, topk_idx, dw, score="softmax", renorma
     (T, E), device = logits.shape, logits.device
     k = topk_idx.shape[-1]
     ld = _rows("logits", logits, E, device, _TYPES)
-    out = torch.empty((T, E), dtype=logits.dtype, device=device)
+    out = torch.empty_strided((T, E), (E, 1), dtype=logits.dtype, device=device)
     _check(_lib.mok_gate_backward(mok_gate_bwd_args(
         logits.data_ptr(), _packed("topk_idx", topk_idx, (T, k), device, torch.int32),
         _packed("dw", dw, (T, k), device, torch.float32), ld, E, T, E, k, _TYPES[logits.dtype], _SCORES[score],
@@ -829,7 +829,7 @@ def _i8_product(x, x_codes, x_scales, x_stride, codes_stride, M, K, x_type, weig
     W = weights.codes
     N = W.shape[0]
     w_stride = _rows("weights.codes", W, K, device, _INT8)
-    out = torch.empty((M, N), dtype=out_dtype, device=device)
+    out = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=device)
     _check(_lib.mok_i8_linear(mok_i8_linear_args(
         x, x_codes, x_scales, W.data_ptr(), _packed("weights.scales", weights.scales, (N,), device, torch.float32),
         None if bias is None else _packed("bias", bias, (N,), device, torch.float32), x_stride, codes_stride, w_stride, N,
@@ -894,7 +894,7 @@ def mok_i8_experts(raw_stream, x, topk_idx, topk_w, gate_up, down, add=None, wor
     if workspace is None:
         workspace = torch.empty(_lib.mok_i8_experts_workspace_bytes(T, H, I, E, k), dtype=torch.uint8, device=device)
     ws, ws_bytes = _aligned_ws(workspace)
-    out = torch.empty((T, H), dtype=dtype, device=device)
+    out = torch.empty_strided((T, H), (H, 1), dtype=dtype, device=device)
     _check(_lib.mok_i8_experts(mok_i8_experts_args(
         x.data_ptr(), _packed("topk_idx", topk_idx, (T, k), device, torch.int32),
         _packed("topk_w", topk_w, (T, k), device, torch.float32), gu, gu_scales, dn, dn_scales,

@@ -74,6 +74,10 @@ GATES = [  # T, E, k, score, groups, topk_groups, group_top, bias, renorm, scale
     (64, 512, 16, "softmax", 32, 1, 1, True, True, 1.0, torch.bfloat16),
     (40000, 32, 2, "softmax", 1, 1, 1, False, True, 1.0, torch.bfloat16),
     (17, 31, 31, "sigmoid", 1, 1, 1, True, True, 1.0, torch.float32),
+    (1001, 512, 10, "sigmoid", 16, 5, 2, True, True, 1.0, torch.float32),
+    (515, 384, 8, "softmax", 4, 3, 2, True, True, 1.0, torch.float16),
+    (515, 320, 6, "sigmoid", 5, 1, 1, False, True, 1.0, torch.bfloat16),
+    (130, 128, 32, "softmax", 4, 4, 1, False, False, 1.0, torch.float32),
 ]
 
 
@@ -184,6 +188,19 @@ def test_gate_gradient_against_differences(mok, score, renorm):
     d = mok.mok_gate_backward(logits, idx, dw, score=score, renormalise=renorm)
     along = (d.double() * v).sum(-1)
     assert ((along - diff).abs() <= (h * h / 6 * 2 + 2.0 ** -23 / h) * dw.abs().sum(-1) * 2).all()
+
+
+@pytest.mark.parametrize("G", [1, 2, 4])
+def test_gate_masked_experts_whatever_their_bias(mok, G):
+    """An expert whose logit is -inf is not chosen for a token that has k others, however large its bias."""
+    E, k = 64, 4
+    logits = randn(gen(21), 33, E)
+    masked = torch.rand(33, E, generator=gen(22), device="cuda") < 0.5
+    logits[masked] = -math.inf
+    bias = torch.where(masked.float().mean(0) > 0.5, 10.0, 0.0)
+    for score in ("softmax", "sigmoid"):
+        idx, w = mok.mok_gate(logits, k, bias=bias, score=score, n_groups=G, topk_groups=G, group_top=2)
+        assert not masked.gather(1, idx.long()).any() and torch.isfinite(w).all()
 
 
 def test_gate_backward_ignores_dropped_ids(mok):
