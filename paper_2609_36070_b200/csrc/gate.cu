@@ -34,7 +34,17 @@ __device__ __forceinline__ void store_f(__half* p, float v) { *p = __float2half_
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
 
 // For the comparison of scores: within 2^-22 of the exact value, which is what an fp32 score is worth.
-__device__ __forceinline__ float sigmoid_near(float l) { return __fdividef(1.f, 1.f + __expf(-l)); }
+__device__ __forceinline__ float exp2_near(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+constexpr float LOG2_E = 1.44269504f;
+__device__ __forceinline__ float sigmoid_near(float l) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_near(-LOG2_E * l)));
+    return r;
+}
 // Keys that compare as the values do: absent or taken experts 0, NaN 1, then -inf ... +inf.  -0 counts as 0.
 __device__ __forceinline__ unsigned choice_key(float v) {
     if (v != v) return 1u;
@@ -229,9 +239,12 @@ __device__ __forceinline__ float sum8(float v) {
 // Values that compare below every other one, so that -inf can stand for "not there": NaN, then -inf, then the finite ones.
 constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOWEST = -3.40282306e38f;
 
+// Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.
+constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 8 ? 5 : 2; }
+
 // No groups, or groups of whole 32 experts: four tokens per warp.  NI pieces of four experts per lane (E <= 32 NI).
 template <class L, int NI, bool VEC>
-__global__ void __launch_bounds__(32 * WARPS)
+__global__ void __launch_bounds__(32 * WARPS, gate_blocks(NI))
 gate_kernel(const Params p) {
     extern __shared__ __align__(16) float s_mem[];   // per warp: values [4][32 NI], then chosen ids [4][MAX_K]
     pdl_enter();
@@ -305,30 +318,26 @@ gate_kernel(const Params p) {
             *reinterpret_cast<float4*>(vals + (sub + 8 * i) * 4) = make_float4(c[i][0], c[i][1], c[i][2], c[i][3]);
         }
         if (G > 1) {
-            // values of groups sub and sub + 8 (of at most 16): every group's two best are reduced over the eight lanes
-            float v0 = -INFINITY, v1 = -INFINITY, b1 = -INFINITY, b2 = -INFINITY;
-            int g = 0, until = span;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const float h0 = fmaxf(c[i][0], c[i][1]), h1 = fmaxf(c[i][2], c[i][3]);
-                const float second = fmaxf(fminf(h0, h1), fmaxf(fminf(c[i][0], c[i][1]), fminf(c[i][2], c[i][3])));
-                b2 = fmaxf(fmaxf(b2, second), fminf(b1, top[i]));
-                b1 = fmaxf(b1, top[i]);
-                if (--until == 0 && g < G) {
-#pragma unroll
-                    for (int off = 1; off < 8; off <<= 1) {
-                        const float o1 = __shfl_xor_sync(0xffffffffu, b1, off), o2 = __shfl_xor_sync(0xffffffffu, b2, off);
-                        b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
-                        b1 = fmaxf(b1, o1);
-                    }
-                    const float v = p.group_top == 2 ? b1 + b2 : b1;
-                    if (g == sub) v0 = v;
-                    if (g == sub + 8) v1 = v;
-                    ++g;
-                    until = span;
-                    b1 = b2 = -INFINITY;
+            // lane sub finds the two best of group sub, then of group sub + 8 (of at most 16), from the values in shared
+            // memory; the lanes start at different pieces, so that they do not meet in a bank
+            __syncwarp();
+            const int pieces = 8 * span;
+            float v0 = -INFINITY, v1 = -INFINITY;
+            for (int g = sub; g < G; g += 8) {
+                const float4* mine = reinterpret_cast<const float4*>(vals + g * 32 * span);
+                float b1 = -INFINITY, b2 = -INFINITY;
+                for (int it = 0; it < pieces; ++it) {
+                    const float4 f = mine[(it & ~7) | ((it + sub) & 7)];
+                    const float h0 = fmaxf(f.x, f.y), h1 = fmaxf(f.z, f.w), h = fmaxf(h0, h1);
+                    const float second = fmaxf(fminf(h0, h1), fmaxf(fminf(f.x, f.y), fminf(f.z, f.w)));
+                    b2 = fmaxf(fmaxf(b2, second), fminf(b1, h));
+                    b1 = fmaxf(b1, h);
                 }
+                const float v = p.group_top == 2 ? b1 + b2 : b1;
+                if (g < 8) v0 = v;
+                else v1 = v;
             }
+            __syncwarp();
             int rank0 = 0, rank1 = 0;
             for (int q = 0; q < G; ++q) {
                 const float other = __shfl_sync(0xffffffffu, q < 8 ? v0 : v1, (lane & 24) + (q & 7));
@@ -338,8 +347,7 @@ gate_kernel(const Params p) {
             const unsigned k0 = __ballot_sync(0xffffffffu, rank0 < p.topk_groups);
             const unsigned k1 = NI > 8 ? __ballot_sync(0xffffffffu, rank1 < p.topk_groups) : 0u;
             const unsigned kept = ((k0 >> (lane & 24)) & 0xffu) | (((k1 >> (lane & 24)) & 0xffu) << 8);
-            g = 0;
-            until = span;
+            int g = 0, until = span;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 if (!((kept >> g) & 1u)) top[i] = -INFINITY;
@@ -348,23 +356,26 @@ gate_kernel(const Params p) {
         }
         __syncwarp();
         for (int s = 0; s < k; ++s) {
-            float best = top[0];
+            float mine = top[0];
+#pragma unroll
+            for (int i = 1; i < NI; ++i) mine = fmaxf(mine, top[i]);
+            const float best = max8(mine);
+            unsigned holders = (__ballot_sync(0xffffffffu, mine == best) >> (lane & 24)) & 0xffu;
             int bi = 0;
+            if (mine == best) {
 #pragma unroll
-            for (int i = 1; i < NI; ++i)
-                if (top[i] > best) { best = top[i]; bi = i; }          // strict: the lowest ids of the lane's equals
-            const int mine = sub + 8 * bi;
-            int piece = mine;
-#pragma unroll
-            for (int off = 1; off < 8; off <<= 1) {
-                const float o = __shfl_xor_sync(0xffffffffu, best, off);
-                const int op = __shfl_xor_sync(0xffffffffu, piece, off);
-                const bool take = o > best || (o == best && op < piece);
-                best = take ? o : best;
-                piece = take ? op : piece;
+                for (int i = NI - 1; i >= 0; --i)
+                    if (top[i] == best) bi = i;      // the lane's lowest ids
             }
-            if (piece == mine) {                     // this lane's piece holds it: take it out, find the piece's next
-                float4 v = *reinterpret_cast<const float4*>(vals + piece * 4);
+            const int piece = sub + 8 * bi;
+            if (__any_sync(0xffffffffu, holders & (holders - 1))) {    // equal values in several lanes: the lowest piece
+                int low = mine == best ? piece : 0x7fffffff;
+#pragma unroll
+                for (int off = 1; off < 8; off <<= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, off));
+                holders = 1u << (low & 7);
+            }
+            if (holders == 1u << sub) {              // this lane's piece holds it: take it out, find the piece's next
+                const float4 v = *reinterpret_cast<const float4*>(vals + piece * 4);
                 const int j = v.x == best ? 0 : v.y == best ? 1 : v.z == best ? 2 : 3;
                 vals[piece * 4 + j] = -INFINITY;
                 chosen[s] = piece * 4 + j;
@@ -507,8 +518,9 @@ template <class L, int NI>
 static cudaError_t launch_four(const Params& p, cudaStream_t s) {
     const bool vec = p.E % 4 == 0 && (p.T == 1 || p.stride % 4 == 0) && (reinterpret_cast<uintptr_t>(p.logits) & (4 * sizeof(L) - 1)) == 0 &&
                      (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0;
-    long long blocks = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS);
-    if (blocks > 148 * 8) blocks = 148 * 8;
+    // one wave of blocks with the same number of rounds each
+    const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * gate_blocks(NI);
+    const long long rounds = (units + wave - 1) / wave, blocks = (units + rounds - 1) / rounds;
     const size_t smem = sizeof(float) * WARPS * 4 * (32 * NI + MAX_K);
     const dim3 grid((unsigned)blocks), block(32 * WARPS);
     return vec ? launch_pdl(gate_kernel<L, NI, true>, grid, block, smem, s, p) : launch_pdl(gate_kernel<L, NI, false>, grid, block, smem, s, p);
