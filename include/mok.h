@@ -557,11 +557,13 @@ typedef struct mok_i8_linear_args {
     int64_t x_stride, codes_stride, w_stride, out_stride;
     int32_t M, K, N, x_type, out_type;
     void* out;                               /* [M, N] of out_type, rows out_stride elements apart */
-    void* workspace;                         /* mok_i8_linear_workspace_bytes(M, K), 256-byte aligned (x given) */
+    void* workspace;                         /* mok_i8_linear_workspace_bytes(...), 256-byte aligned (NULL for 0) */
     size_t workspace_bytes;
     void* stream;
 } mok_i8_linear_args;
-size_t mok_i8_linear_workspace_bytes(int M, int K);
+/* Scratch of that call (0: few tokens, which need none, or codes, or invalid sizes).  M (round(K to 16) + 4) + 512 bytes
+ * always do. */
+size_t mok_i8_linear_workspace_bytes(const mok_i8_linear_args* args);
 int mok_i8_linear(const mok_i8_linear_args* args);
 
 /*

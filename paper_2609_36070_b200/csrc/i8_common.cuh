@@ -25,15 +25,41 @@ __device__ __forceinline__ uint32_t pack4(uint32_t a, uint32_t b, uint32_t c, ui
     return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
 }
 // The two factors of a row: q = (v * times) / by.  Above 2^120 the product 127 v would overflow: both are then 2^8 smaller.
-struct RowRule { float times, by; };
+// `near` is their quotient to within 2^-22.
+struct RowRule { float times, by, near; };
 __device__ __forceinline__ RowRule row_rule(float amax) {
-    return amax > 1.329228e36f ? RowRule{127.f / 256.f, amax * (1.f / 256.f)} : RowRule{127.f, amax};
+    const bool big = amax > 1.329228e36f;
+    const float times = big ? 127.f / 256.f : 127.f, by = big ? amax * (1.f / 256.f) : amax;
+    return RowRule{times, by, __fdividef(times, by)};
 }
+// The exact code costs a division.  v * near is within 4e-5 of the quotient, so unless it comes within 2e-4 of a tie its
+// rounding is the quotient's: four codes cost a dozen instructions and one value in 2500 a division.
 __device__ __forceinline__ uint32_t code_bits(float v, RowRule r) { return round_byte(__fdiv_rn(__fmul_rn(v, r.times), r.by)); }
+static __device__ __noinline__ uint32_t four_exact_codes(float v0, float v1, float v2, float v3, float times, float by) {
+    const RowRule r = {times, by, 0.f};
+    return pack4(code_bits(v0, r), code_bits(v1, r), code_bits(v2, r), code_bits(v3, r));
+}
+// CALL: the divisions in a function, for code that runs once and should be short (a call costs its caller registers)
+template <bool CALL = false>
+__device__ __forceinline__ uint32_t four_codes(float v0, float v1, float v2, float v3, RowRule r) {
+    constexpr float MAGIC = 12582912.f;
+    const float m0 = fmaf(v0, r.near, MAGIC), m1 = fmaf(v1, r.near, MAGIC), m2 = fmaf(v2, r.near, MAGIC), m3 = fmaf(v3, r.near, MAGIC);
+    const float d0 = fabsf(fmaf(v0, r.near, MAGIC - m0)), d1 = fabsf(fmaf(v1, r.near, MAGIC - m1));
+    const float d2 = fabsf(fmaf(v2, r.near, MAGIC - m2)), d3 = fabsf(fmaf(v3, r.near, MAGIC - m3));
+    if (d0 <= 0.4998f && d1 <= 0.4998f && d2 <= 0.4998f && d3 <= 0.4998f)      // (false for NaN, too)
+        return pack4(__float_as_uint(m0), __float_as_uint(m1), __float_as_uint(m2), __float_as_uint(m3));
+    if (CALL) return four_exact_codes(v0, v1, v2, v3, r.times, r.by);
+    return pack4(code_bits(v0, r), code_bits(v1, r), code_bits(v2, r), code_bits(v3, r));
+}
 
 __device__ __forceinline__ float to_f(float v) { return v; }
 __device__ __forceinline__ float to_f(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ float to_f(__half v) { return __half2float(v); }
+
+template <class T> __device__ __forceinline__ T from_f(float v);
+template <> __device__ __forceinline__ float from_f<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
 inline bool type_ok(int t) { return t == MOK_TYPE_BF16 || t == MOK_TYPE_F16 || t == MOK_TYPE_F32; }
 inline size_t type_bytes(int t) { return t == MOK_TYPE_F32 ? 4 : 2; }
@@ -73,6 +99,9 @@ struct RouteArgs {
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s);
+// few tokens (EPI_PLAIN, dense): whether the kernel for them takes the product; quantises: activations instead of codes
+bool narrow_product(int M, int K, int N, int x_type, unsigned long long x_align, bool* quantises);
+cudaError_t launch_narrow(const ProductArgs& a, const void* x, int x_type, long long ldx, cudaStream_t s);
 cudaError_t status_header(WsHeader** out);
 
 }  // namespace i8

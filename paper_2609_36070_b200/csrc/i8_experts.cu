@@ -67,16 +67,12 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
             if (c >= pieces) break;
             uint32_t o = 0u;
             if (codable)
-                o = pack4(code_bits(v[i].x, rule), code_bits(v[i].y, rule), code_bits(v[i].z, rule), code_bits(v[i].w, rule));
+                o = four_codes(v[i].x, v[i].y, v[i].z, v[i].w, rule);
             *reinterpret_cast<uint32_t*>(dst + c * 4) = o;
         }
         if (sub == 0) factor[p] = amax / 127.f * (b_max[e] * inv_unit);
     }
 }
-
-template <class T> __device__ __forceinline__ T from_f(float v);
-template <> __device__ __forceinline__ __nv_bfloat16 from_f<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <> __device__ __forceinline__ __half from_f<__half>(float v) { return __float2half_rn(v); }
 
 // One block per token.  Slots whose expert id is outside 0 .. E-1 are not routed.
 template <class T>
@@ -208,10 +204,15 @@ int mok_i8_quantize(const void* x, int type, long long rows, int K, long long x_
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);
 }
 
-size_t mok_i8_linear_workspace_bytes(int M, int K) {
-    if (M < 0 || K < 1 || K > i8::MAX_CONTRACTION) return 0;
-    const size_t m = M > 0 ? M : 1;
-    return align_up(m * i8::pitch_of(K), 256) + align_up(m * sizeof(float), 256);
+static unsigned long long x_alignment(const mok_i8_linear_args* a) {
+    return reinterpret_cast<uintptr_t>(a->x) | (a->M > 1 ? (unsigned long long)a->x_stride * i8::type_bytes(a->x_type) : 0ull);
+}
+static size_t codes_bytes(int M, int K) { return align_up((size_t)M * i8::pitch_of(K), 256) + align_up((size_t)M * sizeof(float), 256); }
+
+size_t mok_i8_linear_workspace_bytes(const mok_i8_linear_args* a) {
+    if (!a || !a->x || a->M < 1 || a->K < 1 || a->N < 1 || a->K > i8::MAX_CONTRACTION || !i8::type_ok(a->x_type)) return 0;
+    bool quantises = false;
+    return i8::narrow_product(a->M, a->K, a->N, a->x_type, x_alignment(a), &quantises) && quantises ? 0 : codes_bytes(a->M, a->K);
 }
 
 int mok_i8_linear(const mok_i8_linear_args* a) {
@@ -235,23 +236,6 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
     i8::ProductArgs g = {};
     cudaError_t e = i8::status_header(&g.header);
     if (e != cudaSuccess) return cuda_fail(e);
-    if (coded) {
-        g.A = a->x_codes;
-        g.lda = a->codes_stride;
-        g.a_scale = a->x_scales;
-    } else {
-        if (!a->workspace || !i8::aligned(a->workspace, 256) || a->workspace_bytes < mok_i8_linear_workspace_bytes(a->M, a->K))
-            return MOK_ERR_WORKSPACE;
-        char* ws = reinterpret_cast<char*>(a->workspace);
-        int8_t* codes = reinterpret_cast<int8_t*>(ws);
-        const int pitch = i8::pitch_of(a->K);
-        float* scales = reinterpret_cast<float*>(ws + align_up((size_t)a->M * pitch, 256));
-        e = i8::launch_quantize(a->x, a->x_type, a->M, a->K, a->x_stride, codes, pitch, scales, s);
-        if (e != cudaSuccess) return cuda_fail(e);
-        g.A = codes;
-        g.lda = pitch;
-        g.a_scale = scales;
-    }
     g.a_rows = a->M;
     g.B = a->W_codes;
     g.ldb = a->w_stride;
@@ -263,7 +247,29 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
     g.c_type = a->out_type;
     g.dense_rows = a->M;
     g.max_mt = (a->M + 2 * TILE_M - 1) / (2 * TILE_M);
-    e = i8::launch_product(g, i8::EPI_PLAIN, s);
+    bool quantises = false;
+    const bool narrow = i8::narrow_product(a->M, a->K, a->N, a->x_type, x_alignment(a), &quantises);
+    if (coded) {
+        g.A = a->x_codes;
+        g.lda = a->codes_stride;
+        g.a_scale = a->x_scales;
+    } else {
+        if (narrow && quantises) {
+            e = i8::launch_narrow(g, a->x, a->x_type, a->x_stride, s);
+            return e == cudaSuccess ? MOK_OK : cuda_fail(e);
+        }
+        if (!a->workspace || !i8::aligned(a->workspace, 256) || a->workspace_bytes < codes_bytes(a->M, a->K)) return MOK_ERR_WORKSPACE;
+        char* ws = reinterpret_cast<char*>(a->workspace);
+        int8_t* codes = reinterpret_cast<int8_t*>(ws);
+        const int pitch = i8::pitch_of(a->K);
+        float* scales = reinterpret_cast<float*>(ws + align_up((size_t)a->M * pitch, 256));
+        e = i8::launch_quantize(a->x, a->x_type, a->M, a->K, a->x_stride, codes, pitch, scales, s);
+        if (e != cudaSuccess) return cuda_fail(e);
+        g.A = codes;
+        g.lda = pitch;
+        g.a_scale = scales;
+    }
+    e = narrow ? i8::launch_narrow(g, nullptr, 0, 0, s) : i8::launch_product(g, i8::EPI_PLAIN, s);
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);
 }
 

@@ -5,18 +5,20 @@ namespace mok {
 namespace i8 {
 
 constexpr int THREADS = 256;
-constexpr int VEC_PER_THREAD = 8;      // 16-byte pieces of a row that one thread keeps in registers
+constexpr int HELD = 4;                // 16-byte pieces of a row that one thread keeps in registers: with more, too few
+                                       // blocks fit on an SM to cover the memory's latency
 
-// `TPR` threads share a row (32: eight rows per block; 256: the block); returns the maximum over them.
-template <int TPR>
+// `TPR` threads share a row (a warp, or the warps of a part of the block); returns the maximum over them.  Called by all threads.
+template <int TPR, int BLOCK>
 __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* s_max) {
     v = __reduce_max_sync(0xffffffffu, v);
     if (TPR > 32) {
+        constexpr int WARPS = TPR / 32;
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         __syncthreads();
         if (lane == 0) s_max[warp] = v;
         __syncthreads();
-        v = __reduce_max_sync(0xffffffffu, lane < THREADS / 32 ? s_max[lane] : 0u);
+        v = __reduce_max_sync(0xffffffffu, lane < WARPS ? s_max[warp / WARPS * WARPS + lane] : 0u);
     }
     return v;
 }
@@ -50,50 +52,49 @@ __device__ __forceinline__ void write_tiles(const RouteArgs& q) {
 }
 
 // Rows of whole 16-byte pieces that fit into the registers of their threads: one pass over memory.
-template <class T, int TPR, bool ROUTED>
-__global__ void __launch_bounds__(THREADS)
+template <class T, int TPR, int BLOCK, bool ROUTED>
+__global__ void __launch_bounds__(BLOCK, 1280 / BLOCK)
 quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ldx, int8_t* __restrict__ codes, long long ldc,
                     float* __restrict__ scales, const RouteArgs routes) {
     constexpr int PER = 16 / sizeof(T);
-    __shared__ uint32_t s_max[THREADS / 32];
+    __shared__ uint32_t s_max[BLOCK / 32];
     pdl_enter();
     if (ROUTED) write_tiles(routes);
     const int sub = threadIdx.x % TPR, pieces = K / PER;
-    constexpr int ROWS = THREADS / TPR;
+    constexpr int ROWS = BLOCK / TPR;
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < rows; r0 += (long long)gridDim.x * ROWS) {
         const long long r = r0 + threadIdx.x / TPR;
-        const bool live = r < rows;                  // (whole warps: TPR >= 32)
+        const bool live = r < rows;
         const uint4* src = reinterpret_cast<const uint4*>(x + (live ? r : 0) * ldx);
-        uint4 raw[VEC_PER_THREAD];
+        uint4 raw[HELD];
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < VEC_PER_THREAD; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             const int c = sub + i * TPR;
             raw[i] = make_uint4(0u, 0u, 0u, 0u);
             if (live && c < pieces) raw[i] = __ldg(src + c);
         }
 #pragma unroll
-        for (int i = 0; i < VEC_PER_THREAD; ++i) {
+        for (int i = 0; i < HELD; ++i) {
             const T* v = reinterpret_cast<const T*>(&raw[i]);
 #pragma unroll
             for (int j = 0; j < PER; ++j) m = max(m, abs_bits(to_f(v[j])));
         }
-        m = row_max<TPR>(m, s_max);
+        m = row_max<TPR, BLOCK>(m, s_max);
         if (!live) continue;
         const float amax = __uint_as_float(m);
         const bool codable = m > 0 && finite_bits(m);
         const RowRule rule = row_rule(amax);
-        uint32_t o[VEC_PER_THREAD][PER / 4];
 #pragma unroll
-        for (int i = 0; i < VEC_PER_THREAD; ++i) {
+        for (int i = 0; i < HELD; ++i) {         // the codes take the place of the values
             const T* v = reinterpret_cast<const T*>(&raw[i]);
-#pragma unroll
-            for (int q = 0; q < PER / 4; ++q) {
-                o[i][q] = 0u;
-                if (codable && sub + i * TPR < pieces)
-                    o[i][q] = pack4(code_bits(to_f(v[4 * q]), rule), code_bits(to_f(v[4 * q + 1]), rule),
-                                    code_bits(to_f(v[4 * q + 2]), rule), code_bits(to_f(v[4 * q + 3]), rule));
+            uint2 o = make_uint2(0u, 0u);
+            if (codable && sub + i * TPR < pieces) {
+                o.x = four_codes(to_f(v[0]), to_f(v[1]), to_f(v[2]), to_f(v[3]), rule);
+                if (PER == 8) o.y = four_codes(to_f(v[PER - 4]), to_f(v[PER - 3]), to_f(v[PER - 2]), to_f(v[PER - 1]), rule);
             }
+            raw[i].x = o.x;
+            raw[i].y = o.y;
         }
         const Targets<ROUTED> to(r, routes);
         for (int s = 0; s < to.n; ++s) {
@@ -101,11 +102,11 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
             if (row < 0) continue;
             int8_t* dst = codes + row * ldc;
 #pragma unroll
-            for (int i = 0; i < VEC_PER_THREAD; ++i) {
+            for (int i = 0; i < HELD; ++i) {
                 const int c = sub + i * TPR;
                 if (c >= pieces) break;
-                if (PER == 8) *reinterpret_cast<uint2*>(dst + c * 8) = make_uint2(o[i][0], o[i][PER / 4 - 1]);
-                else *reinterpret_cast<uint32_t*>(dst + c * 4) = o[i][0];
+                if (PER == 8) *reinterpret_cast<uint2*>(dst + c * 8) = make_uint2(raw[i].x, raw[i].y);
+                else *reinterpret_cast<uint32_t*>(dst + c * 4) = raw[i].x;
             }
             if (sub == 0) scales[row] = amax / 127.f;
             for (int c = K + sub; c < ldc && c < K + 16; c += TPR) dst[c] = 0;     // the pitch's tail
@@ -125,7 +126,7 @@ quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ld
         const T* src = x + r * ldx;
         uint32_t m = 0;
         for (int c = threadIdx.x; c < K; c += THREADS) m = max(m, abs_bits(to_f(src[c])));
-        m = row_max<THREADS>(m, s_max);
+        m = row_max<THREADS, THREADS>(m, s_max);
         const float amax = __uint_as_float(m);
         const bool codable = m > 0 && finite_bits(m);
         const RowRule rule = row_rule(amax);
@@ -151,15 +152,22 @@ static cudaError_t launch_typed(const void* xv, long long rows, int K, long long
     const bool vec = (reinterpret_cast<uintptr_t>(x) & 15u) == 0 && K % PER == 0 && (ldx % PER == 0 || rows == 1) &&
                      (reinterpret_cast<uintptr_t>(codes) & 15u) == 0 && (ldc % 16 == 0 || one);
     const long long most = 148 * 16;
-    if (vec && K <= 32 * VEC_PER_THREAD * PER && rows >= 148 * 8) {      // enough rows for a warp each
-        const long long blocks = (rows + 7) / 8;
-        return launch_pdl(quantize_vec_kernel<T, 32, ROUTED>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(THREADS), 0, s,
-                          x, rows, K, ldx, codes, ldc, scales, routes);
-    }
-    const dim3 grid((unsigned)(rows < most ? rows : most));
-    if (vec && K <= THREADS * VEC_PER_THREAD * PER)
-        return launch_pdl(quantize_vec_kernel<T, THREADS, ROUTED>, grid, dim3(THREADS), 0, s, x, rows, K, ldx, codes, ldc, scales,
-                          routes);
+    // as few threads per row as hold it: a warp needs no barrier, but few rows want more threads each
+    const bool many = rows >= 148 * 8;
+    auto blocks = [&](int per_block) {
+        const long long n = (rows + per_block - 1) / per_block;
+        return dim3((unsigned)(n < most ? n : most));
+    };
+#define MOK_ROWS(TPR, BLOCK)                                                                                                   \
+    return launch_pdl(quantize_vec_kernel<T, TPR, BLOCK, ROUTED>, blocks(BLOCK / TPR), dim3(BLOCK), 0, s, x, rows, K, ldx, codes, \
+                      ldc, scales, routes)
+    if (vec && many && K <= 32 * HELD * PER) MOK_ROWS(32, 256);
+    if (vec && many && K <= 64 * HELD * PER) MOK_ROWS(64, 256);
+    if (vec && many && K <= 128 * HELD * PER) MOK_ROWS(128, 256);
+    if (vec && K <= 256 * HELD * PER) MOK_ROWS(256, 256);
+    if (vec && K <= 512 * HELD * PER) MOK_ROWS(512, 512);
+#undef MOK_ROWS
+    const dim3 grid = blocks(1);
     return launch_pdl(quantize_any_kernel<T, ROUTED>, grid, dim3(THREADS), 0, s, x, rows, K, ldx, codes, ldc, scales, routes);
 }
 

@@ -176,7 +176,7 @@ _lib.mok_i8_quantize.restype = ctypes.c_int
 _lib.mok_i8_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong,
                                  ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p]
 _lib.mok_i8_linear_workspace_bytes.restype = ctypes.c_size_t
-_lib.mok_i8_linear_workspace_bytes.argtypes = [ctypes.c_int] * 2
+_lib.mok_i8_linear_workspace_bytes.argtypes = [ctypes.POINTER(mok_i8_linear_args)]
 _lib.mok_i8_linear.restype = ctypes.c_int
 _lib.mok_i8_linear.argtypes = [ctypes.POINTER(mok_i8_linear_args)]
 _lib.mok_i8_experts_workspace_bytes.restype = ctypes.c_size_t
@@ -824,30 +824,34 @@ class I8Weights:
         return cls(*mok_i8_quantize(W, stream=stream))
 
 
-def _i8_product(x, x_codes, x_scales, x_stride, codes_stride, M, K, x_type, weights, bias, out_dtype, workspace,
-                workspace_bytes, device, raw_stream):
+def _i8_product(x, x_codes, x_scales, x_stride, codes_stride, M, K, x_type, weights, bias, out_dtype, workspace, device,
+                raw_stream):
     W = weights.codes
     N = W.shape[0]
     w_stride = _rows("weights.codes", W, K, device, _INT8)
     out = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=device)
-    _check(_lib.mok_i8_linear(mok_i8_linear_args(
+    a = mok_i8_linear_args(
         x, x_codes, x_scales, W.data_ptr(), _packed("weights.scales", weights.scales, (N,), device, torch.float32),
         None if bias is None else _packed("bias", bias, (N,), device, torch.float32), x_stride, codes_stride, w_stride, N,
-        M, K, N, x_type, _TYPES[out_dtype], out.data_ptr(), workspace, workspace_bytes, raw_stream)))
+        M, K, N, x_type, _TYPES[out_dtype], out.data_ptr(), None, 0, raw_stream)
+    if workspace is not None:
+        a.workspace, a.workspace_bytes = _aligned_ws(workspace)
+    elif x is not None:
+        n = _lib.mok_i8_linear_workspace_bytes(a)
+        if n:
+            workspace = torch.empty_strided((n,), (1,), dtype=torch.uint8, device=device)
+            a.workspace, a.workspace_bytes = workspace.data_ptr(), n
+    _check(_lib.mok_i8_linear(a))
     return out
 
 
 @_on_stream
 def mok_i8_linear(raw_stream, x, weights, bias=None, out_dtype=None, workspace=None):
     """out [M, N] = quantise(x [M, K]) W8^T (+ bias): the rows of x are quantised in the call.  weights: I8Weights [N, K];
-    out_dtype defaults to x's.  workspace: a uint8 tensor of mok_i8_linear_workspace_bytes(M, K) + 256 (None: allocated)."""
+    out_dtype defaults to x's.  workspace: a uint8 tensor of M * (K + 20) + 768 bytes (None: allocated if the call needs it)."""
     (M, K), device, dtype = x.shape, x.device, x.dtype
-    ldx = _rows("x", x, K, device, _TYPES)
-    if workspace is None:
-        workspace = torch.empty(_lib.mok_i8_linear_workspace_bytes(M, K), dtype=torch.uint8, device=device)
-    ws, ws_bytes = _aligned_ws(workspace)
-    return _i8_product(x.data_ptr(), None, None, ldx, 0, M, K, _TYPES[dtype], weights, bias, out_dtype or dtype, ws, ws_bytes,
-                       device, raw_stream)
+    return _i8_product(x.data_ptr(), None, None, _rows("x", x, K, device, _TYPES), 0, M, K, _TYPES[dtype], weights, bias,
+                       out_dtype or dtype, workspace, device, raw_stream)
 
 
 @_on_stream
@@ -855,9 +859,8 @@ def mok_i8_matmul(raw_stream, codes, scales, weights, K=None, bias=None, out_dty
     """out [M, N] from rows that are 8-bit already (mok_i8_quantize): codes int8 [M, >= K], scales fp32 [M]."""
     M, device = codes.shape[0], codes.device
     K = weights.codes.shape[1] if K is None else K
-    ldc = _rows("codes", codes, K, device, _INT8)
-    return _i8_product(None, codes.data_ptr(), _packed("scales", scales, (M,), device, torch.float32), 0, ldc, M, K, 0, weights,
-                       bias, out_dtype, None, 0, device, raw_stream)
+    return _i8_product(None, codes.data_ptr(), _packed("scales", scales, (M,), device, torch.float32), 0,
+                       _rows("codes", codes, K, device, _INT8), M, K, 0, weights, bias, out_dtype, None, device, raw_stream)
 
 
 def alloc_i8_workspace(T, H, I, E, k, device="cuda"):
@@ -901,10 +904,6 @@ def mok_i8_experts(raw_stream, x, topk_idx, topk_w, gate_up, down, add=None, wor
         _packed("down.max", down.max, (E,), device, torch.float32), None if add is None else add.data_ptr(),
         ldx, gu_pitch, dn_pitch, ld_add, H, T, H, I, E, k, _TYPES[dtype], out.data_ptr(), ws, ws_bytes, raw_stream)))
     return out
-
-
-def mok_i8_linear_workspace_bytes(M, K):
-    return int(_lib.mok_i8_linear_workspace_bytes(M, K))
 
 
 def mok_i8_experts_workspace_bytes(T, H, I, E, k):

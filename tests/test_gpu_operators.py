@@ -320,6 +320,20 @@ def test_linear_rows_do_not_depend_on_the_batch(mok):
         assert torch.equal(mok.mok_i8_linear(x[:M], w, out_dtype=torch.float32), whole[:M]), M
 
 
+@pytest.mark.parametrize("M,K,N", [(1, 16384, 128), (1, 300, 2000), (2, 640, 1), (5, 384, 300), (9, 900, 2300), (16, 14336, 130), (24, 5000, 640),
+                                   (40, 1100, 4100), (48, 2048, 1024), (63, 900, 300), (64, 7168, 256), (64, 24000, 64),
+                                   (64, 128, 128), (33, 127, 20000)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_linear_few_tokens(mok, M, K, N, dtype):
+    """The shapes by which a product of few tokens is split over K, quantised in the kernel or before it."""
+    g = gen(M + K + N)
+    x, w = randn(g, M, K).to(dtype), weights(mok, g, N, K)
+    out = mok.mok_i8_linear(x, w, out_dtype=torch.float32)
+    codes, scales = mok.mok_i8_quantize(x)
+    check_product(out, product64(codes, scales, w, None, K), None, torch.float32)
+    assert torch.equal(out, mok.mok_i8_matmul(codes, scales, w, K=K, out_dtype=torch.float32))
+
+
 def test_linear_largest_sums_and_poisoned_rows(mok):
     K = 131072
     codes = torch.full((3, K), 127, device="cuda", dtype=torch.int8)
@@ -519,7 +533,7 @@ def test_refusals(mok):
                           mok.I8Weights(w.codes[:, :24].contiguous(), w.scales))
     assert err.value.status == mok.MOK_ERR_ALIGN                                            # rows of 24 bytes
     with pytest.raises(E) as err:
-        mok.mok_i8_linear(x, w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+        mok.mok_i8_linear(randn(g, 300, 32).bfloat16(), w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
     assert err.value.status == mok.MOK_ERR_WORKSPACE
     idx, tw = routes(g, 4, 4, 2)
     gu, dn = weights(mok, g, 4, 16, 32), weights(mok, g, 4, 32, 8)
