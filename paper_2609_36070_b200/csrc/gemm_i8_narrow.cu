@@ -1,13 +1,12 @@
 // Products of 8-bit operands with few tokens (a decoding step): bound by reading the weights once, so the shape is chosen for
 // memory, not for the tensor cores.
 //
-// The weights sit on the MMA's M side (128 output channels per tile, tcgen05.mma.kind::i8), the tokens on its N side (16, 32
-// or 64 columns).  A cluster of S CTAs shares one channel tile and splits K: with a few dozen channel tiles a split is what
+// The weights sit on the MMA's M side (128 output channels per tile, tcgen05.mma.kind::i8), the tokens on its N side (16 to
+// 256 columns).  A cluster of S CTAs shares one channel tile and splits K: with a few dozen channel tiles a split is what
 // puts the reading onto all SMs.  Per CTA
-//   1. a TMA ring starts to stream the CTA's K range of the 128 weight rows
-//   2. meanwhile all warps bring the tokens' K range into shared memory as the (swizzled) B operand, which stays resident:
-//      codes are copied; activations are quantised right here -- every CTA takes the maxima of its range, the cluster
-//      exchanges them -- which spares a launch and a round trip through memory
+//   1. a TMA ring streams the CTA's K range of the 128 weight rows and of the tokens' codes
+//   2. or, a few rows of activations are quantised right here, into a (128-byte swizzled) B operand that stays: every CTA
+//      takes the maxima of its range, the cluster exchanges them, which spares a launch and a round trip through memory
 //   3. one thread issues the MMAs as the stages land
 //   4. the 32-bit sums go from TMEM to shared memory; each CTA of the cluster adds up its share of the tokens over the
 //      cluster (integer sums: exact in any order), scales and stores them
@@ -24,13 +23,15 @@ constexpr int NARROW_THREADS = 512, NARROW_WARPS = NARROW_THREADS / 32;
 constexpr int NARROW_STAGE = 128 * 128;          // 128 channels x 128 bytes of K
 constexpr int NARROW_MAX_STAGES = 10;
 constexpr int NARROW_SMEM = 232448;
-constexpr int NARROW_CTRL = 1024;                // barriers, row maxima
+constexpr int NARROW_CTRL = 2048;                // barriers, row maxima and scales
+constexpr int NARROW_TOKENS = 256;               // most columns of the MMA
+constexpr int NARROW_HELD = 64;                  // most rows that are quantised in the kernel
 
 struct NarrowCtrl {
     uint64_t full[NARROW_MAX_STAGES], empty[NARROW_MAX_STAGES], tfull;
     uint32_t tmem_base, abort;
-    uint32_t amax[64], top[64];                  // row maxima over this CTA's K range, and over the cluster's
-    float scale[64];
+    uint32_t amax[NARROW_HELD], top[NARROW_HELD];    // row maxima over this CTA's K range, and over the cluster's
+    float scale[NARROW_TOKENS];
 };
 static_assert(sizeof(NarrowCtrl) <= NARROW_CTRL, "control block too large");
 
@@ -43,6 +44,12 @@ __device__ __forceinline__ uint32_t ld_cluster(uint32_t addr, uint32_t rank) {
     uint32_t v;
     asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %1, %2;\n\tld.shared::cluster.u32 %0, [ra];\n\t}"
                  : "=r"(v) : "r"(addr), "r"(rank) : "memory");
+    return v;
+}
+__device__ __forceinline__ int4 ld_cluster4(uint32_t addr, uint32_t rank) {
+    int4 v;
+    asm volatile("{\n\t.reg .b32 ra;\n\tmapa.shared::cluster.u32 ra, %4, %5;\n\tld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [ra];\n\t}"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr), "r"(rank) : "memory");
     return v;
 }
 __device__ __forceinline__ constexpr uint32_t narrow_idesc(int n) {
@@ -69,12 +76,11 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
 template <class T> struct Held { static constexpr int pieces = sizeof(T) == 2 ? 4 : 2; };
 
 struct NarrowArgs {
-    const void* x;               // activations of x_type, or NULL: codes and scales are given
-    const int8_t* codes;
+    const void* x;               // activations, or NULL: codes and scales are given
     const float* scales;
-    long long ldx, ldc;          // elements of x, bytes of codes
+    long long ldx;
     int32_t M, K, N;
-    int32_t bn;                  // columns of the MMA: 16, 32 or 64
+    int32_t bn;                  // columns of the MMA: 16, 32, 64, 128 or 256
     int32_t stages;
     const float* w_scale;
     const float* bias;
@@ -145,19 +151,24 @@ __device__ __forceinline__ void quantise_range(const NarrowArgs& a, int k0, int 
 // X: the activations' type, int8_t for codes
 template <class X, class O>
 __global__ void __launch_bounds__(NARROW_THREADS, 1)
-product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_constant__ NarrowArgs a) {
+product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_constant__ CUtensorMap tmapX,
+                      const __grid_constant__ NarrowArgs a) {
+    constexpr bool CODES = sizeof(X) == 1;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int S = (int)cluster_size(), rank = (int)cluster_ctarank();
-    const int tile = blockIdx.x / S;
+    const int tiles_n = (a.N + 127) / 128, unit = blockIdx.x / S, tile = unit % tiles_n;     // channel tile ...
+    const int t0 = unit / tiles_n * a.bn, M = min(a.bn, a.M - t0);                            // ... and tokens of this cluster
     const int kb_all = (a.K + 127) / 128;
     const int kb0 = (int)((long long)kb_all * rank / S), kb1 = (int)((long long)kb_all * (rank + 1) / S), n_kb = kb1 - kb0;
     const int k0 = kb0 * 128, k1 = kb1 * 128;
-    // ring of weight stages | tokens [n_kb][bn][128 bytes] | control block; the sums reuse the ring
-    uint8_t* tok = smem + a.stages * NARROW_STAGE;
-    const int most_kb = (kb_all + S - 1) / S;
-    NarrowCtrl* ctrl = reinterpret_cast<NarrowCtrl*>(tok + (size_t)most_kb * a.bn * 128);
+    // ring of stages (weights, codes) | quantised tokens [n_kb][bn][128 bytes] | control block; the sums reuse the ring
+    const uint32_t tok_bytes = (uint32_t)a.bn * 128, stage_bytes = NARROW_STAGE + (CODES ? tok_bytes : 0u);
+    uint8_t* tok = smem + a.stages * stage_bytes;
+    const int most_kb = CODES ? 0 : (kb_all + S - 1) / S;
+    const uint32_t tmem_cols = a.bn <= 64 ? 64u : (uint32_t)a.bn;
+    NarrowCtrl* ctrl = reinterpret_cast<NarrowCtrl*>(tok + (size_t)most_kb * tok_bytes);
     volatile uint32_t* abort_flag = &ctrl->abort;
 
     if (threadIdx.x == 0) {
@@ -170,10 +181,10 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (threadIdx.x < 64) ctrl->amax[threadIdx.x] = 0u;
+    if (threadIdx.x < NARROW_HELD) ctrl->amax[threadIdx.x] = 0u;
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(&ctrl->tmem_base)), "r"(64u) : "memory");
+                     ::"r"(smem_u32(&ctrl->tmem_base)), "r"(tmem_cols) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -184,26 +195,19 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
 
     // the first stages of the weights are on their way before the tokens are looked at
     const int ahead = n_kb < a.stages ? n_kb : a.stages;
-    if (threadIdx.x == 0) {
-        for (int s = 0; s < ahead; ++s) {
-            mbar_expect_tx(smem_u32(&ctrl->full[s]), NARROW_STAGE);
-            tma_load_2d(base + s * NARROW_STAGE, &tmapW, smem_u32(&ctrl->full[s]), (kb0 + s) * 128, tile * 128);
-        }
-    }
+    auto load = [&](int s, int kb) {
+        const uint32_t full = smem_u32(&ctrl->full[s]);
+        mbar_expect_tx(full, stage_bytes);
+        tma_load_2d(base + s * stage_bytes, &tmapW, full, (kb0 + kb) * 128, tile * 128);
+        if (CODES) tma_load_2d(base + s * stage_bytes + NARROW_STAGE, &tmapX, full, (kb0 + kb) * 128, t0);
+    };
+    if (threadIdx.x == 0)
+        for (int s = 0; s < ahead; ++s) load(s, s);
     __syncwarp();
-    if constexpr (sizeof(X) > 1) {
-        quantise_range<X>(a, k0, k1, tok, ctrl, warp, lane, S);
+    if constexpr (CODES) {
+        if ((int)threadIdx.x < M) ctrl->scale[threadIdx.x] = __ldg(a.scales + t0 + threadIdx.x);
     } else {
-        // codes, in 16-byte pieces; zeros past K
-        const int pieces = n_kb * 8;
-        for (int i = threadIdx.x; i < a.M * pieces; i += NARROW_THREADS) {
-            const int r = i / pieces, c = i - r * pieces;
-            const uint32_t dst = smem_u32(tok) + ((c >> 3) * a.bn + r) * 128 + (((c & 7) ^ (r & 7)) << 4);
-            const int left = a.K - (k0 + c * 16);
-            cp_async_16(dst, left > 0 ? a.codes + r * a.ldc + k0 + c * 16 : a.codes, left >= 16 ? 16u : left > 0 ? (uint32_t)left : 0u);
-        }
-        if ((int)threadIdx.x < a.M) ctrl->scale[threadIdx.x] = __ldg(a.scales + threadIdx.x);
-        asm volatile("cp.async.wait_all;" ::: "memory");
+        quantise_range<X>(a, k0, k1, tok, ctrl, warp, lane, S);
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the MMAs read what was just written
     __syncthreads();
@@ -214,8 +218,7 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
             uint32_t ph = 0;
             for (int kb = ahead; kb < n_kb; ++kb) {
                 if (!mbar_wait(smem_u32(&ctrl->empty[s]), ph, abort_flag, a.header, 21)) break;
-                mbar_expect_tx(smem_u32(&ctrl->full[s]), NARROW_STAGE);
-                tma_load_2d(base + s * NARROW_STAGE, &tmapW, smem_u32(&ctrl->full[s]), (kb0 + kb) * 128, tile * 128);
+                load(s, kb);
                 if (++s == a.stages) { s = 0; ph ^= 1u; }
             }
         }
@@ -228,8 +231,8 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
             for (int kb = 0; kb < n_kb; ++kb) {
                 if (!mbar_wait(smem_u32(&ctrl->full[s]), ph, abort_flag, a.header, 22)) break;
                 tc_fence_after();
-                const uint64_t adesc = make_smem_desc(base + s * NARROW_STAGE);
-                const uint64_t bdesc = make_smem_desc(smem_u32(tok) + kb * a.bn * 128);
+                const uint64_t adesc = make_smem_desc(base + s * stage_bytes);
+                const uint64_t bdesc = make_smem_desc(CODES ? base + s * stage_bytes + NARROW_STAGE : smem_u32(tok) + kb * tok_bytes);
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     mma_one(tmem, adesc + (uint64_t)(j * 2), bdesc + (uint64_t)(j * 2), idesc, (kb | j) ? 1u : 0u);
@@ -246,32 +249,53 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
     int32_t* sums = reinterpret_cast<int32_t*>(smem);
     ok = __all_sync(0xffffffffu, ok);
     if (ok && n_kb > 0) {
-        const int c = (warp >> 2) * 16;          // four warps per 16 tokens
-        if (c < a.M) {
+        for (int c = (warp >> 2) * 16; c < M; c += NARROW_WARPS * 4) {     // four warps per 16 tokens
             uint32_t r[16];
             tc_ld16(tmem + (uint32_t)c + ((uint32_t)((warp & 3) * 32) << 16), r);
             tc_wait_ld();
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (c + i < a.M) sums[(c + i) * 128 + (warp & 3) * 32 + lane] = (int32_t)r[i];
+                if (c + i < M) sums[(c + i) * 128 + (warp & 3) * 32 + lane] = (int32_t)r[i];
         }
     } else {
-        for (int i = threadIdx.x; i < a.M * 128; i += NARROW_THREADS) sums[i] = 0;       // an empty K range
+        for (int i = threadIdx.x; i < M * 128; i += NARROW_THREADS) sums[i] = 0;       // an empty K range
     }
     tc_fence_before();
     __syncthreads();
     if (S > 1) cluster_sync();
     {
-        const int ch = threadIdx.x & 127, n = tile * 128 + ch;
-        if (n < a.N) {
-            const float ws = __ldg(a.w_scale + n), b = a.bias ? __ldg(a.bias + n) : 0.f;
-            for (int t = rank + S * (threadIdx.x >> 7); t < a.M; t += NARROW_THREADS / 128 * S) {
-                int32_t sum = 0;
-                if (S == 1) sum = sums[t * 128 + ch];
-                else
-                    for (int q = 0; q < S; ++q) sum += (int32_t)ld_cluster(base + (uint32_t)(t * 128 + ch) * 4, (uint32_t)q);
-                const float v = (float)sum * ctrl->scale[t] * ws + b;
-                reinterpret_cast<O*>(a.out)[(long long)t * a.ldo + n] = from_f<O>(v);
+        // a warp takes a token, a lane four channels
+        const int ch = lane * 4, n = tile * 128 + ch;
+        float ws[4], bs[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            ws[j] = n + j < a.N ? __ldg(a.w_scale + n + j) : 0.f;
+            bs[j] = a.bias && n + j < a.N ? __ldg(a.bias + n + j) : 0.f;
+        }
+        const bool vec = n + 4 <= a.N && ((reinterpret_cast<uintptr_t>(a.out) | (uintptr_t)(a.ldo * sizeof(O))) & (4 * sizeof(O) - 1)) == 0;
+        for (int t = rank + S * warp; t < M; t += NARROW_WARPS * S) {
+            int4 sum = make_int4(0, 0, 0, 0);
+            if (S == 1) {
+                sum = *reinterpret_cast<const int4*>(sums + t * 128 + ch);
+            } else {
+                for (int q = 0; q < S; ++q) {
+                    const int4 p = ld_cluster4(base + (uint32_t)(t * 128 + ch) * 4, (uint32_t)q);
+                    sum.x += p.x; sum.y += p.y; sum.z += p.z; sum.w += p.w;
+                }
+            }
+            const float xs = ctrl->scale[t];
+            const float v[4] = {(float)sum.x * xs * ws[0] + bs[0], (float)sum.y * xs * ws[1] + bs[1],
+                                (float)sum.z * xs * ws[2] + bs[2], (float)sum.w * xs * ws[3] + bs[3]};
+            O* dst = reinterpret_cast<O*>(a.out) + (long long)(t0 + t) * a.ldo + n;
+            if (vec) {
+                struct alignas(4 * sizeof(O)) { O e[4]; } o;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o.e[j] = from_f<O>(v[j]);
+                *reinterpret_cast<decltype(o)*>(dst) = o;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (n + j < a.N) dst[j] = from_f<O>(v[j]);
             }
         }
     }
@@ -283,12 +307,12 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
     if (S > 1) cluster_sync();                   // the peers have read this CTA's sums
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(64u) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(tmem_cols) : "memory");
     }
 }
 
 template <class X, class O>
-static cudaError_t launch_narrow_typed(const CUtensorMap& mW, const NarrowArgs& a, int S, int tiles, size_t smem, cudaStream_t s) {
+static cudaError_t launch_narrow_typed(const CUtensorMap& mW, const CUtensorMap& mX, const NarrowArgs& a, int S, int tiles, size_t smem, cudaStream_t s) {
     static PerDevice configured;
     auto kernel = product_narrow_kernel<X, O>;
     int dev = 0, sms = 0;
@@ -313,64 +337,100 @@ static cudaError_t launch_narrow_typed(const CUtensorMap& mW, const NarrowArgs& 
     cfg.stream = s;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, kernel, mW, a);
+    return cudaLaunchKernelEx(&cfg, kernel, mW, mX, a);
 }
 
-// Split of K: the S of 1 .. 8 with the least k-blocks one after the other, if every CTA had an SM; false if the tokens' K
-// range does not fit beside four stages of weights.
-static bool narrow_shape(int M, int K, int N, int* bn, int* split, int* stages, size_t* smem) {
-    if (M > 64) return false;
-    *bn = M <= 16 ? 16 : M <= 32 ? 32 : 64;
-    const int kb = (K + 127) / 128, tiles = (N + 127) / 128;
-    int best = 0;
-    long long cost = 0;
-    for (int S = 1; S <= 8 && S <= kb; ++S) {
-        const int most = (kb + S - 1) / S;
-        const long long room = NARROW_SMEM - NARROW_CTRL - (long long)most * *bn * 128;
-        if (room < 4 * NARROW_STAGE) continue;
-        const long long c = ((long long)tiles * S + 147) / 148 * most * 8 + S;        // (a larger cluster exchanges more)
-        if (!best || c < cost) {
-            best = S;
-            cost = c;
-            const int n = (int)(room / NARROW_STAGE), least = (*bn * 128 * 4 + NARROW_STAGE - 1) / NARROW_STAGE;
-            *stages = n < NARROW_MAX_STAGES ? n : NARROW_MAX_STAGES;
-            if (*stages > most) *stages = most > least ? most : least;                // (the sums need room too)
-            *smem = (size_t)*stages * NARROW_STAGE + (size_t)most * *bn * 128 + NARROW_CTRL;
+// Clusters of S CTAs with a whole SM each that run at once (how many fit depends on how the SMs are grouped: 148 SMs hold 33
+// clusters of four, but only 15 of eight).
+static int narrow_clusters(int S) {
+    static PerDevice known[9];
+    int dev = 0, n = 0;
+    if (current_device(&dev) == cudaSuccess &&
+        known[S].get(dev, &n, [&](int, int* out) {
+            auto kernel = product_narrow_kernel<int8_t, __nv_bfloat16>;
+            cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NARROW_SMEM);
+            if (e != cudaSuccess) return e;
+            cudaLaunchConfig_t cfg = {};
+            cudaLaunchAttribute attr[1];
+            attr[0].id = cudaLaunchAttributeClusterDimension;
+            attr[0].val.clusterDim.x = (unsigned)S;
+            attr[0].val.clusterDim.y = 1;
+            attr[0].val.clusterDim.z = 1;
+            cfg.gridDim = dim3((unsigned)(148 * S));
+            cfg.blockDim = dim3(NARROW_THREADS);
+            cfg.dynamicSmemBytes = NARROW_SMEM;
+            cfg.attrs = attr;
+            cfg.numAttrs = 1;
+            return cudaOccupancyMaxActiveClusters(out, kernel, &cfg);
+        }) == cudaSuccess)
+        return n;
+    return 128 / S;
+}
+
+// The tile width and the split of K by which the product is done first.  Measured: 4.8 us for a wave of CTAs and 15 us for
+// each MB that one of them brings in (16 tokens, 4096 x 4096: 7.0; 256 tokens: 10.7).  held: the tokens are quantised in the
+// kernel, their K range has to fit beside the ring.
+struct NarrowShape { int bn, split, stages; size_t smem; double us; };
+static bool narrow_shape(int M, int K, int N, bool held, NarrowShape* out) {
+    if (held && M > NARROW_HELD) return false;
+    const int kb = (K + 127) / 128, tiles_n = (N + 127) / 128;
+    out->split = 0;
+    for (int bn = 16; bn <= NARROW_TOKENS; bn *= 2) {
+        if (M > bn && bn < 128) continue;                                // (only the wide tiles are laid side by side)
+        const long long tiles = (long long)tiles_n * ((M + bn - 1) / bn);
+        if (tiles > 1 << 16) continue;
+        for (int S = 1; S <= 8 && S <= kb; ++S) {
+            const int most = (kb + S - 1) / S, stage = NARROW_STAGE + (held ? 0 : bn * 128);
+            const long long tok = held ? (long long)most * bn * 128 : 0;
+            int stages = (int)((NARROW_SMEM - NARROW_CTRL - tok) / stage);
+            const int least = (bn * 128 * 4 + stage - 1) / stage;        // (the sums reuse the ring)
+            if (stages < 4 || stages < least) continue;
+            const int at_once = narrow_clusters(S);
+            const double us = (double)((tiles + at_once - 1) / at_once) * (4.8 + 15e-6 * most * (NARROW_STAGE + bn * 128));
+            if (out->split && us >= out->us) continue;
+            if (stages > NARROW_MAX_STAGES) stages = NARROW_MAX_STAGES;
+            if (stages > most) stages = most > least ? most : least;
+            *out = NarrowShape{bn, S, stages, (size_t)stages * stage + (size_t)tok + NARROW_CTRL, us};
         }
+        if (M <= bn) break;                                              // (a wider tile would only hold more padding)
     }
-    *split = best;
-    return best > 0;
+    return out->split > 0;
 }
 
-// Whether the narrow kernel takes a product, and whether it quantises the activations itself: as far as the registers hold a
-// CTA's share, from whole 16-byte pieces (x_align: the bits that x's address and row pitch have set).
+// Whether the narrow kernel takes a product: unless the pair tiles of 256 x 256 are done sooner (measured: 8.4 us and 6 to
+// 11 us for each MB that a pair's SM brings in, 32 KB for each k-block).  quantises: it takes activations, as far as the registers hold a CTA's share of them, from whole 16-byte pieces
+// (x_align: the bits that x's address and row pitch have set).
 bool narrow_product(int M, int K, int N, int x_type, unsigned long long x_align, bool* quantises) {
-    int bn, S, stages;
-    size_t smem;
-    if (!narrow_shape(M, K, N, &bn, &S, &stages, &smem)) return false;
-    const int most = ((K + 127) / 128 + S - 1) / S;
-    *quantises = K % 8 == 0 && (x_align & 15u) == 0 &&
-                 M * ((most + 1) / 2) <= NARROW_WARPS * (x_type == MOK_TYPE_F32 ? Held<float>::pieces : Held<__half>::pieces);
-    return true;
+    NarrowShape held, shape;
+    *quantises = false;
+    if (x_type >= 0 && K % 8 == 0 && (x_align & 15u) == 0 && narrow_shape(M, K, N, true, &held)) {
+        const int most = ((K + 127) / 128 + held.split - 1) / held.split;
+        *quantises = M * ((most + 1) / 2) <= NARROW_WARPS * (x_type == MOK_TYPE_F32 ? Held<float>::pieces : Held<__half>::pieces);
+    }
+    if (*quantises) return true;
+    if (!narrow_shape(M, K, N, false, &shape)) return false;
+    const long long waves = ((long long)((N + 255) / 256) * ((M + 255) / 256) + 73) / 74;
+    return shape.us <= 8.4 + 8e-6 * (double)waves * ((K + 127) / 128) * 32768;
 }
 
 template <class X>
-static cudaError_t launch_narrow_out(const CUtensorMap& mW, const NarrowArgs& a, int c_type, int S, int tiles, size_t smem,
+static cudaError_t launch_narrow_out(const CUtensorMap& mW, const CUtensorMap& mX, const NarrowArgs& a, int c_type, int S, int tiles, size_t smem,
                                      cudaStream_t s) {
-    if (c_type == MOK_TYPE_F32) return launch_narrow_typed<X, float>(mW, a, S, tiles, smem, s);
-    if (c_type == MOK_TYPE_F16) return launch_narrow_typed<X, __half>(mW, a, S, tiles, smem, s);
-    return launch_narrow_typed<X, __nv_bfloat16>(mW, a, S, tiles, smem, s);
+    if (c_type == MOK_TYPE_F32) return launch_narrow_typed<X, float>(mW, mX, a, S, tiles, smem, s);
+    if (c_type == MOK_TYPE_F16) return launch_narrow_typed<X, __half>(mW, mX, a, S, tiles, smem, s);
+    return launch_narrow_typed<X, __nv_bfloat16>(mW, mX, a, S, tiles, smem, s);
 }
 
 cudaError_t launch_narrow(const ProductArgs& g, const void* x, int x_type, long long ldx, cudaStream_t s) {
     NarrowArgs a = {};
-    int S = 1;
-    size_t smem = 0;
-    if (!narrow_shape(g.dense_rows, g.K, g.N, &a.bn, &S, &a.stages, &smem)) return cudaErrorInvalidValue;
+    NarrowShape shape;
+    if (!narrow_shape(g.dense_rows, g.K, g.N, x != nullptr, &shape)) return cudaErrorInvalidValue;
+    const int S = shape.split;
+    const size_t smem = shape.smem;
+    a.bn = shape.bn;
+    a.stages = shape.stages;
     a.x = x;
     a.ldx = ldx;
-    a.codes = g.A;
-    a.ldc = g.lda;
     a.scales = g.a_scale;
     a.M = g.dense_rows; a.K = g.K; a.N = g.N;
     a.w_scale = g.b_scale;
@@ -383,10 +443,14 @@ cudaError_t launch_narrow(const ProductArgs& g, const void* x, int x_type, long 
                          CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
     const int tiles = (g.N + 127) / 128;
-    if (!x) return launch_narrow_out<int8_t>(mW, a, g.c_type, S, tiles, smem, s);
-    if (x_type == MOK_TYPE_F32) return launch_narrow_out<float>(mW, a, g.c_type, S, tiles, smem, s);
-    if (x_type == MOK_TYPE_F16) return launch_narrow_out<__half>(mW, a, g.c_type, S, tiles, smem, s);
-    return launch_narrow_out<__nv_bfloat16>(mW, a, g.c_type, S, tiles, smem, s);
+    CUtensorMap mX = mW;
+    if (!x && !tmap::encode_2d(&mX, CU_TENSOR_MAP_DATA_TYPE_UINT8, g.A, (uint64_t)a.M, (uint64_t)g.K, (uint64_t)g.lda, 128,
+                               (uint32_t)a.bn, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    if (!x) return launch_narrow_out<int8_t>(mW, mX, a, g.c_type, S, tiles * ((g.dense_rows + a.bn - 1) / a.bn), smem, s);
+    if (x_type == MOK_TYPE_F32) return launch_narrow_out<float>(mW, mX, a, g.c_type, S, tiles, smem, s);
+    if (x_type == MOK_TYPE_F16) return launch_narrow_out<__half>(mW, mX, a, g.c_type, S, tiles, smem, s);
+    return launch_narrow_out<__nv_bfloat16>(mW, mX, a, g.c_type, S, tiles, smem, s);
 }
 
 }  // namespace i8

@@ -99,7 +99,8 @@ struct RouteArgs {
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s);
-// few tokens (EPI_PLAIN, dense): whether the kernel for them takes the product; quantises: activations instead of codes
+// few tokens (EPI_PLAIN, dense): whether the kernel for them takes the product; quantises: from the activations (of x_type, -1:
+// there are only codes)
 bool narrow_product(int M, int K, int N, int x_type, unsigned long long x_align, bool* quantises);
 cudaError_t launch_narrow(const ProductArgs& a, const void* x, int x_type, long long ldx, cudaStream_t s);
 cudaError_t status_header(WsHeader** out);

@@ -248,7 +248,7 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
     g.dense_rows = a->M;
     g.max_mt = (a->M + 2 * TILE_M - 1) / (2 * TILE_M);
     bool quantises = false;
-    const bool narrow = i8::narrow_product(a->M, a->K, a->N, a->x_type, x_alignment(a), &quantises);
+    const bool narrow = i8::narrow_product(a->M, a->K, a->N, coded ? -1 : a->x_type, x_alignment(a), &quantises);
     if (coded) {
         g.A = a->x_codes;
         g.lda = a->codes_stride;

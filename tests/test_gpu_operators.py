@@ -322,7 +322,9 @@ def test_linear_rows_do_not_depend_on_the_batch(mok):
 
 @pytest.mark.parametrize("M,K,N", [(1, 16384, 128), (1, 300, 2000), (2, 640, 1), (5, 384, 300), (9, 900, 2300), (16, 14336, 130), (24, 5000, 640),
                                    (40, 1100, 4100), (48, 2048, 1024), (63, 900, 300), (64, 7168, 256), (64, 24000, 64),
-                                   (64, 128, 128), (33, 127, 20000)])
+                                   (64, 128, 128), (33, 127, 20000),
+                                   (65, 4096, 4096), (100, 2000, 1000), (128, 7168, 2048), (129, 1024, 500), (200, 4096, 4100),
+                                   (256, 2048, 7168), (256, 130, 300), (255, 14336, 512)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_linear_few_tokens(mok, M, K, N, dtype):
     """The shapes by which a product of few tokens is split over K, quantised in the kernel or before it."""
