@@ -20,7 +20,7 @@
 // K, N and the rows may be ragged: TMA fills bytes past K and rows past the tensor with zeros, stores are masked.
 // All mbarrier waits are bounded; on a timeout the CTA records MOK_ERR_TIMEOUT and leaves cleanly.
 #include "i8_common.cuh"
-#include "tc_ptx.cuh"
+#include "i8_ptx.cuh"
 #include "tensor_map.cuh"
 
 namespace mok {
@@ -171,10 +171,6 @@ __device__ __forceinline__ void store_any(const float (&v)[32], uint32_t slabs, 
         }
     }
 }
-
-// silu(g) u.  The exponential and the quotient are good to about 2^-21: what follows is a rounding to 8-bit codes, which an
-// 11-bit tanh would move in one case of fifty.
-__device__ __forceinline__ float gated(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
 
 template <int EPI>
 __global__ void __launch_bounds__(THREADS, 1)

@@ -11,7 +11,7 @@
 //   4. the 32-bit sums go from TMEM to shared memory; each CTA of the cluster adds up its share of the tokens over the
 //      cluster (integer sums: exact in any order), scales and stores them
 #include "i8_common.cuh"
-#include "tc_ptx.cuh"
+#include "i8_ptx.cuh"
 #include "tensor_map.cuh"
 
 namespace mok {
@@ -55,22 +55,6 @@ __device__ __forceinline__ int4 ld_cluster4(uint32_t addr, uint32_t rank) {
 __device__ __forceinline__ constexpr uint32_t narrow_idesc(int n) {
     return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-__device__ __forceinline__ void mma_one(uint32_t d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::i8 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-__device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
-}
-
 // Pieces of eight activations that a thread holds.  Few, and no path for unaligned rows: code that runs once is paid for by
 // its instruction fetches (twelve pieces: 3000 instructions per warp, 15 us).
 template <class T> struct Held { static constexpr int pieces = sizeof(T) == 2 ? 4 : 2; };
@@ -342,14 +326,16 @@ static cudaError_t launch_narrow_typed(const CUtensorMap& mW, const CUtensorMap&
 
 // Clusters of S CTAs with a whole SM each that run at once (how many fit depends on how the SMs are grouped: 148 SMs hold 33
 // clusters of four, but only 15 of eight).
-static int narrow_clusters(int S) {
-    static PerDevice known[9];
-    int dev = 0, n = 0;
-    if (current_device(&dev) == cudaSuccess &&
-        known[S].get(dev, &n, [&](int, int* out) {
-            auto kernel = product_narrow_kernel<int8_t, __nv_bfloat16>;
-            cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NARROW_SMEM);
-            if (e != cudaSuccess) return e;
+static const int* narrow_clusters() {
+    static PerDevice ready;
+    static int known[MAX_DEVICES][9];
+    static const int guess[9] = {0, 148, 74, 45, 33, 26, 22, 15, 15};    // (without a device: the sizes of a workspace query)
+    int dev = 0, one = 0;
+    if (current_device(&dev) != cudaSuccess) return guess;
+    const cudaError_t e = ready.get(dev, &one, [&](int d, int* out) {
+        auto kernel = product_narrow_kernel<int8_t, __nv_bfloat16>;
+        cudaError_t e2 = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, NARROW_SMEM);
+        for (int S = 1; S <= 8 && e2 == cudaSuccess; ++S) {
             cudaLaunchConfig_t cfg = {};
             cudaLaunchAttribute attr[1];
             attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -361,10 +347,13 @@ static int narrow_clusters(int S) {
             cfg.dynamicSmemBytes = NARROW_SMEM;
             cfg.attrs = attr;
             cfg.numAttrs = 1;
-            return cudaOccupancyMaxActiveClusters(out, kernel, &cfg);
-        }) == cudaSuccess)
-        return n;
-    return 128 / S;
+            e2 = cudaOccupancyMaxActiveClusters(&known[d][S], kernel, &cfg);
+            if (known[d][S] < 1) known[d][S] = 1;
+        }
+        *out = 1;
+        return e2;
+    });
+    return e == cudaSuccess ? known[dev] : guess;
 }
 
 // The tile width and the split of K by which the product is done first.  Measured: 4.8 us for a wave of CTAs and 15 us for
@@ -374,6 +363,7 @@ struct NarrowShape { int bn, split, stages; size_t smem; double us; };
 static bool narrow_shape(int M, int K, int N, bool held, NarrowShape* out) {
     if (held && M > NARROW_HELD) return false;
     const int kb = (K + 127) / 128, tiles_n = (N + 127) / 128;
+    const int* at_once = narrow_clusters();
     out->split = 0;
     for (int bn = 16; bn <= NARROW_TOKENS; bn *= 2) {
         if (M > bn && bn < 128) continue;                                // (only the wide tiles are laid side by side)
@@ -385,8 +375,7 @@ static bool narrow_shape(int M, int K, int N, bool held, NarrowShape* out) {
             int stages = (int)((NARROW_SMEM - NARROW_CTRL - tok) / stage);
             const int least = (bn * 128 * 4 + stage - 1) / stage;        // (the sums reuse the ring)
             if (stages < 4 || stages < least) continue;
-            const int at_once = narrow_clusters(S);
-            const double us = (double)((tiles + at_once - 1) / at_once) * (4.8 + 15e-6 * most * (NARROW_STAGE + bn * 128));
+            const double us = (double)((tiles + at_once[S] - 1) / at_once[S]) * (4.8 + 15e-6 * most * (NARROW_STAGE + bn * 128));
             if (out->split && us >= out->us) continue;
             if (stages > NARROW_MAX_STAGES) stages = NARROW_MAX_STAGES;
             if (stages > most) stages = most > least ? most : least;

@@ -89,7 +89,7 @@ struct ProductArgs {
 enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
 
 // Where a token's codes go when its rows are wanted in expert order: row pos[t * k + s] for every routed slot s.
-// The launch also writes the product's tile list from the schedule's tables.
+// With `tiles` the launch also writes the product's list of row tiles from the schedule's tables.
 struct RouteArgs {
     const int32_t *idx, *pos;
     int32_t E, k;
@@ -99,6 +99,8 @@ struct RouteArgs {
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s);
+// few rows per expert (EPI_GATED, EPI_HALF); most_rows: that any expert can have (all routes, for ids may repeat)
+cudaError_t launch_grouped(const ProductArgs& a, int epi, int most_rows, cudaStream_t s);
 // few tokens (EPI_PLAIN, dense): whether the kernel for them takes the product; quantises: from the activations (of x_type, -1:
 // there are only codes)
 bool narrow_product(int M, int K, int N, int x_type, unsigned long long x_align, bool* quantises);

@@ -1,6 +1,6 @@
 // Routed expert FFNs in 8-bit integers: out[t] = add[t] + sum_s w[t, s] f_{idx[t, s]}(x[t]), every product with exact
 // integer sums and one scale per row and per channel.
-//   1. dispatch schedule (the layer's own kernels)
+//   1. dispatch schedule (in one block, or the layer's own kernels)
 //   2. token rows -> codes: found once per token, written once per route, in expert order.  (Gathering the rows in the product
 //      instead, with gathering TMA loads of four rows, took 70 cycles per load and three times the product's own time.)
 //   3. gate/up product, h = silu(g) u in fp32
@@ -74,7 +74,7 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
     }
 }
 
-// One block per token.  Slots whose expert id is outside 0 .. E-1 are not routed.
+// A block per token and 1024 columns, eight columns a thread.  Slots whose expert id is outside 0 .. E-1 are not routed.
 template <class T>
 __global__ void __launch_bounds__(128)
 combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ factor, const int32_t* __restrict__ idx,
@@ -87,28 +87,35 @@ combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ fact
     if (threadIdx.x < k) {
         const size_t j = t * k + threadIdx.x;
         const bool routed = (unsigned)idx[j] < (unsigned)E;
-        const int p = routed ? pos[j] : -1;
+        const int p = routed ? pos[j] : 0;
         s_pos[threadIdx.x] = p;
         s_w[threadIdx.x] = routed ? w[j] * factor[p] : 0.f;
     }
+    const int c = blockIdx.y * 128 + threadIdx.x;
+    const bool mine = c < H >> 3;
+    float acc[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+    if (add && mine) {
+        const uint4 raw = __ldg(reinterpret_cast<const uint4*>(add + t * ld_add + c * 8));
+        const T* v = reinterpret_cast<const T*>(&raw);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[i] = to_f(v[i]);
+    }
     __syncthreads();
-    const int chunks = H >> 3;
-    for (int c = threadIdx.x; c < chunks; c += 128) {
-        float acc[8];
+    if (!mine) return;
+    for (int s0 = 0; s0 < k; s0 += 8) {
+        uint4 raw[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = 0.f;
-        if (add) {
-            const uint4 raw = __ldg(reinterpret_cast<const uint4*>(add + t * ld_add + c * 8));
-            const T* v = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc[i] = to_f(v[i]);
+        for (int s = 0; s < 8; ++s) {            // eight rows on their way at once; unrouted slots bring zeros
+            raw[s] = make_uint4(0u, 0u, 0u, 0u);
+            if (s0 + s < k && s_w[s0 + s] != 0.f) raw[s] = __ldg(reinterpret_cast<const uint4*>(y + (size_t)s_pos[s0 + s] * H + c * 8));
         }
-#pragma unroll 4
-        for (int s = 0; s < k; ++s) {
-            if (s_pos[s] < 0) continue;
-            const uint4 raw = __ldg(reinterpret_cast<const uint4*>(y + (size_t)s_pos[s] * H + c * 8));
-            const __half2* v = reinterpret_cast<const __half2*>(&raw);
-            const float f = s_w[s];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) {
+            if (s0 + s >= k) break;
+            const __half2* v = reinterpret_cast<const __half2*>(&raw[s]);
+            const float f = s_w[s0 + s];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const float2 q = __half22float2(v[i]);
@@ -116,12 +123,72 @@ combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ fact
                 acc[2 * i + 1] = fmaf(f, q.y, acc[2 * i + 1]);
             }
         }
-        uint4 o;
-        T* v = reinterpret_cast<T*>(&o);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = from_f<T>(acc[i]);
-        *reinterpret_cast<uint4*>(out + t * ld_out + c * 8) = o;
     }
+    uint4 o;
+    T* v = reinterpret_cast<T*>(&o);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = from_f<T>(acc[i]);
+    *reinterpret_cast<uint4*>(out + t * ld_out + c * 8) = o;
+}
+
+// The schedule in one block, for batches of up to 16 thousand routes: the layer's own schedule keeps an expert's rows in route
+// order, which takes several passes (three launches); here a row's place inside its expert's segment is whatever an atomic
+// counter gives, because no result depends on it: every row is computed by itself, and the combine reads rows by `pos`.
+constexpr long long GROUPED_ROWS = 112;
+constexpr int ONE_BLOCK = 1024, ROUTES_PER_THREAD = 16;
+__global__ void __launch_bounds__(ONE_BLOCK)
+schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int32_t* __restrict__ counts,
+                    int32_t* __restrict__ pad_offsets, int32_t* __restrict__ tile_expert, int32_t* __restrict__ pos,
+                    int4* __restrict__ tiles, WsHeader* __restrict__ hdr) {
+    __shared__ int32_t s_cnt[MAX_E], s_row0[MAX_E], s_pads[MAX_E / 32], s_tiles[MAX_E / 32];
+    pdl_enter();
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid < MAX_E) s_cnt[tid] = 0;
+    __syncthreads();
+    int e[ROUTES_PER_THREAD], rank[ROUTES_PER_THREAD];
+#pragma unroll
+    for (int i = 0; i < ROUTES_PER_THREAD; ++i) {
+        const int j = tid + i * ONE_BLOCK;
+        e[i] = j < n ? __ldg(idx + j) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < ROUTES_PER_THREAD; ++i) {
+        rank[i] = 0;
+        if ((unsigned)e[i] < (unsigned)E) rank[i] = atomicAdd(&s_cnt[e[i]], 1);
+    }
+    __syncthreads();
+    int c = 0, pads = 0, mine = 0, pads_to = 0, tiles_to = 0;       // of expert tid; the sums run up to and including it
+    if (tid < MAX_E) {
+        c = s_cnt[tid];
+        pads_to = pads = (c + TILE_M - 1) / TILE_M;
+        tiles_to = mine = (c + 2 * TILE_M - 1) / (2 * TILE_M);
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const int p = __shfl_up_sync(0xffffffffu, pads_to, off), t = __shfl_up_sync(0xffffffffu, tiles_to, off);
+            if (lane >= off) { pads_to += p; tiles_to += t; }
+        }
+        if (lane == 31) { s_pads[warp] = pads_to; s_tiles[warp] = tiles_to; }
+    }
+    __syncthreads();
+    if (tid < MAX_E) {
+        for (int q = 0; q < warp; ++q) { pads_to += s_pads[q]; tiles_to += s_tiles[q]; }
+        const int pad0 = pads_to - pads, tile0 = tiles_to - mine;
+        s_row0[tid] = pad0 * TILE_M;
+        if (tid < E) {
+            counts[tid] = c;
+            pad_offsets[tid] = pad0 * TILE_M;
+            for (int q = 0; q < pads; ++q) tile_expert[pad0 + q] = tid;
+            for (int q = 0; q < mine; ++q) tiles[tile0 + q] = make_int4((pad0 + 2 * q) * TILE_M, c - 2 * q * TILE_M, tid, 0);
+        }
+        if (tid == MAX_E - 1) {
+            hdr->n_mtiles = pads_to;
+            hdr->n_mtiles2 = tiles_to;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < ROUTES_PER_THREAD; ++i)
+        if ((unsigned)e[i] < (unsigned)E) pos[tid + i * ONE_BLOCK] = s_row0[e[i]] + rank[i];
 }
 
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -178,7 +245,7 @@ static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) 
 
 template <class T>
 static cudaError_t launch_combine_half(const mok_i8_experts_args* a, const ExpertsLayout& X, char* ws, cudaStream_t s) {
-    return launch_pdl(combine_half_kernel<T>, dim3((unsigned)a->T), dim3(128), 0, s, reinterpret_cast<const __half*>(ws + X.y),
+    return launch_pdl(combine_half_kernel<T>, dim3((unsigned)a->T, (unsigned)((a->H + 1023) / 1024)), dim3(128), 0, s, reinterpret_cast<const __half*>(ws + X.y),
                       reinterpret_cast<const float*>(ws + X.factor), a->topk_idx, a->topk_w,
                       reinterpret_cast<const int32_t*>(ws + X.L.pos), reinterpret_cast<const T*>(a->add),
                       (long long)a->add_stride, a->H, a->E, a->k, reinterpret_cast<T*>(a->out), (long long)a->out_stride);
@@ -302,18 +369,31 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     i8::ProductArgs g = {};
     cudaError_t e = i8::status_header(&g.header);
     if (e != cudaSuccess) return cuda_fail(e);
-    e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
-    if (e != cudaSuccess) return cuda_fail(e);
-    auto table = [&](size_t at) { return reinterpret_cast<const int32_t*>(ws + at); };
+    auto table = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
     int4* tiles = reinterpret_cast<int4*>(ws + X.tiles);
-    const i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k, tiles, &hdr->n_mtiles2, table(X.L.tile_expert2),
-                                  table(X.L.mt_start2), table(X.L.pad_offsets), table(X.L.counts)};
+    // Few rows per expert: the weights, streamed once, are the time; from some hundred on it is the bytes that the tiles pull
+    // into the SMs, of which the pair tiles pull fewer per product.
+    const bool grouped = X.L.R <= i8::GROUPED_ROWS * (long long)a->E;
+    i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k};
+    if (X.L.R <= i8::ONE_BLOCK * i8::ROUTES_PER_THREAD) {
+        e = launch_pdl(i8::schedule_one_kernel, dim3(1), dim3(i8::ONE_BLOCK), 0, s, a->topk_idx, X.L.R, a->E, table(X.L.counts),
+                       table(X.L.pad_offsets), table(X.L.tile_expert), table(X.L.pos), tiles, hdr);
+    } else {
+        e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
+        routes.tiles = tiles;
+        routes.n_mtiles = &hdr->n_mtiles2;
+        routes.tile_expert = table(X.L.tile_expert2);
+        routes.mt_start = table(X.L.mt_start2);
+        routes.pad_offsets = table(X.L.pad_offsets);
+        routes.counts = table(X.L.counts);
+    }
+    g.n_mtiles = &hdr->n_mtiles2;
+    if (e != cudaSuccess) return cuda_fail(e);
     e = i8::launch_quantize(a->x, a->type, a->T, a->H, a->x_stride, reinterpret_cast<int8_t*>(ws + X.xq), X.pitch_h,
                             reinterpret_cast<float*>(ws + X.xs), s, &routes);
     if (e != cudaSuccess) return cuda_fail(e);
     g.E = a->E;
     g.tiles = tiles;
-    g.n_mtiles = &hdr->n_mtiles2;
     g.max_mt = (int32_t)X.max_tiles;
     g.A = reinterpret_cast<const int8_t*>(ws + X.xq);
     g.lda = X.pitch_h;
@@ -325,7 +405,7 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     g.K = a->H; g.N = a->I;
     g.C = ws + X.h;
     g.ldc = a->I;
-    e = i8::launch_product(g, i8::EPI_GATED, s);
+    e = grouped ? i8::launch_grouped(g, i8::EPI_GATED, X.L.R, s) : i8::launch_product(g, i8::EPI_GATED, s);
     if (e != cudaSuccess) return cuda_fail(e);
     float unit = 1.f;                                // |sum| * unit <= 65504
     while (127.0 * 127.0 * a->I * unit > 65504.0) unit *= 0.5f;
@@ -357,7 +437,7 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     g.K = a->I; g.N = a->H;
     g.C = ws + X.y;
     g.ldc = a->H;
-    e = i8::launch_product(g, i8::EPI_HALF, s);
+    e = grouped ? i8::launch_grouped(g, i8::EPI_HALF, X.L.R, s) : i8::launch_product(g, i8::EPI_HALF, s);
     if (e != cudaSuccess) return cuda_fail(e);
     e = a->type == MOK_TYPE_BF16 ? i8::launch_combine_half<__nv_bfloat16>(a, X, ws, s) : i8::launch_combine_half<__half>(a, X, ws, s);
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);

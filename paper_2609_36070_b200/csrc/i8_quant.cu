@@ -45,7 +45,7 @@ struct Targets {
 // The 256-row tiles of the experts' segments: {first row, rows of the segment from there on, expert, -}
 __device__ __forceinline__ void write_tiles(const RouteArgs& q) {
     const int n = *q.n_mtiles;
-    for (int i = blockIdx.x * THREADS + threadIdx.x; i < n; i += gridDim.x * THREADS) {
+    for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
         const int e = q.tile_expert[i], m = i - q.mt_start[e];
         q.tiles[i] = make_int4(q.pad_offsets[e] + m * 2 * TILE_M, q.counts[e] - m * 2 * TILE_M, e, 0);
     }
@@ -59,7 +59,7 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
     constexpr int PER = 16 / sizeof(T);
     __shared__ uint32_t s_max[BLOCK / 32];
     pdl_enter();
-    if (ROUTED) write_tiles(routes);
+    if (ROUTED && routes.tiles) write_tiles(routes);
     const int sub = threadIdx.x % TPR, pieces = K / PER;
     constexpr int ROWS = BLOCK / TPR;
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < rows; r0 += (long long)gridDim.x * ROWS) {
@@ -121,7 +121,7 @@ quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ld
                     float* __restrict__ scales, const RouteArgs routes) {
     __shared__ uint32_t s_max[THREADS / 32];
     pdl_enter();
-    if (ROUTED) write_tiles(routes);
+    if (ROUTED && routes.tiles) write_tiles(routes);
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const T* src = x + r * ldx;
         uint32_t m = 0;

@@ -384,7 +384,8 @@ def routes(g, T, E, k):
 
 
 EXPERTS = [(1, 8, 8, 1, 1), (1, 256, 128, 8, 2), (3, 64, 264, 4, 4), (16, 256, 136, 64, 8), (50, 520, 200, 7, 3), (200, 128, 1032, 4, 2),
-           (300, 264, 384, 3, 2), (1000, 256, 256, 2, 1), (2500, 136, 72, 16, 4), (700, 72, 8200, 2, 2)]
+           (300, 264, 384, 3, 2), (1000, 256, 256, 2, 1), (2500, 136, 72, 16, 4), (700, 72, 8200, 2, 2),
+           (4200, 72, 64, 300, 8), (6000, 64, 40, 8, 4), (130, 2048, 768, 128, 8), (129, 384, 512, 1, 1), (112, 384, 72, 1, 1)]
 
 
 @pytest.mark.parametrize("T,H,I,E,k", EXPERTS)
