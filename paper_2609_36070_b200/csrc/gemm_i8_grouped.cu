@@ -4,8 +4,8 @@
 // weights and nothing else: 256-row tiles would pull 256 mostly empty token rows beside every weight tile.
 //
 // Persistent CTAs over the list of (row tile, channel tile):
-//   warp 0       TMA producer: 128 weight rows and the tile's token rows per 128 bytes of K, six stages (four where a tile may
-//                have more than 128 rows)
+//   warp 0       TMA producer: 128 weight rows and the tile's token rows per 128 bytes of K; eight, six, five or four stages for
+//                tiles of at most 64, 128, 192 or 256 rows
 //   warp 1       MMA issuer (tcgen05.mma.kind::i8, M = 128), two accumulators
 //   warps 2..9   epilogue: lane = channel, so that stores are coalesced as they are
 //   EPI_GATED : the M side holds 64 gate rows and the 64 matching up rows; the warps of the up lanes hand their values over
@@ -22,10 +22,10 @@ namespace i8 {
 using namespace tc;
 
 constexpr int G_EPI = 8, G_THREADS = 64 + 32 * G_EPI;
-constexpr int G_MAX_STAGES = 6;
-// ROWS: most rows of a tile, 128 (batches of so many tokens) or 256
+constexpr int G_MAX_STAGES = 8;
+// ROWS: most rows of a tile
 template <int ROWS> struct Grouped {
-    static constexpr int STAGES = ROWS == 128 ? 6 : 4, STAGE = 16384 + ROWS * 128;      // weights, tokens
+    static constexpr int STAGES = ROWS == 64 ? 8 : ROWS == 128 ? 6 : ROWS == 192 ? 5 : 4, STAGE = 16384 + ROWS * 128;      // weights, tokens
     static constexpr int XCHG = STAGES * STAGE;              // up values: 4 warp pairs x 2 buffers x [16 tokens][32 channels]
     static constexpr int CTRL = XCHG + 4 * 2 * 2048;
     static constexpr int SMEM = CTRL + 512;
@@ -43,7 +43,7 @@ struct RowTile { int row0, n, e, valid; };
 __device__ __forceinline__ RowTile row_tile(const ProductArgs& a, int L, int n_nt) {
     const int q = L / n_nt;
     const int4 d = __ldg(a.tiles + q);
-    return RowTile{d.x, L - q * n_nt, d.z, min(d.y, 2 * TILE_M)};
+    return RowTile{d.x, L - q * n_nt, d.z, min(d.y, a.tile_rows)};
 }
 __device__ __forceinline__ int columns(int valid) { return (valid + 15) & ~15; }      // N of the MMA
 
@@ -51,9 +51,10 @@ template <int EPI, int ROWS>
 __global__ void __launch_bounds__(G_THREADS, 1)
 product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_constant__ CUtensorMap tmap16,
                        const __grid_constant__ CUtensorMap tmap64, const __grid_constant__ CUtensorMap tmap128,
-                       const __grid_constant__ CUtensorMap tmap256, const __grid_constant__ ProductArgs a, const int n_nt, const int k_blocks) {
+                       const __grid_constant__ CUtensorMap tmapRows, const __grid_constant__ ProductArgs a, const int n_nt, const int k_blocks) {
     constexpr bool GATED = EPI == EPI_GATED;
     using G = Grouped<ROWS>;
+    constexpr uint32_t TMEM_COLUMNS = ROWS <= 64 ? 128u : ROWS <= 128 ? 256u : 512u;
     extern __shared__ __align__(1024) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
     GroupedCtrl* ctrl = reinterpret_cast<GroupedCtrl*>(smem + G::CTRL);
@@ -79,7 +80,7 @@ product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_c
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
-                     ::"r"(smem_u32(&ctrl->tmem_base)), "r"(2u * ROWS) : "memory");
+                     ::"r"(smem_u32(&ctrl->tmem_base)), "r"(TMEM_COLUMNS) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -101,8 +102,9 @@ product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_c
                 const RowTile t = next;
                 if (L + (int)gridDim.x < total) next = row_tile(a, L + gridDim.x, n_nt);
                 const int cols = columns(t.valid);
-                const CUtensorMap* map = cols <= 16 ? &tmap16 : cols <= 64 ? &tmap64 : ROWS == 128 || cols <= 128 ? &tmap128 : &tmap256;
-                const uint32_t bytes = 16384u + (cols <= 16 ? 16u : cols <= 64 ? 64u : ROWS == 128 || cols <= 128 ? 128u : 256u) * 128u;
+                const CUtensorMap* map = cols <= 16 ? &tmap16 : ROWS == 64 || cols <= 64 ? &tmap64 : ROWS == 128 || cols <= 128 ? &tmap128 : &tmapRows;
+                const uint32_t box = cols <= 16 ? 16u : ROWS == 64 || cols <= 64 ? 64u : ROWS == 128 || cols <= 128 ? 128u : (uint32_t)ROWS;
+                const uint32_t bytes = 16384u + box * 128u;
                 const int wrow = GATED ? t.e * 2 * a.N + t.n * 64 : t.e * a.N + t.n * 128;
                 bool ok = true;
                 for (int kb = 0; kb < k_blocks; ++kb) {
@@ -237,7 +239,7 @@ product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_c
     __syncthreads();
     if (warp == 1) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2u * ROWS) : "memory");
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(TMEM_COLUMNS) : "memory");
     }
 }
 
@@ -258,7 +260,7 @@ static cudaError_t launch_grouped_epi(const CUtensorMap& mW, const CUtensorMap (
                       mX[1], mX[2], mX[3], a, n_nt, k_blocks);
 }
 
-cudaError_t launch_grouped(const ProductArgs& a, int epi, int most_rows, cudaStream_t s) {
+cudaError_t launch_grouped(const ProductArgs& a, int epi, cudaStream_t s) {
     const bool is_gated = epi == EPI_GATED;
     CUtensorMap mW, mX[4];
     auto map = [&](CUtensorMap* m, const void* p, long long rows, long long pitch, uint32_t box) {
@@ -267,14 +269,21 @@ cudaError_t launch_grouped(const ProductArgs& a, int epi, int most_rows, cudaStr
     };
     if (!map(&mW, a.B, (long long)a.E * (is_gated ? 2 : 1) * a.N, a.ldb, 64) || !map(&mX[0], a.A, a.a_rows, a.lda, 16) ||
         !map(&mX[1], a.A, a.a_rows, a.lda, 64) || !map(&mX[2], a.A, a.a_rows, a.lda, 128) ||
-        !map(&mX[3], a.A, a.a_rows, a.lda, 256))
+        !map(&mX[3], a.A, a.a_rows, a.lda, a.tile_rows == 192 ? 192 : 256))
         return cudaErrorInvalidValue;
     const int n_nt = is_gated ? (a.N + 63) / 64 : (a.N + 127) / 128, k_blocks = (a.K + 127) / 128;
     const long long tiles = (long long)a.max_mt * n_nt;
     if (tiles <= 0 || tiles > 0x7fffffffll) return cudaErrorInvalidValue;
-    if (most_rows <= 128)
+    if (a.tile_rows == 64)
+        return is_gated ? launch_grouped_epi<EPI_GATED, 64>(mW, mX, a, n_nt, k_blocks, tiles, s)
+                        : launch_grouped_epi<EPI_HALF, 64>(mW, mX, a, n_nt, k_blocks, tiles, s);
+    if (a.tile_rows == 128)
         return is_gated ? launch_grouped_epi<EPI_GATED, 128>(mW, mX, a, n_nt, k_blocks, tiles, s)
                         : launch_grouped_epi<EPI_HALF, 128>(mW, mX, a, n_nt, k_blocks, tiles, s);
+    if (a.tile_rows == 192)
+        return is_gated ? launch_grouped_epi<EPI_GATED, 192>(mW, mX, a, n_nt, k_blocks, tiles, s)
+                        : launch_grouped_epi<EPI_HALF, 192>(mW, mX, a, n_nt, k_blocks, tiles, s);
+    if (a.tile_rows != 256) return cudaErrorInvalidValue;
     return is_gated ? launch_grouped_epi<EPI_GATED, 256>(mW, mX, a, n_nt, k_blocks, tiles, s)
                     : launch_grouped_epi<EPI_HALF, 256>(mW, mX, a, n_nt, k_blocks, tiles, s);
 }

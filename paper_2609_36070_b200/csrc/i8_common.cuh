@@ -80,7 +80,8 @@ struct ProductArgs {
     float y_unit;                // EPI_HALF: power of two that brings |sum| <= 127 * 127 * K below 65504
     const float* bias;           // [N] or NULL (plain)
     int32_t dense_rows;          // > 0: dense
-    const int4* tiles;           // grouped: {first row, rows of the segment from there on, expert, -} of every 256-row tile
+    const int4* tiles;           // grouped: {first row, rows of the segment from there on, expert, -} of every row tile
+    int32_t tile_rows;           // their rows: 256 (launch_product); 64, 128, 192 or 256 (launch_grouped)
     const int32_t* n_mtiles;     // how many
     int32_t max_mt;              // at most
     int32_t c_mapped;            // set by the launcher: C is stored through a tensor map
@@ -93,14 +94,15 @@ enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
 struct RouteArgs {
     const int32_t *idx, *pos;
     int32_t E, k;
+    int32_t tile_rows;           // 128 or 256
     int4* tiles;
     const int32_t *n_mtiles, *tile_expert, *mt_start, *pad_offsets, *counts;
 };
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s);
-// few rows per expert (EPI_GATED, EPI_HALF); most_rows: that any expert can have (all routes, for ids may repeat)
-cudaError_t launch_grouped(const ProductArgs& a, int epi, int most_rows, cudaStream_t s);
+// few rows per expert (EPI_GATED, EPI_HALF)
+cudaError_t launch_grouped(const ProductArgs& a, int epi, cudaStream_t s);
 // few tokens (EPI_PLAIN, dense): whether the kernel for them takes the product; quantises: from the activations (of x_type, -1:
 // there are only codes)
 bool narrow_product(int M, int K, int N, int x_type, unsigned long long x_align, bool* quantises);

@@ -14,6 +14,8 @@ namespace mok {
 namespace i8 {
 
 constexpr int THREADS = 256;
+constexpr int ONE_BLOCK = 1024, ROUTES_PER_THREAD = 16;      // of the schedule in one block
+constexpr long long GROUPED_ROWS = 112;                      // rows per expert up to which launch_grouped is the faster one
 
 // Rows of h (fp32, padded row space) -> codes.  factor = scale * b_max / y_unit: what the combine multiplies a row by.
 // Pad rows are left alone.
@@ -134,10 +136,8 @@ combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ fact
 // The schedule in one block, for batches of up to 16 thousand routes: the layer's own schedule keeps an expert's rows in route
 // order, which takes several passes (three launches); here a row's place inside its expert's segment is whatever an atomic
 // counter gives, because no result depends on it: every row is computed by itself, and the combine reads rows by `pos`.
-constexpr long long GROUPED_ROWS = 112;
-constexpr int ONE_BLOCK = 1024, ROUTES_PER_THREAD = 16;
 __global__ void __launch_bounds__(ONE_BLOCK)
-schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int32_t* __restrict__ counts,
+schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows, int32_t* __restrict__ counts,
                     int32_t* __restrict__ pad_offsets, int32_t* __restrict__ tile_expert, int32_t* __restrict__ pos,
                     int4* __restrict__ tiles, WsHeader* __restrict__ hdr) {
     __shared__ int32_t s_cnt[MAX_E], s_row0[MAX_E], s_pads[MAX_E / 32], s_tiles[MAX_E / 32];
@@ -161,7 +161,7 @@ schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int32_t* __re
     if (tid < MAX_E) {
         c = s_cnt[tid];
         pads_to = pads = (c + TILE_M - 1) / TILE_M;
-        tiles_to = mine = (c + 2 * TILE_M - 1) / (2 * TILE_M);
+        tiles_to = mine = (c + tile_rows - 1) / tile_rows;
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) {
             const int p = __shfl_up_sync(0xffffffffu, pads_to, off), t = __shfl_up_sync(0xffffffffu, tiles_to, off);
@@ -178,11 +178,11 @@ schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int32_t* __re
             counts[tid] = c;
             pad_offsets[tid] = pad0 * TILE_M;
             for (int q = 0; q < pads; ++q) tile_expert[pad0 + q] = tid;
-            for (int q = 0; q < mine; ++q) tiles[tile0 + q] = make_int4((pad0 + 2 * q) * TILE_M, c - 2 * q * TILE_M, tid, 0);
+            for (int q = 0; q < mine; ++q) tiles[tile0 + q] = make_int4(pad0 * TILE_M + q * tile_rows, c - q * tile_rows, tid, 0);
         }
         if (tid == MAX_E - 1) {
             hdr->n_mtiles = pads_to;
-            hdr->n_mtiles2 = tiles_to;
+            hdr->n_ftiles = tiles_to;
         }
     }
     __syncthreads();
@@ -198,7 +198,9 @@ struct ExpertsLayout {
     WsLayout L;
     size_t tiles, xq, xs, h, hq, factor, y, total;
     int pitch_h, pitch_i;
-    long long max_tiles;         // upper bound of 256-row tiles
+    bool grouped;                // the products for few rows per expert
+    int tile_rows;               // of the products' row tiles
+    long long max_tiles;         // upper bound of their number
 };
 
 static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) {
@@ -213,7 +215,13 @@ static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) 
     L.max_mt = L.Rpad / TILE_M;
     L.n_blk = (int32_t)((R + SCHED_CHUNK - 1) / SCHED_CHUNK);
     if (L.n_blk < 1) L.n_blk = 1;
-    X->max_tiles = R / (2 * TILE_M) + nonempty;
+    // Few rows per expert: the weights, streamed once, are the time; from some hundred on it is the bytes that the tiles pull
+    // into the SMs, of which the pair tiles pull fewer per product.  Small tiles leave room for more stages, a tile too small
+    // streams its expert's weights twice.
+    X->grouped = R <= GROUPED_ROWS * (long long)E;
+    const bool any = R <= ONE_BLOCK * ROUTES_PER_THREAD;                 // (the layer's schedule knows tiles of 128 and 256 rows)
+    X->tile_rows = !X->grouped ? 2 * TILE_M : any && R <= 32ll * E ? 64 : R <= 64ll * E ? TILE_M : any ? 192 : 2 * TILE_M;
+    X->max_tiles = R / X->tile_rows + nonempty;
     X->pitch_h = pitch_of(H);
     X->pitch_i = pitch_of(I);
     size_t off = 0;
@@ -371,29 +379,29 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     if (e != cudaSuccess) return cuda_fail(e);
     auto table = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
     int4* tiles = reinterpret_cast<int4*>(ws + X.tiles);
-    // Few rows per expert: the weights, streamed once, are the time; from some hundred on it is the bytes that the tiles pull
-    // into the SMs, of which the pair tiles pull fewer per product.
-    const bool grouped = X.L.R <= i8::GROUPED_ROWS * (long long)a->E;
-    i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k};
+    i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k, X.tile_rows};
     if (X.L.R <= i8::ONE_BLOCK * i8::ROUTES_PER_THREAD) {
-        e = launch_pdl(i8::schedule_one_kernel, dim3(1), dim3(i8::ONE_BLOCK), 0, s, a->topk_idx, X.L.R, a->E, table(X.L.counts),
-                       table(X.L.pad_offsets), table(X.L.tile_expert), table(X.L.pos), tiles, hdr);
+        e = launch_pdl(i8::schedule_one_kernel, dim3(1), dim3(i8::ONE_BLOCK), 0, s, a->topk_idx, X.L.R, a->E, X.tile_rows,
+                       table(X.L.counts), table(X.L.pad_offsets), table(X.L.tile_expert), table(X.L.pos), tiles, hdr);
+        g.n_mtiles = &hdr->n_ftiles;
     } else {
         e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
+        const bool half = X.tile_rows == TILE_M;
+        g.n_mtiles = half ? &hdr->n_mtiles : &hdr->n_mtiles2;
         routes.tiles = tiles;
-        routes.n_mtiles = &hdr->n_mtiles2;
-        routes.tile_expert = table(X.L.tile_expert2);
-        routes.mt_start = table(X.L.mt_start2);
+        routes.n_mtiles = g.n_mtiles;
+        routes.tile_expert = table(half ? X.L.tile_expert : X.L.tile_expert2);
+        routes.mt_start = table(half ? X.L.mt_start : X.L.mt_start2);
         routes.pad_offsets = table(X.L.pad_offsets);
         routes.counts = table(X.L.counts);
     }
-    g.n_mtiles = &hdr->n_mtiles2;
     if (e != cudaSuccess) return cuda_fail(e);
     e = i8::launch_quantize(a->x, a->type, a->T, a->H, a->x_stride, reinterpret_cast<int8_t*>(ws + X.xq), X.pitch_h,
                             reinterpret_cast<float*>(ws + X.xs), s, &routes);
     if (e != cudaSuccess) return cuda_fail(e);
     g.E = a->E;
     g.tiles = tiles;
+    g.tile_rows = X.tile_rows;
     g.max_mt = (int32_t)X.max_tiles;
     g.A = reinterpret_cast<const int8_t*>(ws + X.xq);
     g.lda = X.pitch_h;
@@ -405,7 +413,7 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     g.K = a->H; g.N = a->I;
     g.C = ws + X.h;
     g.ldc = a->I;
-    e = grouped ? i8::launch_grouped(g, i8::EPI_GATED, X.L.R, s) : i8::launch_product(g, i8::EPI_GATED, s);
+    e = X.grouped ? i8::launch_grouped(g, i8::EPI_GATED, s) : i8::launch_product(g, i8::EPI_GATED, s);
     if (e != cudaSuccess) return cuda_fail(e);
     float unit = 1.f;                                // |sum| * unit <= 65504
     while (127.0 * 127.0 * a->I * unit > 65504.0) unit *= 0.5f;
@@ -437,7 +445,7 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     g.K = a->I; g.N = a->H;
     g.C = ws + X.y;
     g.ldc = a->H;
-    e = grouped ? i8::launch_grouped(g, i8::EPI_HALF, X.L.R, s) : i8::launch_product(g, i8::EPI_HALF, s);
+    e = X.grouped ? i8::launch_grouped(g, i8::EPI_HALF, s) : i8::launch_product(g, i8::EPI_HALF, s);
     if (e != cudaSuccess) return cuda_fail(e);
     e = a->type == MOK_TYPE_BF16 ? i8::launch_combine_half<__nv_bfloat16>(a, X, ws, s) : i8::launch_combine_half<__half>(a, X, ws, s);
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);

@@ -42,12 +42,12 @@ struct Targets {
     }
 };
 
-// The 256-row tiles of the experts' segments: {first row, rows of the segment from there on, expert, -}
+// The row tiles of the experts' segments: {first row, rows of the segment from there on, expert, -}
 __device__ __forceinline__ void write_tiles(const RouteArgs& q) {
     const int n = *q.n_mtiles;
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
         const int e = q.tile_expert[i], m = i - q.mt_start[e];
-        q.tiles[i] = make_int4(q.pad_offsets[e] + m * 2 * TILE_M, q.counts[e] - m * 2 * TILE_M, e, 0);
+        q.tiles[i] = make_int4(q.pad_offsets[e] + m * q.tile_rows, q.counts[e] - m * q.tile_rows, e, 0);
     }
 }
 
