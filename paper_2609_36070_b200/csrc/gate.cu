@@ -430,54 +430,67 @@ struct BwdParams {
 //   as they are   sigmoid: dl_i = g_i s_i (1 - s_i)
 //                 softmax: dl_e = s_e (g_e - sum_j g_j s_j)                         for every expert e, g_e = 0 if not chosen
 // Only the last one is non-zero outside the chosen experts (and reads all logits).  1 - s is sigmoid(-l), without the
-// cancellation.  One warp per token; the row is put together in shared memory and written once, coalesced.  Chosen ids
-// outside 0 .. E-1 (routes that were dropped) have no part in it.
+// cancellation.  Four tokens per warp, eight lanes each, as in the forward kernel; a token's row is put together in shared
+// memory and written once, in 16-byte pieces.  Chosen ids outside 0 .. E-1 (routes that were dropped) have no part in it.
 template <class L>
 __global__ void __launch_bounds__(32 * WARPS)
 gate_backward_kernel(const BwdParams p) {
-    extern __shared__ __align__(16) float s_row[];   // [WARPS][E rounded up to 8], zero between tokens
-    constexpr int PER = 16 / sizeof(L);
+    extern __shared__ __align__(16) float s_row[];   // [WARPS][4][E rounded up to 8], zero between tokens
+    constexpr int PER = 16 / sizeof(L), SLOTS = MAX_K / 8;
     pdl_enter();
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int E = p.E, k = p.k;
-    float* mine = s_row + warp * ((E + 7) & ~7);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 7, own = lane >> 3;
+    const int E = p.E, k = p.k, pitch = (E + 7) & ~7;
+    float* mine = s_row + (warp * 4 + own) * pitch;
     const bool vec = E % PER == 0 && p.d_stride % PER == 0 && (reinterpret_cast<uintptr_t>(p.dlogits) & 15u) == 0;
-    for (int i = lane; i < E; i += 32) mine[i] = 0.f;
+    for (int i = sub; i < E; i += 8) mine[i] = 0.f;
     __syncwarp();
-    for (int t = blockIdx.x * WARPS + warp; t < p.T; t += gridDim.x * WARPS) {
-        const L* row = reinterpret_cast<const L*>(p.logits) + (long long)t * p.stride;
-        L* out = reinterpret_cast<L*>(p.dlogits) + (long long)t * p.d_stride;
-        int e = -1;
-        float g = 0.f, l = 0.f;
-        if (lane < k) {
-            e = p.idx[(size_t)t * k + lane];
-            g = p.dw[(size_t)t * k + lane] * p.scale;
-            if ((unsigned)e >= (unsigned)E) e = -1;
-            if (e >= 0) l = load_f(row + e);
-            else g = 0.f;
+    for (long long t0 = ((long long)blockIdx.x * WARPS + warp) * 4; t0 < p.T; t0 += (long long)gridDim.x * WARPS * 4) {
+        const bool live = t0 + own < p.T;
+        const long long t = live ? t0 + own : p.T - 1;
+        const L* row = reinterpret_cast<const L*>(p.logits) + t * p.stride;
+        L* out = reinterpret_cast<L*>(p.dlogits) + t * p.d_stride;
+        int e[SLOTS];                                // slots sub, sub + 8, ...
+        float g[SLOTS], l[SLOTS];
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q) {
+            e[q] = -1;
+            g[q] = l[q] = 0.f;
+            if (8 * q + sub < k) {
+                e[q] = p.idx[t * k + 8 * q + sub];
+                g[q] = p.dw[t * k + 8 * q + sub] * p.scale;
+                if ((unsigned)e[q] >= (unsigned)E) e[q] = -1;
+                if (e[q] >= 0) l[q] = load_f(row + e[q]);
+                else g[q] = 0.f;
+            }
         }
         if (!p.softmax || p.renormalise) {
-            float d = 0.f;
+            float s[SLOTS], total = 0.f, dot = 0.f, m = -INFINITY;
             if (p.softmax) {
-                const float m = warp_max(e >= 0 ? l : -INFINITY);
-                const float q = e >= 0 ? exp_below(l, m) : 0.f;
-                const float S = warp_sum(q);
-                const float pi = S > 0.f ? q / S : 0.f;
-                d = pi * (g - warp_sum(g * pi));
-            } else {
-                const float s = e >= 0 ? sigmoid(l) : 0.f;
-                const float slope = s * sigmoid(-l);
-                if (p.renormalise) {
-                    const float S = warp_sum(s), inv = S > 0.f ? 1.f / S : 0.f;
-                    d = slope * inv * (g - warp_sum(g * s) * inv);
-                } else {
-                    d = g * slope;
-                }
+#pragma unroll
+                for (int q = 0; q < SLOTS; ++q) m = fmaxf(m, e[q] >= 0 ? l[q] : -INFINITY);
+                m = max8(m);
             }
-            if (e >= 0) mine[e] = d;
+#pragma unroll
+            for (int q = 0; q < SLOTS; ++q) {
+                s[q] = 0.f;
+                if (e[q] >= 0) s[q] = p.softmax ? exp_below(l[q], m) : sigmoid(l[q]);
+                total += s[q];
+                dot += g[q] * s[q];
+            }
+            total = sum8(total);
+            dot = sum8(dot);
+            const float inv = total > 0.f ? 1.f / total : 0.f;
+            const float mean = dot * inv;
+#pragma unroll
+            for (int q = 0; q < SLOTS; ++q) {
+                if (e[q] < 0) continue;
+                mine[e[q]] = p.softmax ? s[q] * inv * (g[q] - mean)
+                             : p.renormalise ? s[q] * sigmoid(-l[q]) * inv * (g[q] - mean) : g[q] * s[q] * sigmoid(-l[q]);
+            }
             __syncwarp();
-            if (vec) {
-                for (int i = lane; i < E / PER; i += 32) {
+            if (!live) {
+            } else if (vec) {
+                for (int i = sub; i < E / PER; i += 8) {
                     uint4 o;
                     L* v = reinterpret_cast<L*>(&o);
 #pragma unroll
@@ -491,25 +504,30 @@ gate_backward_kernel(const BwdParams p) {
                     *reinterpret_cast<uint4*>(out + i * PER) = o;
                 }
             } else {
-                for (int i = lane; i < E; i += 32) store_f(out + i, mine[i]);
+                for (int i = sub; i < E; i += 8) store_f(out + i, mine[i]);
             }
         } else {
-            float m = -INFINITY, sum = 0.f;
-            for (int i = lane; i < E; i += 32) m = fmaxf(m, load_f(row + i));
-            m = warp_max(m);
-            for (int i = lane; i < E; i += 32) sum += exp_below(load_f(row + i), m);
-            sum = warp_sum(sum);
+            float m = -INFINITY, sum = 0.f, dot = 0.f;
+            for (int i = sub; i < E; i += 8) m = fmaxf(m, load_f(row + i));
+            m = max8(m);
+            for (int i = sub; i < E; i += 8) sum += exp_below(load_f(row + i), m);
+            sum = sum8(sum);
             const float inv = sum > 0.f ? 1.f / sum : 0.f;
-            const float dot = warp_sum(e >= 0 ? g * exp_below(l, m) * inv : 0.f);
-            if (e >= 0) mine[e] = g;
-            __syncwarp();
-            for (int i = lane; i < E; i += 32) {
-                const float s = exp_below(load_f(row + i), m) * inv;
-                store_f(out + i, s * (mine[i] - dot));
+#pragma unroll
+            for (int q = 0; q < SLOTS; ++q) {
+                if (e[q] < 0) continue;
+                dot += g[q] * exp_below(l[q], m) * inv;
+                mine[e[q]] = g[q];
             }
+            dot = sum8(dot);
+            __syncwarp();
+            if (live)
+                for (int i = sub; i < E; i += 8) store_f(out + i, exp_below(load_f(row + i), m) * inv * (mine[i] - dot));
         }
         __syncwarp();
-        if (e >= 0) mine[e] = 0.f;
+#pragma unroll
+        for (int q = 0; q < SLOTS; ++q)
+            if (e[q] >= 0) mine[e[q]] = 0.f;
         __syncwarp();
     }
 }
@@ -549,9 +567,10 @@ static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
 
 template <class L>
 static cudaError_t launch_backward(const BwdParams& p, cudaStream_t s) {
-    long long blocks = ((long long)p.T + WARPS - 1) / WARPS;
-    if (blocks > 148 * 12) blocks = 148 * 12;
-    return launch_pdl(gate_backward_kernel<L>, dim3((unsigned)blocks), dim3(32 * WARPS), sizeof(float) * WARPS * ((p.E + 7) & ~7), s, p);
+    const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * 8;
+    const long long rounds = (units + wave - 1) / wave, blocks = (units + rounds - 1) / rounds;
+    return launch_pdl(gate_backward_kernel<L>, dim3((unsigned)blocks), dim3(32 * WARPS), sizeof(float) * WARPS * 4 * ((p.E + 7) & ~7),
+                      s, p);
 }
 
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
