@@ -1,4 +1,5 @@
-"""Build libmok.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a.
+"""Build libmok.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _binding.so (its C++ entry points for torch
+tensors) with g++.
 
 `python -m paper_2609_36070_b200.build [--force] [--verbose]`.  nvcc cross-compiles without a GPU.
 """
@@ -6,11 +7,14 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmok.so")
+BINDING = os.path.join(PKG, "_binding.so")
+BINDING_SRC = os.path.join(CSRC, "binding.cpp")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -29,9 +33,32 @@ def _stale():
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_binding(force: bool = False) -> str:
+    """The Python extension module, linked against libmok.so beside it and against torch's libraries (loaded by torch)."""
+    deps = [BINDING_SRC, os.path.join(ROOT, "include", "mok.h")]
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(d) <= os.path.getmtime(BINDING) for d in deps):
+        return BINDING
+    import torch
+    site = os.path.join(os.path.dirname(torch.__file__), "")
+    cuda = os.path.dirname(os.path.dirname(NVCC))
+    include = [os.path.join(ROOT, "include"), site + "include", site + "include/torch/csrc/api/include",
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    libs = ["c10", "c10_cuda", "torch", "torch_cpu", "torch_cuda", "torch_python"]
+    subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    *(f"-I{d}" for d in include), BINDING_SRC, "-o", BINDING + ".tmp", f"-L{site}lib", *(f"-l{n}" for n in libs),
+                    f"-L{PKG}", "-l:libmok.so", "-Wl,-rpath,$ORIGIN"], check=True)
+    os.replace(BINDING + ".tmp", BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False) -> str:
-    if not force and not _stale():
-        return LIB
+    if force or _stale():
+        build_library(verbose)
+    build_binding(force)
+    return LIB
+
+
+def build_library(verbose: bool = False) -> str:
     objdir = os.path.join(PKG, "build")
     os.makedirs(objdir, exist_ok=True)
     objs = []

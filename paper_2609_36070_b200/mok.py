@@ -5,8 +5,6 @@ device memory and streams.  Importing this module fails loudly if the library ha
 (`python -m paper_2609_36070_b200.build`); there is no CPU or PyTorch fallback.
 """
 import ctypes
-import functools
-import inspect
 import os
 
 import torch
@@ -15,6 +13,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmok.so"
 if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2609_36070_b200.build`")
 _lib = ctypes.CDLL(_LIB_PATH)
+from . import _binding  # noqa: E402  (needs torch and the library; fails as loudly)
 
 MOK_OK = 0
 MOK_ERR_NULL, MOK_ERR_SHAPE, MOK_ERR_ALIGN, MOK_ERR_WORKSPACE = -1, -2, -3, -4
@@ -38,8 +37,6 @@ MOK_MAX_RANKS = 16
 MOK_NOALLOC_MAX_ROUTES = 32768
 MOK_DEBUG_STARVE = 2
 MOK_DEBUG_NO_ARRIVALS = 3
-MOK_TYPE_BF16, MOK_TYPE_F16, MOK_TYPE_F32 = 0, 1, 2
-MOK_SCORE_SOFTMAX, MOK_SCORE_SIGMOID = 0, 1
 STAGES = ["router", "schedule", "gather", "gemm1", "gemm2", "shared_gemm1", "shared_gemm2", "combine"]
 
 
@@ -132,57 +129,8 @@ class mok_bwd_args(ctypes.Structure):
                 ("config", ctypes.POINTER(mok_config)), ("stream", ctypes.c_void_p)]
 
 
-class mok_gate_args(ctypes.Structure):
-    _fields_ = [("logits", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("logits_stride", ctypes.c_int64),
-                ("T", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("logits_type", ctypes.c_int32),
-                ("score", ctypes.c_int32), ("n_groups", ctypes.c_int32), ("topk_groups", ctypes.c_int32),
-                ("group_top", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float),
-                ("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
-
-
-class mok_gate_bwd_args(ctypes.Structure):
-    _fields_ = [("logits", ctypes.c_void_p), ("topk_idx", ctypes.c_void_p), ("dw", ctypes.c_void_p),
-                ("logits_stride", ctypes.c_int64), ("dlogits_stride", ctypes.c_int64),
-                ("T", ctypes.c_int32), ("E", ctypes.c_int32), ("k", ctypes.c_int32), ("logits_type", ctypes.c_int32),
-                ("score", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("scale", ctypes.c_float),
-                ("dlogits", ctypes.c_void_p), ("stream", ctypes.c_void_p)]
-
-
-class mok_i8_linear_args(ctypes.Structure):
-    _fields_ = [("x", ctypes.c_void_p), ("x_codes", ctypes.c_void_p), ("x_scales", ctypes.c_void_p),
-                ("W_codes", ctypes.c_void_p), ("W_scales", ctypes.c_void_p), ("bias", ctypes.c_void_p),
-                ("x_stride", ctypes.c_int64), ("codes_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64),
-                ("out_stride", ctypes.c_int64), ("M", ctypes.c_int32), ("K", ctypes.c_int32), ("N", ctypes.c_int32),
-                ("x_type", ctypes.c_int32), ("out_type", ctypes.c_int32), ("out", ctypes.c_void_p),
-                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
-
-
-class mok_i8_experts_args(ctypes.Structure):
-    _fields_ = [("x", ctypes.c_void_p), ("topk_idx", ctypes.c_void_p), ("topk_w", ctypes.c_void_p),
-                ("gate_up_codes", ctypes.c_void_p), ("gate_up_scales", ctypes.c_void_p),
-                ("down_codes", ctypes.c_void_p), ("down_scales", ctypes.c_void_p), ("down_max", ctypes.c_void_p),
-                ("add", ctypes.c_void_p), ("x_stride", ctypes.c_int64), ("gate_up_stride", ctypes.c_int64),
-                ("down_stride", ctypes.c_int64), ("add_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
-                ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("I", ctypes.c_int32), ("E", ctypes.c_int32),
-                ("k", ctypes.c_int32), ("type", ctypes.c_int32), ("out", ctypes.c_void_p),
-                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)]
-
-
-_lib.mok_gate.restype = ctypes.c_int
-_lib.mok_gate.argtypes = [ctypes.POINTER(mok_gate_args)]
-_lib.mok_gate_backward.restype = ctypes.c_int
-_lib.mok_gate_backward.argtypes = [ctypes.POINTER(mok_gate_bwd_args)]
-_lib.mok_i8_quantize.restype = ctypes.c_int
-_lib.mok_i8_quantize.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong,
-                                 ctypes.c_void_p, ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p]
-_lib.mok_i8_linear_workspace_bytes.restype = ctypes.c_size_t
-_lib.mok_i8_linear_workspace_bytes.argtypes = [ctypes.POINTER(mok_i8_linear_args)]
-_lib.mok_i8_linear.restype = ctypes.c_int
-_lib.mok_i8_linear.argtypes = [ctypes.POINTER(mok_i8_linear_args)]
 _lib.mok_i8_experts_workspace_bytes.restype = ctypes.c_size_t
 _lib.mok_i8_experts_workspace_bytes.argtypes = [ctypes.c_int] * 5
-_lib.mok_i8_experts.restype = ctypes.c_int
-_lib.mok_i8_experts.argtypes = [ctypes.POINTER(mok_i8_experts_args)]
 _lib.mok_i8_status.restype = ctypes.c_int
 _lib.mok_i8_status.argtypes = [ctypes.c_void_p]
 _lib.mok_bwd_workspace_bytes.restype = ctypes.c_size_t
@@ -266,6 +214,14 @@ class MokError(RuntimeError):
 def _check(status):
     if status != MOK_OK:
         raise MokError(status)
+
+
+_binding.set_error(MokError)
+# routing from logits, 8-bit products and 8-bit experts: bound in C++ (csrc/binding.cpp), since their smallest calls take as
+# long as the host does
+mok_gate, mok_gate_backward = _binding.mok_gate, _binding.mok_gate_backward
+mok_i8_quantize, mok_i8_linear, mok_i8_matmul = _binding.mok_i8_quantize, _binding.mok_i8_linear, _binding.mok_i8_matmul
+mok_i8_experts = _binding.mok_i8_experts
 
 
 def _p(t):
@@ -716,98 +672,6 @@ def mok_moe_backward(x, W_gate_up, W_down, W_shared_gate_up, W_shared_down, topk
     return res
 
 
-_TYPES = {torch.bfloat16: MOK_TYPE_BF16, torch.float16: MOK_TYPE_F16, torch.float32: MOK_TYPE_F32}
-_HALVES, _INT8 = (torch.bfloat16, torch.float16), (torch.int8,)
-_SCORES = {"softmax": MOK_SCORE_SOFTMAX, "sigmoid": MOK_SCORE_SIGMOID}
-
-
-_current_device = torch._C._cuda_getDevice                 # (torch.cuda.current_device / current_stream without their checks:
-_raw_stream = torch._C._cuda_getCurrentRawStream           #  a third of the host time of a small call)
-
-
-def _on_stream(call):
-    """For the entry points below: runs the call on the device of its first tensor and, with stream=, on that stream, so that
-    outputs and scratch that it allocates belong to the stream that writes them."""
-    @functools.wraps(call)
-    def wrapped(first, *args, stream=None, **kwargs):
-        device = first.get_device()
-        if device < 0:
-            raise ValueError(f"{call.__name__}: tensors have to be on a CUDA device, got {first.device}")
-        if stream is None and device == _current_device():
-            return call(_raw_stream(device), first, *args, **kwargs)
-        with torch.cuda.device(device):
-            if stream is None:
-                return call(_raw_stream(device), first, *args, **kwargs)
-            with torch.cuda.stream(stream):
-                return call(stream.cuda_stream, first, *args, **kwargs)
-    sig = inspect.signature(call)                          # what a caller sees: the tensor first, stream= last
-    first, *rest = list(sig.parameters.values())[1:]
-    wrapped.__signature__ = sig.replace(parameters=[
-        first.replace(kind=inspect.Parameter.POSITIONAL_ONLY), *rest,
-        inspect.Parameter("stream", inspect.Parameter.KEYWORD_ONLY, default=None)])
-    return wrapped
-
-
-def _rows(name, t, width, device, dtypes):
-    """Checks a matrix argument [rows, width] whose last index is contiguous; returns the elements between its rows."""
-    shape, strides = t.shape, t.stride()
-    if len(shape) != 2 or shape[1] < width or t.dtype not in dtypes or t.device != device or (strides[1] != 1 and shape[1] > 1):
-        raise ValueError(f"{name}: expected rows of {width} contiguous elements of {tuple(dtypes)} on {device}, got shape "
-                         f"{tuple(shape)}, strides {strides}, {t.dtype} on {t.device}")
-    return strides[0] if shape[0] > 1 else shape[1]
-
-
-def _packed(name, t, shape, device, dtype):
-    """Checks an argument that has to be contiguous; returns its address."""
-    if t.shape != shape or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}, got shape {tuple(t.shape)}, "
-                         f"strides {t.stride()}, {t.dtype} on {t.device}")
-    return t.data_ptr()
-
-
-@_on_stream
-def mok_gate(raw_stream, logits, k, bias=None, score="softmax", n_groups=1, topk_groups=1, group_top=2, renormalise=True, scale=1.0):
-    """Routing from logits [T, E] (bf16, fp16 or fp32): returns (topk_idx int32 [T, k], topk_w fp32 [T, k]).  score:
-    "softmax" or "sigmoid"; bias fp32 [E] takes part in the selection only; see include/mok.h for groups and weights."""
-    (T, E), device = logits.shape, logits.device
-    ld = _rows("logits", logits, E, device, _TYPES)
-    idx = torch.empty_strided((T, k), (k, 1), dtype=torch.int32, device=device)      # (1 us less host time than empty)
-    w = torch.empty_strided((T, k), (k, 1), dtype=torch.float32, device=device)
-    _check(_lib.mok_gate(mok_gate_args(
-        logits.data_ptr(), None if bias is None else _packed("bias", bias, (E,), device, torch.float32), ld, T, E, k,
-        _TYPES[logits.dtype], _SCORES[score], n_groups, topk_groups, group_top, bool(renormalise), scale, idx.data_ptr(),
-        w.data_ptr(), raw_stream)))
-    return idx, w
-
-
-@_on_stream
-def mok_gate_backward(raw_stream, logits, topk_idx, dw, score="softmax", renormalise=True, scale=1.0):
-    """dL/dlogits [T, E] (in the logits' type) from dL/dtopk_w (dw) and the chosen experts of mok_gate."""
-    (T, E), device = logits.shape, logits.device
-    k = topk_idx.shape[-1]
-    ld = _rows("logits", logits, E, device, _TYPES)
-    out = torch.empty_strided((T, E), (E, 1), dtype=logits.dtype, device=device)
-    _check(_lib.mok_gate_backward(mok_gate_bwd_args(
-        logits.data_ptr(), _packed("topk_idx", topk_idx, (T, k), device, torch.int32),
-        _packed("dw", dw, (T, k), device, torch.float32), ld, E, T, E, k, _TYPES[logits.dtype], _SCORES[score],
-        bool(renormalise), scale, out.data_ptr(), raw_stream)))
-    return out
-
-
-@_on_stream
-def mok_i8_quantize(raw_stream, x):
-    """Rows of x [..., K] (bf16, fp16 or fp32) -> (codes int8 [..., K rounded up to 16], scales fp32 [...])."""
-    K = x.shape[-1]
-    rows = x if x.dim() == 2 else x.reshape(-1, K)
-    ldx = _rows("x", rows, K, x.device, _TYPES)
-    pitch = (K + 15) // 16 * 16
-    codes = torch.empty((*x.shape[:-1], pitch), dtype=torch.int8, device=x.device)
-    scales = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-    _check(_lib.mok_i8_quantize(rows.data_ptr(), _TYPES[x.dtype], rows.shape[0], K, ldx, codes.data_ptr(), pitch,
-                                scales.data_ptr(), raw_stream))
-    return codes, scales
-
-
 class I8Weights:
     """8-bit weights with a scale for each output channel: codes int8 [N, K] or [E, N, K] (rows of a multiple of 16 bytes;
     columns past the activations' K are not read), scales fp32 [N] or [E, N], and max, the largest scale of each matrix
@@ -824,86 +688,12 @@ class I8Weights:
         return cls(*mok_i8_quantize(W, stream=stream))
 
 
-def _i8_product(x, x_codes, x_scales, x_stride, codes_stride, M, K, x_type, weights, bias, out_dtype, workspace, device,
-                raw_stream):
-    W = weights.codes
-    N = W.shape[0]
-    w_stride = _rows("weights.codes", W, K, device, _INT8)
-    out = torch.empty_strided((M, N), (N, 1), dtype=out_dtype, device=device)
-    a = mok_i8_linear_args(
-        x, x_codes, x_scales, W.data_ptr(), _packed("weights.scales", weights.scales, (N,), device, torch.float32),
-        None if bias is None else _packed("bias", bias, (N,), device, torch.float32), x_stride, codes_stride, w_stride, N,
-        M, K, N, x_type, _TYPES[out_dtype], out.data_ptr(), None, 0, raw_stream)
-    if workspace is not None:
-        a.workspace, a.workspace_bytes = _aligned_ws(workspace)
-    elif x is not None:
-        n = _lib.mok_i8_linear_workspace_bytes(a)
-        if n:
-            workspace = torch.empty_strided((n,), (1,), dtype=torch.uint8, device=device)
-            a.workspace, a.workspace_bytes = workspace.data_ptr(), n
-    _check(_lib.mok_i8_linear(a))
-    return out
-
-
-@_on_stream
-def mok_i8_linear(raw_stream, x, weights, bias=None, out_dtype=None, workspace=None):
-    """out [M, N] = quantise(x [M, K]) W8^T (+ bias): the rows of x are quantised in the call.  weights: I8Weights [N, K];
-    out_dtype defaults to x's.  workspace: a uint8 tensor of M * (K + 20) + 768 bytes (None: allocated if the call needs it)."""
-    (M, K), device, dtype = x.shape, x.device, x.dtype
-    return _i8_product(x.data_ptr(), None, None, _rows("x", x, K, device, _TYPES), 0, M, K, _TYPES[dtype], weights, bias,
-                       out_dtype or dtype, workspace, device, raw_stream)
-
-
-@_on_stream
-def mok_i8_matmul(raw_stream, codes, scales, weights, K=None, bias=None, out_dtype=torch.bfloat16):
-    """out [M, N] from rows that are 8-bit already (mok_i8_quantize): codes int8 [M, >= K], scales fp32 [M]."""
-    M, device = codes.shape[0], codes.device
-    K = weights.codes.shape[1] if K is None else K
-    return _i8_product(None, codes.data_ptr(), _packed("scales", scales, (M,), device, torch.float32), 0,
-                       _rows("codes", codes, K, device, _INT8), M, K, 0, weights, bias, out_dtype, None, device, raw_stream)
-
-
 def alloc_i8_workspace(T, H, I, E, k, device="cuda"):
     """A torch uint8 buffer large enough for mok_i8_experts."""
     n = int(_lib.mok_i8_experts_workspace_bytes(T, H, I, E, k))
     if n == 0:
         raise MokError(MOK_ERR_SHAPE)
     return torch.empty(n + 256, dtype=torch.uint8, device=device)
-
-
-def _expert_weights(name, w, E, n, width, device):
-    """Addresses of a stack of 8-bit matrices [E, n, >= width] and of its scales, and its row pitch."""
-    pitch = w.codes.shape[-1]
-    if pitch < width:
-        raise ValueError(f"{name}.codes: expected [{E}, {n}, >= {width}], got {tuple(w.codes.shape)}")
-    return (_packed(name + ".codes", w.codes, (E, n, pitch), device, torch.int8),
-            _packed(name + ".scales", w.scales, (E, n), device, torch.float32), pitch)
-
-
-@_on_stream
-def mok_i8_experts(raw_stream, x, topk_idx, topk_w, gate_up, down, add=None, workspace=None):
-    """out [T, H] = add + sum_s topk_w[:, s] f_{topk_idx[:, s]}(x) on 8-bit operands; gate_up: I8Weights [E, 2I, H], down:
-    I8Weights [E, H, I].  Ids outside 0 .. E-1 are not routed.  workspace: from alloc_i8_workspace (None: allocated)."""
-    (T, H), device, dtype = x.shape, x.device, x.dtype
-    k, E, I = topk_idx.shape[-1], gate_up.codes.shape[0], gate_up.codes.shape[-2] // 2
-    ldx = _rows("x", x, H, device, _HALVES)
-    gu, gu_scales, gu_pitch = _expert_weights("gate_up", gate_up, E, 2 * I, H, device)
-    dn, dn_scales, dn_pitch = _expert_weights("down", down, E, H, I, device)
-    ld_add = 0
-    if add is not None:
-        ld_add = _rows("add", add, H, device, (dtype,))
-        if add.shape != x.shape:
-            raise ValueError(f"add: expected {tuple(x.shape)}, got {tuple(add.shape)}")
-    if workspace is None:
-        workspace = torch.empty(_lib.mok_i8_experts_workspace_bytes(T, H, I, E, k), dtype=torch.uint8, device=device)
-    ws, ws_bytes = _aligned_ws(workspace)
-    out = torch.empty_strided((T, H), (H, 1), dtype=dtype, device=device)
-    _check(_lib.mok_i8_experts(mok_i8_experts_args(
-        x.data_ptr(), _packed("topk_idx", topk_idx, (T, k), device, torch.int32),
-        _packed("topk_w", topk_w, (T, k), device, torch.float32), gu, gu_scales, dn, dn_scales,
-        _packed("down.max", down.max, (E,), device, torch.float32), None if add is None else add.data_ptr(),
-        ldx, gu_pitch, dn_pitch, ld_add, H, T, H, I, E, k, _TYPES[dtype], out.data_ptr(), ws, ws_bytes, raw_stream)))
-    return out
 
 
 def mok_i8_experts_workspace_bytes(T, H, I, E, k):

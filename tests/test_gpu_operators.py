@@ -524,8 +524,12 @@ def test_refusals(mok):
                  lambda: mok.mok_gate_backward(logits, torch.zeros(4, 2, device="cuda", dtype=torch.int32), randn(g, 4, 3))):
         with pytest.raises(ValueError):
             call()
-    with pytest.raises(KeyError):
+    with pytest.raises(ValueError):
         mok.mok_gate(logits, 2, score="tanh")
+    for call in (lambda: mok.mok_gate(logits), lambda: mok.mok_gate(logits, 2, groups=2), lambda: mok.mok_gate(logits, 2, k=2),
+                 lambda: mok.mok_gate([1.0], 1), lambda: mok.mok_gate(logits, 2, score=3)):
+        with pytest.raises(TypeError):
+            call()
     x, w = randn(g, 4, 32).bfloat16(), weights(mok, g, 24, 32)
     with pytest.raises(ValueError):
         mok.mok_i8_linear(randn(g, 4, 33).bfloat16(), w)                                    # weights narrower than x
