@@ -9,12 +9,13 @@
 // The scores rise with the logits, so without a bias and without sums of two scores the logits themselves are compared:
 // two logits that a score rounds to the same number keep their order, and no score but the chosen ones is computed.
 //
-// The kernels are bound by instructions, not by the logits' bytes (32768 tokens of 256 experts: 5 us of memory traffic), so
-// the common case, no groups or groups of whole 32 experts, puts FOUR tokens into a warp, eight lanes each: every step
+// With many tokens the kernels are bound by instructions, not by the logits' bytes (32768 tokens of 256 experts: 5 us of
+// memory traffic), so the common case, no groups or groups of whole 32 experts, puts FOUR tokens into a warp, eight lanes each: every step
 // across lanes then serves four tokens.  Lane p of a token holds pieces p, p + 8, ... of four consecutive experts and the
 // largest value of each piece; a round of the selection is a maximum over the lane's pieces, three shuffles across the
 // eight lanes, and a refill of the one piece that lost its largest value (the values wait in shared memory).
-// 275 instructions per token against 1100 with a warp per token.  Other groupings take the warp-per-token kernel.
+// 480 instructions per token against 1300 with a warp per token.  Other groupings, and batches that do not fill the GPU (up to
+// some 2300 tokens: 4.7 against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
 #include "mok_internal.cuh"
 #include <cuda_fp16.h>
 #include <float.h>
@@ -432,7 +433,8 @@ struct BwdParams {
 // Only the last one is non-zero outside the chosen experts (and reads all logits).  1 - s is sigmoid(-l), without the
 // cancellation.  Four tokens per warp, eight lanes each, as in the forward kernel; a token's row is put together in shared
 // memory and written once, in 16-byte pieces.  Chosen ids outside 0 .. E-1 (routes that were dropped) have no part in it.
-template <class L>
+// NI: pieces of four experts per lane, as in the forward kernel; 0 where only the chosen experts have a gradient.
+template <class L, int NI, bool VEC>
 __global__ void __launch_bounds__(32 * WARPS)
 gate_backward_kernel(const BwdParams p) {
     extern __shared__ __align__(16) float s_row[];   // [WARPS][4][E rounded up to 8], zero between tokens
@@ -441,7 +443,9 @@ gate_backward_kernel(const BwdParams p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 7, own = lane >> 3;
     const int E = p.E, k = p.k, pitch = (E + 7) & ~7;
     float* mine = s_row + (warp * 4 + own) * pitch;
-    const bool vec = E % PER == 0 && p.d_stride % PER == 0 && (reinterpret_cast<uintptr_t>(p.dlogits) & 15u) == 0;
+    // (16-byte pieces; of four experts with NI > 0)
+    constexpr int PIECE = NI == 0 ? PER : 4;
+    const bool vec = E % PIECE == 0 && p.d_stride % PIECE == 0 && (reinterpret_cast<uintptr_t>(p.dlogits) & (PIECE * sizeof(L) - 1)) == 0;
     for (int i = sub; i < E; i += 8) mine[i] = 0.f;
     __syncwarp();
     for (long long t0 = ((long long)blockIdx.x * WARPS + warp) * 4; t0 < p.T; t0 += (long long)gridDim.x * WARPS * 4) {
@@ -463,7 +467,7 @@ gate_backward_kernel(const BwdParams p) {
                 else g[q] = 0.f;
             }
         }
-        if (!p.softmax || p.renormalise) {
+        if constexpr (NI == 0) {
             float s[SLOTS], total = 0.f, dot = 0.f, m = -INFINITY;
             if (p.softmax) {
 #pragma unroll
@@ -507,10 +511,20 @@ gate_backward_kernel(const BwdParams p) {
                 for (int i = sub; i < E; i += 8) store_f(out + i, mine[i]);
             }
         } else {
-            float m = -INFINITY, sum = 0.f, dot = 0.f;
-            for (int i = sub; i < E; i += 8) m = fmaxf(m, load_f(row + i));
+            // every expert: the row's exponentials stay in registers, the chosen ones' gradients wait in shared memory
+            float c[NI][4], m = -INFINITY, sum = 0.f, dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) load4<VEC>(row, (sub + 8 * i) * 4, E, c[i]);
+#pragma unroll
+            for (int i = 0; i < NI; ++i) m = fmaxf(m, fmaxf(fmaxf(c[i][0], c[i][1]), fmaxf(c[i][2], c[i][3])));
             m = max8(m);
-            for (int i = sub; i < E; i += 8) sum += exp_below(load_f(row + i), m);
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    c[i][j] = exp_below(c[i][j], m);
+                    sum += c[i][j];
+                }
             sum = sum8(sum);
             const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
@@ -521,8 +535,24 @@ gate_backward_kernel(const BwdParams p) {
             }
             dot = sum8(dot);
             __syncwarp();
-            if (live)
-                for (int i = sub; i < E; i += 8) store_f(out + i, exp_below(load_f(row + i), m) * inv * (mine[i] - dot));
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int at = (sub + 8 * i) * 4;
+                if (!live || at >= E) continue;
+                float v[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] = c[i][j] * inv * ((VEC || at + j < E ? mine[at + j] : 0.f) - dot);
+                if (VEC && vec) {
+                    struct alignas(4 * sizeof(L)) { L v[4]; } o;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) store_f(o.v + j, v[j]);
+                    *reinterpret_cast<decltype(o)*>(out + at) = o;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (at + j < E) store_f(out + at + j, v[j]);
+                }
+            }
         }
         __syncwarp();
 #pragma unroll
@@ -547,7 +577,7 @@ static cudaError_t launch_four(const Params& p, cudaStream_t s) {
 template <class L>
 static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
     const int n = (p.E + 31) / 32;
-    if (p.n_groups == 1 || p.E / p.n_groups % 32 == 0) {
+    if (p.T > 148 * 16 && (p.n_groups == 1 || p.E / p.n_groups % 32 == 0)) {
         if (n <= 1) return launch_four<L, 1>(p, s);
         if (n <= 2) return launch_four<L, 2>(p, s);
         if (n <= 4) return launch_four<L, 4>(p, s);
@@ -565,12 +595,25 @@ static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
     return launch_pdl(gate_warp_kernel<L, 16>, grid, block, smem, s, p);
 }
 
-template <class L>
-static cudaError_t launch_backward(const BwdParams& p, cudaStream_t s) {
+template <class L, int NI>
+static cudaError_t launch_backward_four(const BwdParams& p, cudaStream_t s) {
+    const bool vec = p.E % 4 == 0 && (p.T == 1 || p.stride % 4 == 0) && (reinterpret_cast<uintptr_t>(p.logits) & (4 * sizeof(L) - 1)) == 0;
     const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * 8;
     const long long rounds = (units + wave - 1) / wave, blocks = (units + rounds - 1) / rounds;
-    return launch_pdl(gate_backward_kernel<L>, dim3((unsigned)blocks), dim3(32 * WARPS), sizeof(float) * WARPS * 4 * ((p.E + 7) & ~7),
-                      s, p);
+    const size_t smem = sizeof(float) * WARPS * 4 * ((p.E + 7) & ~7);
+    const dim3 grid((unsigned)blocks), block(32 * WARPS);
+    return NI > 0 && vec ? launch_pdl(gate_backward_kernel<L, NI, true>, grid, block, smem, s, p)
+                         : launch_pdl(gate_backward_kernel<L, NI, false>, grid, block, smem, s, p);
+}
+
+template <class L>
+static cudaError_t launch_backward(const BwdParams& p, cudaStream_t s) {
+    if (!p.softmax || p.renormalise) return launch_backward_four<L, 0>(p, s);
+    const int n = (p.E + 31) / 32;
+    if (n <= 2) return launch_backward_four<L, 2>(p, s);
+    if (n <= 4) return launch_backward_four<L, 4>(p, s);
+    if (n <= 8) return launch_backward_four<L, 8>(p, s);
+    return launch_backward_four<L, 16>(p, s);
 }
 
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
