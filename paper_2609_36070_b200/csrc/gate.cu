@@ -12,8 +12,13 @@
 // With many tokens the kernels are bound by instructions, not by the logits' bytes (32768 tokens of 256 experts: 5 us of
 // memory traffic), so the common case, no groups or groups of whole 32 experts, puts FOUR tokens into a warp, eight lanes each: every step
 // across lanes then serves four tokens.  Lane p of a token holds pieces p, p + 8, ... of four consecutive experts and the
-// largest value of each piece; a round of the selection is a maximum over the lane's pieces, three shuffles across the
-// eight lanes, and a refill of the one piece that lost its largest value (the values wait in shared memory).
+// largest value of each piece.  Two ways to the k largest:
+//   - lists (k = 5 .. 16): the k-th largest of the sixteen half-lane maxima is a lower bound of the k-th largest value; the
+//     values that reach it, a few more than k, are listed in shared memory, and a value's place is the number of listed
+//     values before it.
+//   - rounds (small k, where they are cheaper; large k; and tokens with more than 32 values in reach, which equal values can
+//     bring): a maximum over the lane's pieces, three shuffles across the eight lanes, and a refill of the one piece that
+//     lost its largest value.
 // 480 instructions per token against 1300 with a warp per token.  Other groupings, and batches that do not fill the GPU (up to
 // some 2300 tokens: 4.7 against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
 #include "mok_internal.cuh"
@@ -240,6 +245,8 @@ __device__ __forceinline__ float sum8(float v) {
 // Values that compare below every other one, so that -inf can stand for "not there": NaN, then -inf, then the finite ones.
 constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOWEST = -3.40282306e38f;
 
+template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      // shared memory of a warp
+
 // Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.
 constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 8 ? 5 : 2; }
 
@@ -247,14 +254,16 @@ constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 8 ? 5 : 2; }
 template <class L, int NI, bool VEC>
 __global__ void __launch_bounds__(32 * WARPS, gate_blocks(NI))
 gate_kernel(const Params p) {
-    extern __shared__ __align__(16) float s_mem[];   // per warp: values [4][32 NI], then chosen ids [4][MAX_K]
+    extern __shared__ __align__(16) float s_mem[];   // per warp: values [4][32 NI], chosen ids [4][MAX_K], lists [4][32][2]
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 7, own = lane >> 3;
     const int E = p.E, k = p.k, G = p.n_groups, span = G > 1 ? E / G / 32 : NI;
     const bool by_score = p.bias != nullptr || (G > 1 && p.group_top == 2);
     const bool full_sum = p.softmax && (by_score || !p.renormalise);
-    float* vals = s_mem + (size_t)warp * 4 * (32 * NI + MAX_K) + own * 32 * NI;
-    int* chosen = reinterpret_cast<int*>(s_mem + (size_t)warp * 4 * (32 * NI + MAX_K) + 4 * 32 * NI) + own * MAX_K;
+    float* space = s_mem + (size_t)warp * GATE_FLOATS<NI>;
+    float* vals = space + own * 32 * NI;
+    int* chosen = reinterpret_cast<int*>(space + 4 * 32 * NI) + own * MAX_K;
+    float2* list = reinterpret_cast<float2*>(space + 4 * (32 * NI + MAX_K)) + own * 32;
     for (long long t0 = ((long long)blockIdx.x * WARPS + warp) * 4; t0 < p.T; t0 += (long long)gridDim.x * WARPS * 4) {
         const long long t = t0 + own < p.T ? t0 + own : p.T - 1;       // (past the end: the last token again, not written)
         const L* row = reinterpret_cast<const L*>(p.logits) + t * p.stride;
@@ -356,35 +365,107 @@ gate_kernel(const Params p) {
             }
         }
         __syncwarp();
-        for (int s = 0; s < k; ++s) {
-            float mine = top[0];
+        bool listed = NI <= 8 && k > 4 && k <= 16;
+        if (listed) {
+            float h0, h1;                            // the lane's two half maxima
+            if (NI == 1) {
+                h0 = fmaxf(c[0][0], c[0][1]);
+                h1 = fmaxf(c[0][2], c[0][3]);
+            } else {
+                h0 = top[0];
+                h1 = top[NI / 2];
 #pragma unroll
-            for (int i = 1; i < NI; ++i) mine = fmaxf(mine, top[i]);
-            const float best = max8(mine);
-            unsigned holders = (__ballot_sync(0xffffffffu, mine == best) >> (lane & 24)) & 0xffu;
-            int bi = 0;
-            if (mine == best) {
-#pragma unroll
-                for (int i = NI - 1; i >= 0; --i)
-                    if (top[i] == best) bi = i;      // the lane's lowest ids
+                for (int i = 1; i < NI / 2; ++i) {
+                    h0 = fmaxf(h0, top[i]);
+                    h1 = fmaxf(h1, top[NI / 2 + i]);
+                }
             }
-            const int piece = sub + 8 * bi;
-            if (__any_sync(0xffffffffu, holders & (holders - 1))) {    // equal values in several lanes: the lowest piece
-                int low = mine == best ? piece : 0x7fffffff;
+            int above0 = 0, above1 = 0;              // how many of the sixteen are larger
 #pragma unroll
-                for (int off = 1; off < 8; off <<= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, off));
-                holders = 1u << (low & 7);
+            for (int q = 0; q < 8; ++q) {
+                const float o0 = __shfl_sync(0xffffffffu, h0, (lane & 24) + q), o1 = __shfl_sync(0xffffffffu, h1, (lane & 24) + q);
+                above0 += (o0 > h0 ? 1 : 0) + (o1 > h0 ? 1 : 0);
+                above1 += (o0 > h1 ? 1 : 0) + (o1 > h1 ? 1 : 0);
             }
-            if (holders == 1u << sub) {              // this lane's piece holds it: take it out, find the piece's next
-                const float4 v = *reinterpret_cast<const float4*>(vals + piece * 4);
-                const int j = v.x == best ? 0 : v.y == best ? 1 : v.z == best ? 2 : 3;
-                vals[piece * 4 + j] = -INFINITY;
-                chosen[s] = piece * 4 + j;
-                const float a = j == 0 ? v.y : v.x, b = j <= 1 ? v.z : v.y, d = j == 3 ? v.z : v.w;
-                const float next = fmaxf(fmaxf(a, b), d);
+            float reach = fminf(above0 < k ? h0 : INFINITY, above1 < k ? h1 : INFINITY);
 #pragma unroll
-                for (int i = 0; i < NI; ++i)
-                    if (i == bi) top[i] = next;
+            for (int off = 1; off < 8; off <<= 1) reach = fminf(reach, __shfl_xor_sync(0xffffffffu, reach, off));
+            unsigned mask = 0u;                      // bit 4 i + j: value j of piece i
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                if (NI <= 8 && top[i] >= reach) {    // (pieces of other groups have lost their maximum)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mask |= (c[i][j] >= reach ? 1u : 0u) << (4 * i + j);
+                }
+            }
+            const int mine = __popc(mask);
+            int upto = mine;
+#pragma unroll
+            for (int off = 1; off < 8; off <<= 1) {
+                const int o = __shfl_up_sync(0xffffffffu, upto, off, 8);
+                if (sub >= off) upto += o;
+            }
+            const int n = __shfl_sync(0xffffffffu, upto, lane | 7);
+            const int most = __reduce_max_sync(0xffffffffu, n);
+            listed = most <= 32 && reach > -INFINITY && __all_sync(0xffffffffu, n >= k);
+            listed = __all_sync(0xffffffffu, listed);
+            if (listed) {
+                int at = upto - mine;
+                while (mask) {
+                    const int b = __ffs(mask) - 1, e = (sub + 8 * (b >> 2)) * 4 + (b & 3);
+                    mask &= mask - 1;
+                    list[at++] = make_float2(vals[e], __int_as_float(e));
+                }
+                for (int q = sub; q < most; q += 8)
+                    if (q >= n) list[q] = make_float2(-INFINITY, 0.f);
+                __syncwarp();
+                for (int q0 = 0; q0 < most; q0 += 16) {      // two values per lane
+                    const float2 a = q0 + sub < n ? list[q0 + sub] : make_float2(-INFINITY, 0.f);
+                    const float2 b = q0 + 8 + sub < n ? list[q0 + 8 + sub] : make_float2(-INFINITY, 0.f);
+                    const int ia = __float_as_int(a.y), ib = __float_as_int(b.y);
+                    int ra = 0, rb = 0;
+                    for (int x = 0; x < most; ++x) {
+                        const float2 o = list[x];
+                        const int io = __float_as_int(o.y);
+                        ra += (o.x > a.x || (o.x == a.x && io < ia)) ? 1 : 0;
+                        rb += (o.x > b.x || (o.x == b.x && io < ib)) ? 1 : 0;
+                    }
+                    if (q0 + sub < n && ra < k) chosen[ra] = ia;
+                    if (q0 + 8 + sub < n && rb < k) chosen[rb] = ib;
+                }
+            }
+        }
+        if (!listed) {
+            for (int s = 0; s < k; ++s) {
+                float mine = top[0];
+#pragma unroll
+                for (int i = 1; i < NI; ++i) mine = fmaxf(mine, top[i]);
+                const float best = max8(mine);
+                unsigned holders = (__ballot_sync(0xffffffffu, mine == best) >> (lane & 24)) & 0xffu;
+                int bi = 0;
+                if (mine == best) {
+#pragma unroll
+                    for (int i = NI - 1; i >= 0; --i)
+                        if (top[i] == best) bi = i;      // the lane's lowest ids
+                }
+                const int piece = sub + 8 * bi;
+                if (__any_sync(0xffffffffu, holders & (holders - 1))) {    // equal values in several lanes: the lowest piece
+                    int low = mine == best ? piece : 0x7fffffff;
+#pragma unroll
+                    for (int off = 1; off < 8; off <<= 1) low = min(low, __shfl_xor_sync(0xffffffffu, low, off));
+                    holders = 1u << (low & 7);
+                }
+                if (holders == 1u << sub) {              // this lane's piece holds it: take it out, find the piece's next
+                    const float4 v = *reinterpret_cast<const float4*>(vals + piece * 4);
+                    const int j = v.x == best ? 0 : v.y == best ? 1 : v.z == best ? 2 : 3;
+                    vals[piece * 4 + j] = -INFINITY;
+                    chosen[s] = piece * 4 + j;
+                    const float a = j == 0 ? v.y : v.x, b = j <= 1 ? v.z : v.y, d = j == 3 ? v.z : v.w;
+                    const float next = fmaxf(fmaxf(a, b), d);
+#pragma unroll
+                    for (int i = 0; i < NI; ++i)
+                        if (i == bi) top[i] = next;
+                }
             }
         }
         __syncwarp();
@@ -569,7 +650,7 @@ static cudaError_t launch_four(const Params& p, cudaStream_t s) {
     // one wave of blocks with the same number of rounds each
     const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * gate_blocks(NI);
     const long long rounds = (units + wave - 1) / wave, blocks = (units + rounds - 1) / rounds;
-    const size_t smem = sizeof(float) * WARPS * 4 * (32 * NI + MAX_K);
+    const size_t smem = sizeof(float) * WARPS * GATE_FLOATS<NI>;
     const dim3 grid((unsigned)blocks), block(32 * WARPS);
     return vec ? launch_pdl(gate_kernel<L, NI, true>, grid, block, smem, s, p) : launch_pdl(gate_kernel<L, NI, false>, grid, block, smem, s, p);
 }
