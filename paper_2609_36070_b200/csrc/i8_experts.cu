@@ -17,27 +17,22 @@ constexpr int THREADS = 256;
 constexpr int ONE_BLOCK = 1024, ROUTES_PER_THREAD = 16;      // of the schedule in one block
 constexpr long long GROUPED_ROWS = 112;                      // rows per expert up to which launch_grouped is the faster one
 
-// Rows of h (fp32, padded row space) -> codes.  factor = scale * b_max / y_unit: what the combine multiplies a row by.
-// Pad rows are left alone.
+// Rows of h (fp32) -> codes, one per route: route j's row is pos[j].  factor = scale * b_max / y_unit: what the combine
+// multiplies a row by.
 template <int TPR, int NV>
 __global__ void __launch_bounds__(THREADS)
 quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ codes, int ldc, float* __restrict__ factor,
-                       const float* __restrict__ b_max, float inv_unit, const WsHeader* __restrict__ hdr,
-                       const int32_t* __restrict__ tile_expert, const int32_t* __restrict__ pad_offsets,
-                       const int32_t* __restrict__ counts) {
+                       const float* __restrict__ b_max, float inv_unit, const int32_t* __restrict__ idx,
+                       const int32_t* __restrict__ pos, int n, int E) {
     __shared__ uint32_t s_max[THREADS / 32];
     pdl_enter();
-    constexpr int ROWS = THREADS / TPR;
+    constexpr int ROWS = THREADS / TPR, WARPS = TPR / 32;
     const int sub = threadIdx.x % TPR, pieces = I >> 2;
-    const int rows = hdr->n_mtiles * TILE_M;
-    for (int p0 = blockIdx.x * ROWS; p0 < rows; p0 += gridDim.x * ROWS) {
-        const int p = p0 + threadIdx.x / TPR;
-        int e = 0;
-        bool live = p < rows;
-        if (live) {
-            e = __ldg(tile_expert + p / TILE_M);
-            live = p - __ldg(pad_offsets + e) < __ldg(counts + e);
-        }
+    for (int j0 = blockIdx.x * ROWS; j0 < n; j0 += gridDim.x * ROWS) {
+        const int j = j0 + threadIdx.x / TPR;
+        const int e = j < n ? __ldg(idx + j) : -1;
+        const bool live = (unsigned)e < (unsigned)E;
+        const int p = live ? __ldg(pos + j) : 0;
         const float4* src = reinterpret_cast<const float4*>(h + (size_t)p * I);
         float4 v[NV];
         uint32_t m = 0;
@@ -47,6 +42,7 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
             v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (live && c < pieces) v[i] = __ldcs(src + c);
         }
+        const float top = live ? __ldg(b_max + e) : 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             m = max(max(m, max(abs_bits(v[i].x), abs_bits(v[i].y))), max(abs_bits(v[i].z), abs_bits(v[i].w)));
@@ -56,7 +52,7 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
             __syncthreads();
             if (lane == 0) s_max[warp] = m;
             __syncthreads();
-            m = __reduce_max_sync(0xffffffffu, lane < THREADS / 32 ? s_max[lane] : 0u);
+            m = __reduce_max_sync(0xffffffffu, lane < WARPS ? s_max[warp / WARPS * WARPS + lane] : 0u);
         }
         if (!live) continue;
         const float amax = __uint_as_float(m);
@@ -68,11 +64,10 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
             const int c = sub + i * TPR;
             if (c >= pieces) break;
             uint32_t o = 0u;
-            if (codable)
-                o = four_codes(v[i].x, v[i].y, v[i].z, v[i].w, rule);
+            if (codable) o = four_codes(v[i].x, v[i].y, v[i].z, v[i].w, rule);
             *reinterpret_cast<uint32_t*>(dst + c * 4) = o;
         }
-        if (sub == 0) factor[p] = amax / 127.f * (b_max[e] * inv_unit);
+        if (sub == 0) factor[p] = amax / 127.f * (top * inv_unit);
     }
 }
 
@@ -137,9 +132,8 @@ combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ fact
 // order, which takes several passes (three launches); here a row's place inside its expert's segment is whatever an atomic
 // counter gives, because no result depends on it: every row is computed by itself, and the combine reads rows by `pos`.
 __global__ void __launch_bounds__(ONE_BLOCK)
-schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows, int32_t* __restrict__ counts,
-                    int32_t* __restrict__ pad_offsets, int32_t* __restrict__ tile_expert, int32_t* __restrict__ pos,
-                    int4* __restrict__ tiles, WsHeader* __restrict__ hdr) {
+schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows,
+                    int32_t* __restrict__ pos, int4* __restrict__ tiles, WsHeader* __restrict__ hdr) {
     __shared__ int32_t s_cnt[MAX_E], s_row0[MAX_E], s_pads[MAX_E / 32], s_tiles[MAX_E / 32];
     pdl_enter();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -174,16 +168,8 @@ schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows
         for (int q = 0; q < warp; ++q) { pads_to += s_pads[q]; tiles_to += s_tiles[q]; }
         const int pad0 = pads_to - pads, tile0 = tiles_to - mine;
         s_row0[tid] = pad0 * TILE_M;
-        if (tid < E) {
-            counts[tid] = c;
-            pad_offsets[tid] = pad0 * TILE_M;
-            for (int q = 0; q < pads; ++q) tile_expert[pad0 + q] = tid;
-            for (int q = 0; q < mine; ++q) tiles[tile0 + q] = make_int4(pad0 * TILE_M + q * tile_rows, c - q * tile_rows, tid, 0);
-        }
-        if (tid == MAX_E - 1) {
-            hdr->n_mtiles = pads_to;
-            hdr->n_ftiles = tiles_to;
-        }
+        for (int q = 0; q < mine; ++q) tiles[tile0 + q] = make_int4(pad0 * TILE_M + q * tile_rows, c - q * tile_rows, tid, 0);
+        if (tid == MAX_E - 1) hdr->n_ftiles = tiles_to;
     }
     __syncthreads();
 #pragma unroll
@@ -382,7 +368,7 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k, X.tile_rows};
     if (X.L.R <= i8::ONE_BLOCK * i8::ROUTES_PER_THREAD) {
         e = launch_pdl(i8::schedule_one_kernel, dim3(1), dim3(i8::ONE_BLOCK), 0, s, a->topk_idx, X.L.R, a->E, X.tile_rows,
-                       table(X.L.counts), table(X.L.pad_offsets), table(X.L.tile_expert), table(X.L.pos), tiles, hdr);
+                       table(X.L.pos), tiles, hdr);
         g.n_mtiles = &hdr->n_ftiles;
     } else {
         e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
@@ -421,17 +407,15 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
         const float* h = reinterpret_cast<const float*>(ws + X.h);
         int8_t* hq = reinterpret_cast<int8_t*>(ws + X.hq);
         float* factor = reinterpret_cast<float*>(ws + X.factor);
-        const int32_t *te = table(X.L.tile_expert), *pads = table(X.L.pad_offsets), *counts = table(X.L.counts);
-        const long long rows = X.L.Rpad, most = 148 * 16;
-        const bool warp_rows = a->I <= 1024;
-        const long long blocks = warp_rows ? (rows + 7) / 8 : rows;
-        const dim3 grid((unsigned)(blocks < most ? blocks : most)), block(i8::THREADS);
-        e = warp_rows ? launch_pdl(i8::quantize_hidden_kernel<32, 8>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor, a->down_max,
-                                   1.f / unit, hdr, te, pads, counts)
-            : a->I <= 8192 ? launch_pdl(i8::quantize_hidden_kernel<256, 8>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor,
-                                        a->down_max, 1.f / unit, hdr, te, pads, counts)
-                           : launch_pdl(i8::quantize_hidden_kernel<256, 16>, grid, block, 0, s, h, a->I, hq, X.pitch_i, factor,
-                                        a->down_max, 1.f / unit, hdr, te, pads, counts);
+        auto rows = [&](auto kernel, int per_block) {
+            const int blocks = (X.L.R + per_block - 1) / per_block, most = 148 * 16;
+            return launch_pdl(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(i8::THREADS), 0, s, h, a->I, hq, X.pitch_i,
+                              factor, a->down_max, 1.f / unit, a->topk_idx, table(X.L.pos), X.L.R, a->E);
+        };
+        e = a->I <= 1024 ? rows(i8::quantize_hidden_kernel<32, 8>, 8)
+            : a->I <= 2048 ? rows(i8::quantize_hidden_kernel<128, 4>, 2)
+            : a->I <= 4096 ? rows(i8::quantize_hidden_kernel<256, 4>, 1)
+            : a->I <= 8192 ? rows(i8::quantize_hidden_kernel<256, 8>, 1) : rows(i8::quantize_hidden_kernel<256, 16>, 1);
         if (e != cudaSuccess) return cuda_fail(e);
     }
     g.A = reinterpret_cast<const int8_t*>(ws + X.hq);
