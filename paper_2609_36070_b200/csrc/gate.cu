@@ -10,17 +10,18 @@
 // two logits that a score rounds to the same number keep their order, and no score but the chosen ones is computed.
 //
 // With many tokens the kernels are bound by instructions, not by the logits' bytes (32768 tokens of 256 experts: 5 us of
-// memory traffic), so the common case, no groups or groups of whole 32 experts, puts FOUR tokens into a warp, eight lanes each: every step
-// across lanes then serves four tokens.  Lane p of a token holds pieces p, p + 8, ... of four consecutive experts and the
-// largest value of each piece.  Two ways to the k largest:
+// memory traffic), so the common case, no groups or groups of a multiple of four experts, puts FOUR tokens into a warp,
+// eight lanes each: every step across lanes then serves four tokens.  Lane p of a token holds pieces p, p + 8, ... of four
+// consecutive experts and the largest value of each piece.  Two ways to the k largest:
 //   - lists (k = 5 .. 16): the k-th largest of the sixteen half-lane maxima is a lower bound of the k-th largest value; the
 //     values that reach it, a few more than k, are listed in shared memory, and a value's place is the number of listed
 //     values before it.
 //   - rounds (small k, where they are cheaper; large k; and tokens with more than 32 values in reach, which equal values can
 //     bring): a maximum over the lane's pieces, three shuffles across the eight lanes, and a refill of the one piece that
 //     lost its largest value.
-// 480 instructions per token against 1300 with a warp per token.  Other groupings, and batches that do not fill the GPU (up to
-// some 2300 tokens: 4.7 against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
+// 260 instructions per token (256 experts, k = 8; 440 with groups and a bias) against 610 (1300) with a warp per token: 14 (24)
+// us for 32768 tokens against 25 (53).  Other groupings, and batches that do not fill the GPU (up to some 2300 tokens: 4.7
+// against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
 #include "mok_internal.cuh"
 #include <cuda_fp16.h>
 #include <float.h>
@@ -250,14 +251,16 @@ template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      /
 // Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.
 constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 8 ? 5 : 2; }
 
-// No groups, or groups of whole 32 experts: four tokens per warp.  NI pieces of four experts per lane (E <= 32 NI).
+// No groups, or groups of whole pieces of four experts: four tokens per warp.  NI pieces of four experts per lane (E <= 32 NI).
 template <class L, int NI, bool VEC>
 __global__ void __launch_bounds__(32 * WARPS, gate_blocks(NI))
 gate_kernel(const Params p) {
     extern __shared__ __align__(16) float s_mem[];   // per warp: values [4][32 NI], chosen ids [4][MAX_K], lists [4][32][2]
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 7, own = lane >> 3;
-    const int E = p.E, k = p.k, G = p.n_groups, span = G > 1 ? E / G / 32 : NI;
+    const int E = p.E, k = p.k, G = p.n_groups;
+    // pieces of a group, and the factor by which a piece's number gives its group (of at most 128 pieces: exact)
+    const int per_group = E / G / 4, group_magic = G > 1 ? (65536 + per_group - 1) / per_group : 0;
     const bool by_score = p.bias != nullptr || (G > 1 && p.group_top == 2);
     const bool full_sum = p.softmax && (by_score || !p.renormalise);
     float* space = s_mem + (size_t)warp * GATE_FLOATS<NI>;
@@ -328,41 +331,37 @@ gate_kernel(const Params p) {
             *reinterpret_cast<float4*>(vals + (sub + 8 * i) * 4) = make_float4(c[i][0], c[i][1], c[i][2], c[i][3]);
         }
         if (G > 1) {
-            // lane sub finds the two best of group sub, then of group sub + 8 (of at most 16), from the values in shared
-            // memory; the lanes start at different pieces, so that they do not meet in a bank
+            // lane sub finds the two best of groups sub, sub + 8, ... from the values in shared memory; the lanes start at
+            // different pieces, so that they do not meet in a bank.  Every group's value is then compared with all others.
             __syncwarp();
-            const int pieces = 8 * span;
-            float v0 = -INFINITY, v1 = -INFINITY;
+            float* value = reinterpret_cast<float*>(list);
             for (int g = sub; g < G; g += 8) {
-                const float4* mine = reinterpret_cast<const float4*>(vals + g * 32 * span);
+                const float4* mine = reinterpret_cast<const float4*>(vals) + g * per_group;
                 float b1 = -INFINITY, b2 = -INFINITY;
-                for (int it = 0; it < pieces; ++it) {
-                    const float4 f = mine[(it & ~7) | ((it + sub) & 7)];
+                int at = sub < per_group ? sub : sub % per_group;
+                for (int it = 0; it < per_group; ++it) {
+                    const float4 f = mine[at];
+                    at = at + 1 == per_group ? 0 : at + 1;
                     const float h0 = fmaxf(f.x, f.y), h1 = fmaxf(f.z, f.w), h = fmaxf(h0, h1);
                     const float second = fmaxf(fminf(h0, h1), fmaxf(fminf(f.x, f.y), fminf(f.z, f.w)));
                     b2 = fmaxf(fmaxf(b2, second), fminf(b1, h));
                     b1 = fmaxf(b1, h);
                 }
-                const float v = p.group_top == 2 ? b1 + b2 : b1;
-                if (g < 8) v0 = v;
-                else v1 = v;
+                value[g] = p.group_top == 2 ? b1 + b2 : b1;
             }
             __syncwarp();
-            int rank0 = 0, rank1 = 0;
-            for (int q = 0; q < G; ++q) {
-                const float other = __shfl_sync(0xffffffffu, q < 8 ? v0 : v1, (lane & 24) + (q & 7));
-                rank0 += (other > v0 || (other == v0 && q < sub)) ? 1 : 0;
-                if (NI > 8) rank1 += (other > v1 || (other == v1 && q < sub + 8)) ? 1 : 0;
+            unsigned kept = 0u;
+            for (int g = sub; g < G; g += 8) {
+                const float v = value[g];
+                int rank = 0;
+                for (int q = 0; q < G; ++q) rank += (value[q] > v || (value[q] == v && q < g)) ? 1 : 0;
+                kept |= (rank < p.topk_groups ? 1u : 0u) << g;
             }
-            const unsigned k0 = __ballot_sync(0xffffffffu, rank0 < p.topk_groups);
-            const unsigned k1 = NI > 8 ? __ballot_sync(0xffffffffu, rank1 < p.topk_groups) : 0u;
-            const unsigned kept = ((k0 >> (lane & 24)) & 0xffu) | (((k1 >> (lane & 24)) & 0xffu) << 8);
-            int g = 0, until = span;
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                if (!((kept >> g) & 1u)) top[i] = -INFINITY;
-                if (--until == 0) { ++g; until = span; }
-            }
+            for (int off = 1; off < 8; off <<= 1) kept |= __shfl_xor_sync(0xffffffffu, kept, off);
+#pragma unroll
+            for (int i = 0; i < NI; ++i)
+                if (!((kept >> ((unsigned)((sub + 8 * i) * group_magic) >> 16)) & 1u)) top[i] = -INFINITY;
         }
         __syncwarp();
         bool listed = NI <= 8 && k > 4 && k <= 16;
@@ -658,7 +657,7 @@ static cudaError_t launch_four(const Params& p, cudaStream_t s) {
 template <class L>
 static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
     const int n = (p.E + 31) / 32;
-    if (p.T > 148 * 16 && (p.n_groups == 1 || p.E / p.n_groups % 32 == 0)) {
+    if (p.T > 148 * 16 && (p.n_groups == 1 || p.E / p.n_groups % 4 == 0)) {
         if (n <= 1) return launch_four<L, 1>(p, s);
         if (n <= 2) return launch_four<L, 2>(p, s);
         if (n <= 4) return launch_four<L, 4>(p, s);

@@ -75,6 +75,16 @@ GATES = [  # T, E, k, score, groups, topk_groups, group_top, bias, renorm, scale
     (40000, 32, 2, "softmax", 1, 1, 1, False, True, 1.0, torch.bfloat16),
     (17, 31, 31, "sigmoid", 1, 1, 1, True, True, 1.0, torch.float32),
     (1001, 512, 10, "sigmoid", 16, 5, 2, True, True, 1.0, torch.float32),
+    # enough tokens for four of them in a warp: with and without lists, groups of several sizes, rows that are not aligned
+    (3001, 256, 8, "sigmoid", 8, 4, 2, True, True, 2.5, torch.float32),
+    (2500, 160, 6, "softmax", 8, 3, 1, False, False, 16.0, torch.bfloat16),
+    (2401, 510, 17, "sigmoid", 1, 1, 1, True, True, 1.0, torch.float16),
+    (2402, 512, 16, "sigmoid", 32, 12, 2, True, True, 1.0, torch.float32),
+    (2403, 60, 5, "softmax", 5, 2, 2, True, True, 1.0, torch.float32),
+    (2404, 64, 8, "sigmoid", 16, 4, 2, False, True, 1.0, torch.float32),
+    (5000, 37, 9, "softmax", 1, 1, 1, True, False, 1.0, torch.bfloat16),
+    (2405, 24, 3, "sigmoid", 2, 1, 2, True, True, 1.0, torch.float32),
+    (2406, 8, 8, "softmax", 1, 1, 1, False, True, 1.0, torch.float32),
     (515, 384, 8, "softmax", 4, 3, 2, True, True, 1.0, torch.float16),
     (515, 320, 6, "sigmoid", 5, 1, 1, False, True, 1.0, torch.bfloat16),
     (130, 128, 32, "softmax", 4, 4, 1, False, False, 1.0, torch.float32),
@@ -93,7 +103,8 @@ def test_gate(mok, T, E, k, score, G, tg, gt, with_bias, renorm, scale, dtype):
     s, c, gap = choices64(logits, bias, score, G, tg, gt)
     assert ((idx >= 0) & (idx < E)).all()
     assert (idx.sort(-1).values.diff(dim=-1) > 0).all()                # distinct
-    clear = gap > 1e-6                                                 # fp32 scores decide the groups of the others
+    # fp32 scores decide the groups of the other tokens; where logits are compared, equal ones included, all is decided
+    clear = gap > 1e-6 if bias is not None or (G > 1 and gt == 2) else torch.ones_like(gap, dtype=torch.bool)
     assert clear.float().mean() > 0.97
     mine, best = c.gather(1, idx.long())[clear], c.sort(dim=-1, descending=True).values[:, :k][clear]
     assert (mine - best).abs().max() <= 1e-6                           # scores are below 1, each good to a few 2^-24
@@ -101,10 +112,11 @@ def test_gate(mok, T, E, k, score, G, tg, gt, with_bias, renorm, scale, dtype):
     assert ((w.double() - ref).abs() <= 16 * UNIT[torch.float32] * ref.abs() * 8 + 1e-30).all()
 
 
+@pytest.mark.parametrize("T", [257, 2600])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
-def test_gate_ties_go_to_the_lowest_id(mok, dtype):
+def test_gate_ties_go_to_the_lowest_id(mok, dtype, T):
     g = gen(3)
-    logits = torch.randint(-3, 4, (257, 96), generator=g, device="cuda").to(dtype)      # seven values: ties everywhere
+    logits = torch.randint(-3, 4, (T, 96), generator=g, device="cuda").to(dtype)        # seven values: ties everywhere
     logits[0] = 0.0
     logits[1, ::2] = -0.0                                               # equal to +0
     logits[1, 1::2] = 0.0
@@ -113,17 +125,19 @@ def test_gate_ties_go_to_the_lowest_id(mok, dtype):
         ref = logits.float().add(0.0).sort(dim=-1, descending=True, stable=True).indices[:, :8]
         assert torch.equal(idx.long(), ref)
         # equal groups as well: every group has the same two best
-        tied = torch.zeros(4, 96, device="cuda", dtype=dtype)
-        idx, _ = mok.mok_gate(tied, 4, score=score, n_groups=6, topk_groups=2, group_top=2)
-        assert torch.equal(idx, torch.arange(4, device="cuda", dtype=torch.int32).expand(4, 4))
+        tied = torch.zeros(T, 96, device="cuda", dtype=dtype)
+        for k, G in ((4, 6), (8, 3), (7, 32)):
+            idx, _ = mok.mok_gate(tied, k, score=score, n_groups=G, topk_groups=3, group_top=2)
+            assert torch.equal(idx, torch.arange(k, device="cuda", dtype=torch.int32).expand(T, k))
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
 @pytest.mark.parametrize("renorm", [True, False])
 @pytest.mark.parametrize("with_bias", [True, False])
-def test_gate_masked_and_broken_rows(mok, score, renorm, with_bias):
-    E, k = 40, 4
-    logits = randn(gen(1), 8, E)
+@pytest.mark.parametrize("T,k", [(8, 4), (2408, 4), (2408, 6)])
+def test_gate_masked_and_broken_rows(mok, score, renorm, with_bias, T, k):
+    E = 40
+    logits = randn(gen(1), T, E)
     bias = torch.zeros(E, device="cuda") if with_bias else None
     logits[0] = -math.inf                                               # nothing left
     logits[1, 3:] = -math.inf                                           # fewer experts than k
@@ -132,15 +146,15 @@ def test_gate_masked_and_broken_rows(mok, score, renorm, with_bias):
     logits[4] = math.nan
     logits[5, 7] = math.inf
     logits[6] = torch.finfo(torch.float32).min
-    clean = mok.mok_gate(logits[7:].contiguous(), k, bias=bias, score=score, renormalise=renorm)
+    clean = mok.mok_gate(torch.cat([logits[7:], logits[7:14]])[:T], k, bias=bias, score=score, renormalise=renorm)
     idx, w = mok.mok_gate(logits, k, bias=bias, score=score, renormalise=renorm)
     assert ((idx >= 0) & (idx < E)).all() and (idx.sort(-1).values.diff(dim=-1) > 0).all()
     assert torch.equal(idx[0], torch.arange(k, device="cuda", dtype=torch.int32)) and (w[0] == 0).all()
-    assert idx[1, :3].sort().values.tolist() == [0, 1, 2] and w[1, 3] == 0 and torch.isfinite(w[1]).all()
+    assert idx[1, :3].sort().values.tolist() == [0, 1, 2] and (w[1, 3:] == 0).all() and torch.isfinite(w[1]).all()
     assert (idx[2] % 2 == 1).all() and torch.isfinite(w[2]).all()
-    assert torch.equal(idx[7], clean[0][0]) and torch.equal(w[7], clean[1][0])          # other rows are not touched
+    assert torch.equal(idx[7:], clean[0][:T - 7]) and torch.equal(w[7:], clean[1][:T - 7])      # other rows are not touched
     if score == "softmax" and renorm:
-        assert (w[6] - 0.25).abs().max() < 1e-6                         # a uniform row, however low
+        assert (w[6] - 1 / k).abs().max() < 1e-6                        # a uniform row, however low
     if score == "sigmoid":
         assert idx[5, 0] == 7 and 5 not in idx[3].tolist()
 
@@ -190,12 +204,13 @@ def test_gate_gradient_against_differences(mok, score, renorm):
     assert ((along - diff).abs() <= (h * h / 6 * 2 + 2.0 ** -23 / h) * dw.abs().sum(-1) * 2).all()
 
 
-@pytest.mark.parametrize("G", [1, 2, 4])
-def test_gate_masked_experts_whatever_their_bias(mok, G):
+@pytest.mark.parametrize("T", [33, 2433])
+@pytest.mark.parametrize("G,k", [(1, 4), (2, 4), (4, 4), (4, 6)])
+def test_gate_masked_experts_whatever_their_bias(mok, T, G, k):
     """An expert whose logit is -inf is not chosen for a token that has k others, however large its bias."""
-    E, k = 64, 4
-    logits = randn(gen(21), 33, E)
-    masked = torch.rand(33, E, generator=gen(22), device="cuda") < 0.5
+    E = 64
+    logits = randn(gen(21), T, E)
+    masked = torch.rand(T, E, generator=gen(22), device="cuda") < 0.5
     logits[masked] = -math.inf
     bias = torch.where(masked.float().mean(0) > 0.5, 10.0, 0.0)
     for score in ("softmax", "sigmoid"):
