@@ -90,13 +90,18 @@ struct ProductArgs {
 enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
 
 // Where a token's codes go when its rows are wanted in expert order: row pos[t * k + s] for every routed slot s.
-// With `tiles` the launch also writes the product's list of row tiles from the schedule's tables.
+//   n > 0     : the launch makes the whole schedule of the n routes itself (at most ROUTES_HERE): pos, tiles and their number
+//   tiles     : it writes the products' list of row tiles from the schedule's tables
+//   otherwise : all of it is there
+constexpr int ROUTES_HERE = 1024;
 struct RouteArgs {
-    const int32_t *idx, *pos;
-    int32_t E, k;
-    int32_t tile_rows;           // 128 or 256
+    const int32_t* idx;
+    int32_t* pos;
+    int32_t E, k, n;
+    int32_t tile_rows;
     int4* tiles;
-    const int32_t *n_mtiles, *tile_expert, *mt_start, *pad_offsets, *counts;
+    int32_t* n_tiles;
+    const int32_t *tile_expert, *mt_start, *pad_offsets, *counts;
 };
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);

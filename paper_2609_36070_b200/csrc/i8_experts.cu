@@ -1,6 +1,6 @@
 // Routed expert FFNs in 8-bit integers: out[t] = add[t] + sum_s w[t, s] f_{idx[t, s]}(x[t]), every product with exact
 // integer sums and one scale per row and per channel.
-//   1. dispatch schedule (in one block, or the layer's own kernels)
+//   1. dispatch schedule (small batches: inside step 2; in one block; or the layer's own kernels)
 //   2. token rows -> codes: found once per token, written once per route, in expert order.  (Gathering the rows in the product
 //      instead, with gathering TMA loads of four rows, took 70 cycles per load and three times the product's own time.)
 //   3. gate/up product, h = silu(g) u in fp32
@@ -14,7 +14,7 @@ namespace mok {
 namespace i8 {
 
 constexpr int THREADS = 256;
-constexpr int ONE_BLOCK = 1024, ROUTES_PER_THREAD = 16;      // of the schedule in one block
+constexpr int ONE_BLOCK = 1024, ONE_BLOCK_ROUTES = 32768;    // of the schedule in one block
 constexpr long long GROUPED_ROWS = 112;                      // rows per expert up to which launch_grouped is the faster one
 
 // Rows of h (fp32) -> codes, one per route: route j's row is pos[j].  factor = scale * b_max / y_unit: what the combine
@@ -128,27 +128,26 @@ combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ fact
     *reinterpret_cast<uint4*>(out + t * ld_out + c * 8) = o;
 }
 
-// The schedule in one block, for batches of up to 16 thousand routes: the layer's own schedule keeps an expert's rows in route
-// order, which takes several passes (three launches); here a row's place inside its expert's segment is whatever an atomic
-// counter gives, because no result depends on it: every row is computed by itself, and the combine reads rows by `pos`.
+// The schedule in one block, for batches of up to ONE_BLOCK_ROUTES routes: the layer's own schedule keeps an expert's rows in
+// route order, which takes several passes (three launches); here a row's place inside its expert's segment is whatever an
+// atomic counter gives, because no result depends on it: every row is computed by itself, and the combine reads rows by `pos`.
+// Between the passes pos holds a route's place inside its expert.
 __global__ void __launch_bounds__(ONE_BLOCK)
-schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows,
-                    int32_t* __restrict__ pos, int4* __restrict__ tiles, WsHeader* __restrict__ hdr) {
+schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows, int32_t* pos, int4* __restrict__ tiles,
+                    int32_t* __restrict__ n_tiles) {
     __shared__ int32_t s_cnt[MAX_E], s_row0[MAX_E], s_pads[MAX_E / 32], s_tiles[MAX_E / 32];
+    constexpr int DEEP = 8;                      // routes on their way per thread
     pdl_enter();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     if (tid < MAX_E) s_cnt[tid] = 0;
     __syncthreads();
-    int e[ROUTES_PER_THREAD], rank[ROUTES_PER_THREAD];
+    for (int j0 = tid; j0 < n; j0 += ONE_BLOCK * DEEP) {
+        int e[DEEP];
 #pragma unroll
-    for (int i = 0; i < ROUTES_PER_THREAD; ++i) {
-        const int j = tid + i * ONE_BLOCK;
-        e[i] = j < n ? __ldg(idx + j) : -1;
-    }
+        for (int i = 0; i < DEEP; ++i) e[i] = j0 + i * ONE_BLOCK < n ? __ldg(idx + j0 + i * ONE_BLOCK) : -1;
 #pragma unroll
-    for (int i = 0; i < ROUTES_PER_THREAD; ++i) {
-        rank[i] = 0;
-        if ((unsigned)e[i] < (unsigned)E) rank[i] = atomicAdd(&s_cnt[e[i]], 1);
+        for (int i = 0; i < DEEP; ++i)
+            if ((unsigned)e[i] < (unsigned)E) pos[j0 + i * ONE_BLOCK] = atomicAdd(&s_cnt[e[i]], 1);
     }
     __syncthreads();
     int c = 0, pads = 0, mine = 0, pads_to = 0, tiles_to = 0;       // of expert tid; the sums run up to and including it
@@ -169,12 +168,21 @@ schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows
         const int pad0 = pads_to - pads, tile0 = tiles_to - mine;
         s_row0[tid] = pad0 * TILE_M;
         for (int q = 0; q < mine; ++q) tiles[tile0 + q] = make_int4(pad0 * TILE_M + q * tile_rows, c - q * tile_rows, tid, 0);
-        if (tid == MAX_E - 1) hdr->n_ftiles = tiles_to;
+        if (tid == MAX_E - 1) *n_tiles = tiles_to;
     }
     __syncthreads();
+    for (int j0 = tid; j0 < n; j0 += ONE_BLOCK * DEEP) {
+        int e[DEEP], place[DEEP];
 #pragma unroll
-    for (int i = 0; i < ROUTES_PER_THREAD; ++i)
-        if ((unsigned)e[i] < (unsigned)E) pos[tid + i * ONE_BLOCK] = s_row0[e[i]] + rank[i];
+        for (int i = 0; i < DEEP; ++i) {
+            const int j = j0 + i * ONE_BLOCK;
+            e[i] = j < n ? __ldg(idx + j) : -1;
+            place[i] = (unsigned)e[i] < (unsigned)E ? pos[j] : 0;
+        }
+#pragma unroll
+        for (int i = 0; i < DEEP; ++i)
+            if ((unsigned)e[i] < (unsigned)E) pos[j0 + i * ONE_BLOCK] = s_row0[e[i]] + place[i];
+    }
 }
 
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -205,7 +213,7 @@ static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) 
     // into the SMs, of which the pair tiles pull fewer per product.  Small tiles leave room for more stages, a tile too small
     // streams its expert's weights twice.
     X->grouped = R <= GROUPED_ROWS * (long long)E;
-    const bool any = R <= ONE_BLOCK * ROUTES_PER_THREAD;                 // (the layer's schedule knows tiles of 128 and 256 rows)
+    const bool any = R <= ONE_BLOCK_ROUTES;                 // (the layer's schedule knows tiles of 128 and 256 rows)
     X->tile_rows = !X->grouped ? 2 * TILE_M : any && R <= 32ll * E ? 64 : R <= 64ll * E ? TILE_M : any ? 192 : 2 * TILE_M;
     X->max_tiles = R / X->tile_rows + nonempty;
     X->pitch_h = pitch_of(H);
@@ -365,22 +373,23 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     if (e != cudaSuccess) return cuda_fail(e);
     auto table = [&](size_t at) { return reinterpret_cast<int32_t*>(ws + at); };
     int4* tiles = reinterpret_cast<int4*>(ws + X.tiles);
-    i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k, X.tile_rows};
-    if (X.L.R <= i8::ONE_BLOCK * i8::ROUTES_PER_THREAD) {
+    i8::RouteArgs routes = {a->topk_idx, table(X.L.pos), a->E, a->k, 0, X.tile_rows, tiles, &hdr->n_ftiles};
+    if (X.L.R <= i8::ROUTES_HERE) {
+        routes.n = X.L.R;
+    } else if (X.L.R <= i8::ONE_BLOCK_ROUTES) {
         e = launch_pdl(i8::schedule_one_kernel, dim3(1), dim3(i8::ONE_BLOCK), 0, s, a->topk_idx, X.L.R, a->E, X.tile_rows,
-                       table(X.L.pos), tiles, hdr);
-        g.n_mtiles = &hdr->n_ftiles;
+                       routes.pos, tiles, routes.n_tiles);
+        routes.tiles = nullptr;
     } else {
         e = launch_schedule(a->topk_idx, a->T, a->E, a->k, TILE_M, TILE_M, X.L, ws, nullptr, nullptr, nullptr, nullptr, s);
         const bool half = X.tile_rows == TILE_M;
-        g.n_mtiles = half ? &hdr->n_mtiles : &hdr->n_mtiles2;
-        routes.tiles = tiles;
-        routes.n_mtiles = g.n_mtiles;
+        routes.n_tiles = half ? &hdr->n_mtiles : &hdr->n_mtiles2;
         routes.tile_expert = table(half ? X.L.tile_expert : X.L.tile_expert2);
         routes.mt_start = table(half ? X.L.mt_start : X.L.mt_start2);
         routes.pad_offsets = table(X.L.pad_offsets);
         routes.counts = table(X.L.counts);
     }
+    g.n_mtiles = routes.n_tiles;
     if (e != cudaSuccess) return cuda_fail(e);
     e = i8::launch_quantize(a->x, a->type, a->T, a->H, a->x_stride, reinterpret_cast<int8_t*>(ws + X.xq), X.pitch_h,
                             reinterpret_cast<float*>(ws + X.xs), s, &routes);

@@ -23,13 +23,15 @@ __device__ __forceinline__ uint32_t row_max(uint32_t v, uint32_t* s_max) {
     return v;
 }
 
-// The rows that a quantised row is written to: itself, or with ROUTED one per routed slot of the token.
+// The rows that a quantised row is written to: itself, or with ROUTED one per routed slot of the token (here: their places in
+// shared memory, or NULL).
 template <bool ROUTED>
 struct Targets {
     long long first;
-    const int32_t *idx, *pos;
+    const int32_t *idx, *pos, *here;
     int E, n;
-    __device__ __forceinline__ Targets(long long r, const RouteArgs& q) : first(r), idx(nullptr), pos(nullptr), E(q.E), n(1) {
+    __device__ __forceinline__ Targets(long long r, const RouteArgs& q, const int32_t* places)
+        : first(r), idx(nullptr), pos(nullptr), here(places), E(q.E), n(1) {
         if (ROUTED) {
             n = q.k;
             idx = q.idx + r * q.k;
@@ -38,13 +40,70 @@ struct Targets {
     }
     __device__ __forceinline__ long long row(int s) const {          // -1: the slot is not routed
         if (!ROUTED) return first;
-        return (unsigned)__ldg(idx + s) < (unsigned)E ? (long long)__ldg(pos + s) : -1;
+        if (here) return here[s];
+        return (unsigned)__ldg(idx + s) < (unsigned)E ? (long long)pos[s] : -1;
     }
 };
 
+// The schedule of a small batch, in every block of the quantisation (one block per token) instead of a launch before it: the
+// counts of all experts, the starts of their segments, and the places of token r's rows (the routes of an expert in their
+// order).  Block 0 also writes the list of row tiles.
+template <int BLOCK>
+__device__ __forceinline__ void schedule_here(const RouteArgs& q, long long r, int32_t* s_place) {
+    constexpr int PER = MAX_E / BLOCK, WARPS = BLOCK / 32;           // experts per thread
+    __shared__ int32_t s_cnt[MAX_E], s_row0[MAX_E], s_sums[2][WARPS];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    for (int e = tid; e < MAX_E; e += BLOCK) s_cnt[e] = 0;
+    __syncthreads();
+    for (int j = tid; j < q.n; j += BLOCK) {
+        const int e = __ldg(q.idx + j);
+        if ((unsigned)e < (unsigned)q.E) atomicAdd(&s_cnt[e], 1);
+    }
+    __syncthreads();
+    int pads = 0, tiles = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int c = s_cnt[tid * PER + i];
+        pads += (c + TILE_M - 1) / TILE_M;
+        tiles += (c + q.tile_rows - 1) / q.tile_rows;
+    }
+    int pads_to = pads, tiles_to = tiles;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+        const int p = __shfl_up_sync(0xffffffffu, pads_to, off), t = __shfl_up_sync(0xffffffffu, tiles_to, off);
+        if (lane >= off) { pads_to += p; tiles_to += t; }
+    }
+    if (lane == 31) { s_sums[0][warp] = pads_to; s_sums[1][warp] = tiles_to; }
+    __syncthreads();
+    for (int w = 0; w < warp; ++w) { pads_to += s_sums[0][w]; tiles_to += s_sums[1][w]; }
+    int row0 = (pads_to - pads) * TILE_M, tile = tiles_to - tiles;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int e = tid * PER + i, c = s_cnt[e];
+        s_row0[e] = row0;
+        if (blockIdx.x == 0)
+            for (int m = 0; m < c; m += q.tile_rows) q.tiles[tile++] = make_int4(row0 + m, c - m, e, 0);
+        row0 += (c + TILE_M - 1) / TILE_M * TILE_M;
+    }
+    if (blockIdx.x == 0 && tid == BLOCK - 1) *q.n_tiles = tiles_to;
+    __syncthreads();
+    for (int s = warp; s < q.k; s += WARPS) {
+        const int j0 = (int)r * q.k + s, e = __ldg(q.idx + j0);
+        int before = 0;
+        for (int j = lane; j < j0; j += 32) before += __ldg(q.idx + j) == e ? 1 : 0;
+        before = __reduce_add_sync(0xffffffffu, before);
+        if (lane == 0) {
+            const bool routed = (unsigned)e < (unsigned)q.E;
+            s_place[s] = routed ? s_row0[e] + before : -1;
+            if (routed) q.pos[j0] = s_row0[e] + before;
+        }
+    }
+    __syncthreads();
+}
+
 // The row tiles of the experts' segments: {first row, rows of the segment from there on, expert, -}
 __device__ __forceinline__ void write_tiles(const RouteArgs& q) {
-    const int n = *q.n_mtiles;
+    const int n = *q.n_tiles;
     for (int i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
         const int e = q.tile_expert[i], m = i - q.mt_start[e];
         q.tiles[i] = make_int4(q.pad_offsets[e] + m * q.tile_rows, q.counts[e] - m * q.tile_rows, e, 0);
@@ -58,8 +117,9 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
                     float* __restrict__ scales, const RouteArgs routes) {
     constexpr int PER = 16 / sizeof(T);
     __shared__ uint32_t s_max[BLOCK / 32];
+    __shared__ int32_t s_place[ROUTED ? MAX_K : 1];
     pdl_enter();
-    if (ROUTED && routes.tiles) write_tiles(routes);
+    if (ROUTED && routes.n == 0 && routes.tiles) write_tiles(routes);
     const int sub = threadIdx.x % TPR, pieces = K / PER;
     constexpr int ROWS = BLOCK / TPR;
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < rows; r0 += (long long)gridDim.x * ROWS) {
@@ -73,6 +133,9 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
             const int c = sub + i * TPR;
             raw[i] = make_uint4(0u, 0u, 0u, 0u);
             if (live && c < pieces) raw[i] = __ldg(src + c);
+        }
+        if constexpr (ROUTED && TPR == BLOCK) {          // (while the row is on its way)
+            if (routes.n > 0) schedule_here<BLOCK>(routes, r, s_place);
         }
 #pragma unroll
         for (int i = 0; i < HELD; ++i) {
@@ -96,7 +159,7 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
             raw[i].x = o.x;
             raw[i].y = o.y;
         }
-        const Targets<ROUTED> to(r, routes);
+        const Targets<ROUTED> to(r, routes, ROUTED && routes.n > 0 ? s_place : nullptr);
         for (int s = 0; s < to.n; ++s) {
             const long long row = to.row(s);
             if (row < 0) continue;
@@ -120,17 +183,21 @@ __global__ void __launch_bounds__(THREADS)
 quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ldx, int8_t* __restrict__ codes, long long ldc,
                     float* __restrict__ scales, const RouteArgs routes) {
     __shared__ uint32_t s_max[THREADS / 32];
+    __shared__ int32_t s_place[ROUTED ? MAX_K : 1];
     pdl_enter();
-    if (ROUTED && routes.tiles) write_tiles(routes);
+    if (ROUTED && routes.n == 0 && routes.tiles) write_tiles(routes);
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const T* src = x + r * ldx;
+        if constexpr (ROUTED) {
+            if (routes.n > 0) schedule_here<THREADS>(routes, r, s_place);
+        }
         uint32_t m = 0;
         for (int c = threadIdx.x; c < K; c += THREADS) m = max(m, abs_bits(to_f(src[c])));
         m = row_max<THREADS, THREADS>(m, s_max);
         const float amax = __uint_as_float(m);
         const bool codable = m > 0 && finite_bits(m);
         const RowRule rule = row_rule(amax);
-        const Targets<ROUTED> to(r, routes);
+        const Targets<ROUTED> to(r, routes, ROUTED && routes.n > 0 ? s_place : nullptr);
         for (int s = 0; s < to.n; ++s) {
             const long long row = to.row(s);
             if (row < 0) continue;
