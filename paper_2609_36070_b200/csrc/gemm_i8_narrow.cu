@@ -21,7 +21,7 @@ using namespace tc;
 
 constexpr int NARROW_THREADS = 512, NARROW_WARPS = NARROW_THREADS / 32;
 constexpr int NARROW_STAGE = 128 * 128;          // 128 channels x 128 bytes of K
-constexpr int NARROW_MAX_STAGES = 10;
+constexpr int NARROW_MAX_STAGES = 12;
 constexpr int NARROW_SMEM = 232448;
 constexpr int NARROW_CTRL = 2048;                // barriers, row maxima and scales
 constexpr int NARROW_TOKENS = 256;               // most columns of the MMA
@@ -107,10 +107,14 @@ __device__ __forceinline__ void quantise_range(const NarrowArgs& a, int k0, int 
     __syncthreads();
     if (S > 1) {
         cluster_sync();                          // every CTA's maxima are complete
+        // eight threads per row, one for each CTA of the cluster: the reads go out together
+        static_assert(NARROW_THREADS == 8 * NARROW_HELD, "a thread for each row and CTA");
+        const int r = threadIdx.x >> 3, q = threadIdx.x & 7;
         uint32_t m = 0;
-        if ((int)threadIdx.x < a.M)
-            for (int q = 0; q < S; ++q) m = max(m, ld_cluster(smem_u32(&ctrl->amax[threadIdx.x]), (uint32_t)q));
-        if ((int)threadIdx.x < a.M) ctrl->top[threadIdx.x] = m;
+        if (r < a.M && q < S) m = ld_cluster(smem_u32(&ctrl->amax[r]), (uint32_t)q);
+#pragma unroll
+        for (int off = 1; off < 8; off <<= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, off));
+        if (r < a.M && q == 0) ctrl->top[r] = m;
     } else if ((int)threadIdx.x < a.M) {
         ctrl->top[threadIdx.x] = ctrl->amax[threadIdx.x];
     }
