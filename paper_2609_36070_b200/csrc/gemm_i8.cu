@@ -3,8 +3,9 @@
 //
 // Persistent, warp-specialised, on CTA pairs: the two CTAs of a cluster compute one 256 x 256 tile with cta_group::2 MMAs
 // issued by the even CTA.  Each CTA stages its own 128 rows of A and half of the 256 rows of B (128 bytes of K per stage, 32 KB,
-// six stages), so an SM pulls 32 KB for 256 cycles of MMA; a 128 x 256 tile of one CTA would pull 48 KB for them, and one-byte
-// operands are bound by that rate.
+// six stages), so an SM pulls 32 KB for 512 cycles of MMA; a 128 x 256 tile of one CTA would pull 48 KB for them, and with all
+// SMs at work that rate, some 45 bytes per cycle, is the limit.  The plain product also takes narrower tiles (down to 128
+// columns) where they spread the work better over the SMs.
 //   warp 0       TMA producer : A and B tiles (128-byte swizzle)
 //   warp 1       MMA issuer (even CTA)
 //   warps 2..9   epilogue     : warp w drains TMEM lane quadrant w % 4 and one half of the tile's columns
@@ -68,7 +69,7 @@ __device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
     return v;
 }
 
-struct PairTile { int row0, n, e, valid; };     // valid: rows of the segment from row0 on
+struct PairTile { int row0, n, e, valid; };     // n: column tile; valid: rows of the segment from row0 on
 
 __device__ __forceinline__ PairTile pair_tile(const ProductArgs& a, int L, int n_nt, int n_mt) {
     PairTile t;
@@ -184,6 +185,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = (int)cluster_ctarank();
     const int unit = blockIdx.x >> 1, n_units = gridDim.x >> 1;
+    const int bn = EPI == EPI_PLAIN ? a.bn : BN;                     // columns of a tile
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
@@ -223,7 +225,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             for (int L = unit; L < total; L += n_units) {
                 const PairTile t = next;
                 if (L + n_units < total) next = pair_tile(a, L + n_units, n_nt, n_mt);     // (on its way during this tile)
-                const int brow = GATED ? t.e * 2 * a.N + rank * a.N + t.n * (BN / 2) : t.e * a.N + t.n * BN + rank * (BN / 2);
+                const int brow = GATED ? t.e * 2 * a.N + rank * a.N + t.n * (BN / 2) : t.e * a.N + t.n * bn + rank * (bn / 2);
                 bool ok = true;
                 for (int kb = 0; kb < k_blocks; ++kb) {
                     ok = mbar_wait(smem_u32(&ctrl->empty[s]), ph ^ 1u, abort_flag, a.header, 1);
@@ -231,7 +233,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                     const uint32_t full = smem_u32(&ctrl->full[s]);
                     const uint32_t sa = base + s * STAGE_BYTES, sb = sa + A_BYTES;
                     // the even CTA's barrier collects the bytes of both CTAs of the pair
-                    if (rank == 0) mbar_expect_tx(full, 2 * STAGE_BYTES);
+                    if (rank == 0) mbar_expect_tx(full, 2 * A_BYTES + bn * BKB);
                     tma_load_2d_peer(sa, &tmapA, full, kb * BKB, t.row0 + rank * BM);
                     tma_load_2d_peer(sb, &tmapB, full, kb * BKB, brow);
                     if (++s == STAGES) { s = 0; ph ^= 1u; }
@@ -243,7 +245,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         if (lane == 0 && rank == 0) {
-            constexpr uint32_t idesc = make_idesc(2 * BM, BN);
+            const uint32_t idesc = make_idesc(2 * BM, bn);
             int s = 0, buf = 0;
             uint32_t ph = 0, aph = 0;
             for (int L = unit; L < total; L += n_units) {
@@ -286,7 +288,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             const int n_rows = min(32, t.valid - r0);
             // the row's scale and the warp's column scales, one column of each piece per lane, on their way while the
             // products finish
-            const int first = t.n * (GATED ? BN / 2 : BN) + half * 32 * CHUNKS;
+            const int first = t.n * (GATED ? BN / 2 : bn) + half * 32;           // pieces are dealt to the two halves in turn
             const float* bs = a.b_scale + (size_t)t.e * (GATED ? 2 : 1) * a.N;
             float rs = 0.f, unit_n = 1.f;
             if (EPI != EPI_HALF && lane < n_rows) rs = __ldg(a.a_scale + t.row0 + r0 + lane);
@@ -297,7 +299,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             float s0[CHUNKS], s1[CHUNKS];                            // s1: up scales, or the bias
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
-                const int n = first + c * 32 + lane;
+                const int n = first + c * 64 + lane;
                 s0[c] = n < a.N ? __ldg(bs + n) : 0.f;
                 s1[c] = 0.f;
                 if (GATED && n < a.N) s1[c] = __ldg(bs + a.N + n);
@@ -307,7 +309,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t taddr = tmem_base + (uint32_t)(buf * BN + half * 32 * CHUNKS) + ((uint32_t)(quad * 32) << 16);
+            const uint32_t taddr = tmem_base + (uint32_t)(buf * BN + half * 32) + ((uint32_t)(quad * 32) << 16);
             uint32_t acc[2][32], up[2][GATED ? 32 : 1];
             tc_ld32(taddr, acc[0]);
             if constexpr (GATED) tc_ld32(taddr + BN / 2, up[0]);
@@ -318,16 +320,16 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                 if (EPI != EPI_HALF) st_shared_f32(factors + 128 + lane * 4, s1[c]);
                 tc_wait_ld();
                 if (c + 1 < CHUNKS) {                                // the next piece comes while this one is worked on
-                    tc_ld32(taddr + (c + 1) * 32, acc[b ^ 1]);
-                    if constexpr (GATED) tc_ld32(taddr + BN / 2 + (c + 1) * 32, up[b ^ 1]);
+                    tc_ld32(taddr + (c + 1) * 64, acc[b ^ 1]);       // (columns past a narrow tile: never stored)
+                    if constexpr (GATED) tc_ld32(taddr + BN / 2 + (c + 1) * 64, up[b ^ 1]);
                     __syncwarp();
                 } else {                                             // the accumulator goes back before the last arithmetic
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive_remote(smem_u32(&ctrl->tempty[buf]), 0);
                 }
-                const int n0 = first + c * 32, n_cols = a.N - n0;    // first output column of the piece, and how many exist
-                if (n_rows > 0 && n_cols > 0) {
+                const int n0 = first + c * 64, n_cols = a.N - n0;    // first output column of the piece, and how many exist
+                if (n_rows > 0 && n_cols > 0 && (EPI != EPI_PLAIN || half * 32 + c * 64 < bn)) {
                     float v[32];
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
@@ -447,12 +449,31 @@ static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, con
     return cudaLaunchKernelEx(&cfg, kernel, mA, mB, mC, a, n_nt, k_blocks);
 }
 
+// Columns of a plain tile: those by which 74 pairs are done first.  A k-block of 128 bytes takes a pair two cycles per column on
+// the tensor cores; all pairs together bring some 7500 bytes per cycle into their SMs.  (600 tokens, 8192 x 8192: 192 columns
+// 52 us, 256 columns 58 us; 8192 tokens, 4096 x 7168: 256 columns.)
+static int pair_columns(int M, int N) {
+    int best = BN;
+    double least = 0;
+    for (int bn = BN; bn >= 128; bn -= 32) {
+        const long long tiles = (long long)((M + 2 * BM - 1) / (2 * BM)) * ((N + bn - 1) / bn), waves = (tiles + 73) / 74;
+        const double mma = (double)waves * 2 * bn, bytes = (double)tiles * 2 * (BM + bn / 2) * BKB / 7500;
+        const double c = mma > bytes ? mma : bytes;
+        if (bn == BN || c < least) {
+            least = c;
+            best = bn;
+        }
+    }
+    return best;
+}
+
 cudaError_t launch_product(const ProductArgs& args, int epi, cudaStream_t s) {
     ProductArgs a = args;
     const bool gated = epi == EPI_GATED;
+    a.bn = epi == EPI_PLAIN ? pair_columns(a.dense_rows, a.N) : BN;
     CUtensorMap mA, mB, mC;
     if (!byte_map(&mA, a.A, a.a_rows, a.K, a.lda, BM) ||
-        !byte_map(&mB, a.B, (long long)a.E * (gated ? 2 : 1) * a.N, a.K, a.ldb, BN / 2))
+        !byte_map(&mB, a.B, (long long)a.E * (gated ? 2 : 1) * a.N, a.K, a.ldb, (uint32_t)a.bn / 2))
         return cudaErrorInvalidValue;
     // C in boxes of 32 rows of 64 bytes, where its rows allow it
     const int type = gated ? MOK_TYPE_F32 : epi == EPI_HALF ? MOK_TYPE_F16 : a.c_type;
@@ -463,7 +484,7 @@ cudaError_t launch_product(const ProductArgs& args, int epi, cudaStream_t s) {
                               (uint64_t)(a.dense_rows > 0 ? a.dense_rows : a.a_rows), (uint64_t)a.N, a.ldc * size,
                               (uint32_t)(64 / size), 32, CU_TENSOR_MAP_SWIZZLE_64B))
         return cudaErrorInvalidValue;
-    const int n_nt = gated ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + BN - 1) / BN;
+    const int n_nt = gated ? (a.N + BN / 2 - 1) / (BN / 2) : (a.N + a.bn - 1) / a.bn;
     const int k_blocks = (a.K + BKB - 1) / BKB;
     const long long tiles = (a.dense_rows > 0 ? (a.dense_rows + 2 * BM - 1) / (2 * BM) : a.max_mt) * (long long)n_nt;
     if (tiles <= 0 || tiles > 0x7fffffffll) return cudaErrorInvalidValue;

@@ -85,6 +85,7 @@ struct ProductArgs {
     const int32_t* n_mtiles;     // how many
     int32_t max_mt;              // at most
     int32_t c_mapped;            // set by the launcher: C is stored through a tensor map
+    int32_t bn;                  // set by the launcher: columns of a plain tile
     WsHeader* header;
 };
 enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
