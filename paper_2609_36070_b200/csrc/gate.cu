@@ -513,12 +513,13 @@ struct BwdParams {
 // Only the last one is non-zero outside the chosen experts (and reads all logits).  1 - s is sigmoid(-l), without the
 // cancellation.  Four tokens per warp, eight lanes each, as in the forward kernel; a token's row is put together in shared
 // memory and written once, in 16-byte pieces.  Chosen ids outside 0 .. E-1 (routes that were dropped) have no part in it.
-// NI: pieces of four experts per lane, as in the forward kernel; 0 where only the chosen experts have a gradient.
-template <class L, int NI, bool VEC>
+// NI: pieces of four experts per lane, as in the forward kernel; 0 where only the chosen experts have a gradient.  SLOTS: of a
+// token's k routes per lane.
+template <class L, int NI, bool VEC, int SLOTS>
 __global__ void __launch_bounds__(32 * WARPS)
 gate_backward_kernel(const BwdParams p) {
     extern __shared__ __align__(16) float s_row[];   // [WARPS][4][E rounded up to 8], zero between tokens
-    constexpr int PER = 16 / sizeof(L), SLOTS = MAX_K / 8;
+    constexpr int PER = 16 / sizeof(L);
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 7, own = lane >> 3;
     const int E = p.E, k = p.k, pitch = (E + 7) & ~7;
@@ -675,25 +676,30 @@ static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
     return launch_pdl(gate_warp_kernel<L, 16>, grid, block, smem, s, p);
 }
 
-template <class L, int NI>
+template <class L, int NI, int SLOTS>
 static cudaError_t launch_backward_four(const BwdParams& p, cudaStream_t s) {
     const bool vec = p.E % 4 == 0 && (p.T == 1 || p.stride % 4 == 0) && (reinterpret_cast<uintptr_t>(p.logits) & (4 * sizeof(L) - 1)) == 0;
-    const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * 8;
-    const long long rounds = (units + wave - 1) / wave, blocks = (units + rounds - 1) / rounds;
+    // a block's chain of dependent loads is its time, so the blocks are many and short
+    const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), most = 148 * 64;
     const size_t smem = sizeof(float) * WARPS * 4 * ((p.E + 7) & ~7);
-    const dim3 grid((unsigned)blocks), block(32 * WARPS);
-    return NI > 0 && vec ? launch_pdl(gate_backward_kernel<L, NI, true>, grid, block, smem, s, p)
-                         : launch_pdl(gate_backward_kernel<L, NI, false>, grid, block, smem, s, p);
+    const dim3 grid((unsigned)(units < most ? units : most)), block(32 * WARPS);
+    return NI > 0 && vec ? launch_pdl(gate_backward_kernel<L, NI, true, SLOTS>, grid, block, smem, s, p)
+                         : launch_pdl(gate_backward_kernel<L, NI, false, SLOTS>, grid, block, smem, s, p);
+}
+
+template <class L, int SLOTS>
+static cudaError_t launch_backward_slots(const BwdParams& p, cudaStream_t s) {
+    if (!p.softmax || p.renormalise) return launch_backward_four<L, 0, SLOTS>(p, s);
+    const int n = (p.E + 31) / 32;
+    if (n <= 2) return launch_backward_four<L, 2, SLOTS>(p, s);
+    if (n <= 4) return launch_backward_four<L, 4, SLOTS>(p, s);
+    if (n <= 8) return launch_backward_four<L, 8, SLOTS>(p, s);
+    return launch_backward_four<L, 16, SLOTS>(p, s);
 }
 
 template <class L>
 static cudaError_t launch_backward(const BwdParams& p, cudaStream_t s) {
-    if (!p.softmax || p.renormalise) return launch_backward_four<L, 0>(p, s);
-    const int n = (p.E + 31) / 32;
-    if (n <= 2) return launch_backward_four<L, 2>(p, s);
-    if (n <= 4) return launch_backward_four<L, 4>(p, s);
-    if (n <= 8) return launch_backward_four<L, 8>(p, s);
-    return launch_backward_four<L, 16>(p, s);
+    return p.k <= 8 ? launch_backward_slots<L, 1>(p, s) : launch_backward_slots<L, MAX_K / 8>(p, s);
 }
 
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
