@@ -52,6 +52,17 @@ __device__ __forceinline__ float sigmoid_near(float l) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + exp2_near(-LOG2_E * l)));
     return r;
 }
+// 1 where a > b, to be summed by additions: those run beside the comparisons, and integer additions do not.
+__device__ __forceinline__ float one_if_above(float a, float b) {
+    float r;
+    asm("set.gt.f32.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// The next value below v, any but -inf and NaN.
+__device__ __forceinline__ float next_below(float v) {
+    const int u = __float_as_int(v);
+    return __int_as_float(v > 0.f ? u - 1 : v == 0.f ? (int)0x80000001u : u + 1);
+}
 // Keys that compare as the values do: absent or taken experts 0, NaN 1, then -inf ... +inf.  -0 counts as 0.
 __device__ __forceinline__ unsigned choice_key(float v) {
     if (v != v) return 1u;
@@ -249,13 +260,13 @@ constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOW
 template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      // shared memory of a warp
 
 // Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.
-constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 8 ? 5 : 2; }
+constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 6 ? 6 : NI <= 8 ? 5 : NI <= 12 ? 3 : 2; }
 
 // No groups, or groups of whole pieces of four experts: four tokens per warp.  NI pieces of four experts per lane (E <= 32 NI).
 template <class L, int NI, bool VEC>
 __global__ void __launch_bounds__(32 * WARPS, gate_blocks(NI))
 gate_kernel(const Params p) {
-    extern __shared__ __align__(16) float s_mem[];   // per warp: values [4][32 NI], chosen ids [4][MAX_K], lists [4][32][2]
+    extern __shared__ __align__(16) float s_mem[];   // per warp: values [4][32 NI], chosen ids [4][MAX_K], lists [4][2][32]
     pdl_enter();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane & 7, own = lane >> 3;
     const int E = p.E, k = p.k, G = p.n_groups;
@@ -266,13 +277,29 @@ gate_kernel(const Params p) {
     float* space = s_mem + (size_t)warp * GATE_FLOATS<NI>;
     float* vals = space + own * 32 * NI;
     int* chosen = reinterpret_cast<int*>(space + 4 * 32 * NI) + own * MAX_K;
-    float2* list = reinterpret_cast<float2*>(space + 4 * (32 * NI + MAX_K)) + own * 32;
+    float* list = space + 4 * (32 * NI + MAX_K) + own * 64;                             // the values in reach, and their ids
+    int* list_id = reinterpret_cast<int*>(list + 32);
     for (long long t0 = ((long long)blockIdx.x * WARPS + warp) * 4; t0 < p.T; t0 += (long long)gridDim.x * WARPS * 4) {
         const long long t = t0 + own < p.T ? t0 + own : p.T - 1;       // (past the end: the last token again, not written)
         const L* row = reinterpret_cast<const L*>(p.logits) + t * p.stride;
         float c[NI][4];
 #pragma unroll
         for (int i = 0; i < NI; ++i) load4<VEC>(row, (sub + 8 * i) * 4, E, c[i]);
+        // a sum that is finite holds no NaN and no infinity
+        auto finite = [&]() {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int e = (sub + 8 * i) * 4;
+                if (e + 3 < E) sum += (c[i][0] + c[i][1]) + (c[i][2] + c[i][3]);
+                else if (!VEC) {
+#pragma unroll
+                    for (int j = 0; j < 3; ++j) sum += e + j < E ? c[i][j] : 0.f;
+                }
+            }
+            return fabsf(sum) < INFINITY;
+        };
+        bool ordinary = finite();
         float m = -INFINITY, total = 1.f;
         if (p.softmax) {
 #pragma unroll
@@ -280,11 +307,17 @@ gate_kernel(const Params p) {
             m = max8(m);
         }
         if (full_sum) {
+            // (a term's error, 2^-22 of it and 2^-24 of its exponent, is below the sum's rounding)
+            const float from = m == -INFINITY ? 0.f : m;
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum += exp_below(c[i][j], m);
+                for (int j = 0; j < 4; ++j) {
+                    const float x = exp2_near((c[i][j] - from) * LOG2_E);
+                    sum += x;
+                    if (by_score) c[i][j] = x;
+                }
             sum = sum8(sum);
             total = m == -INFINITY ? 1.f : sum;
         }
@@ -297,31 +330,30 @@ gate_kernel(const Params p) {
                 if (p.bias) load4<VEC>(p.bias, e, E, b);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float s = p.softmax ? (m == -INFINITY ? 0.f : __expf(c[i][j] - m) * inv) : sigmoid_near(c[i][j]);
-                    // (absent, or not to be used whatever its bias)
-                    c[i][j] = c[i][j] == -INFINITY ? -INFINITY : p.bias ? s + b[j] : s;
+                    const float s = p.softmax ? c[i][j] * inv : sigmoid_near(c[i][j]);
+                    c[i][j] = p.bias ? s + b[j] : s;
                 }
             }
-        }
-        {   // a sum that is finite holds no NaN and no infinity
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                const int e = (sub + 8 * i) * 4;
-                if (e + 3 < E) sum += (c[i][0] + c[i][1]) + (c[i][2] + c[i][3]);
-                else if (!VEC) {
-#pragma unroll
-                    for (int j = 0; j < 3; ++j) sum += e + j < E ? c[i][j] : 0.f;
-                }
-            }
-            if (!(fabsf(sum) < INFINITY)) {
+            ordinary = ordinary && finite();
+            if (E < 32 * NI) {
 #pragma unroll
                 for (int i = 0; i < NI; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float v = c[i][j];
-                        c[i][j] = (sub + 8 * i) * 4 + j >= E ? -INFINITY : v != v ? AT_NAN : v == -INFINITY ? AT_MINUS_INF : fmaxf(v, AT_LOWEST);
-                    }
+                    for (int j = 0; j < 4; ++j)
+                        if ((sub + 8 * i) * 4 + j >= E) c[i][j] = -INFINITY;
+            }
+        }
+        if (!ordinary) {
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+                const int e = (sub + 8 * i) * 4;
+                float l[4];
+                load4<VEC>(row, e, E, l);            // (an expert masked by -inf is not to be used whatever its bias)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float v = l[j] == -INFINITY ? -INFINITY : c[i][j];
+                    c[i][j] = e + j >= E ? -INFINITY : v != v ? AT_NAN : v == -INFINITY ? AT_MINUS_INF : fmaxf(v, AT_LOWEST);
+                }
             }
         }
         float top[NI];                               // the largest value of each piece
@@ -330,15 +362,18 @@ gate_kernel(const Params p) {
             top[i] = fmaxf(fmaxf(c[i][0], c[i][1]), fmaxf(c[i][2], c[i][3]));
             *reinterpret_cast<float4*>(vals + (sub + 8 * i) * 4) = make_float4(c[i][0], c[i][1], c[i][2], c[i][3]);
         }
+        constexpr int WORDS = (NI + 7) / 8;          // of a bit per value
+        unsigned dropped[WORDS] = {};                // the values in groups left out
         if (G > 1) {
             // lane sub finds the two best of groups sub, sub + 8, ... from the values in shared memory; the lanes start at
             // different pieces, so that they do not meet in a bank.  Every group's value is then compared with all others.
             __syncwarp();
-            float* value = reinterpret_cast<float*>(list);
+            float* value = list;
             for (int g = sub; g < G; g += 8) {
                 const float4* mine = reinterpret_cast<const float4*>(vals) + g * per_group;
                 float b1 = -INFINITY, b2 = -INFINITY;
                 int at = sub < per_group ? sub : sub % per_group;
+#pragma unroll 4
                 for (int it = 0; it < per_group; ++it) {
                     const float4 f = mine[at];
                     at = at + 1 == per_group ? 0 : at + 1;
@@ -347,24 +382,28 @@ gate_kernel(const Params p) {
                     b2 = fmaxf(fmaxf(b2, second), fminf(b1, h));
                     b1 = fmaxf(b1, h);
                 }
-                value[g] = p.group_top == 2 ? b1 + b2 : b1;
+                value[g] = fmaxf(p.group_top == 2 ? b1 + b2 : b1, -FLT_MAX) + 0.f;      // (two AT_ values; no -0)
             }
             __syncwarp();
             unsigned kept = 0u;
             for (int g = sub; g < G; g += 8) {
-                const float v = value[g];
-                int rank = 0;
-                for (int q = 0; q < G; ++q) rank += (value[q] > v || (value[q] == v && q < g)) ? 1 : 0;
-                kept |= (rank < p.topk_groups ? 1u : 0u) << g;
+                const float v = value[g], below = next_below(v);
+                float rank = 0.f;
+#pragma unroll 4
+                for (int q = 0; q < G; ++q) rank += one_if_above(value[q], q < g ? below : v);      // (of equals the lower id)
+                kept |= (rank < (float)p.topk_groups ? 1u : 0u) << g;
             }
 #pragma unroll
             for (int off = 1; off < 8; off <<= 1) kept |= __shfl_xor_sync(0xffffffffu, kept, off);
 #pragma unroll
             for (int i = 0; i < NI; ++i)
-                if (!((kept >> ((unsigned)((sub + 8 * i) * group_magic) >> 16)) & 1u)) top[i] = -INFINITY;
+                if (!((kept >> ((unsigned)((sub + 8 * i) * group_magic) >> 16)) & 1u)) {
+                    top[i] = -INFINITY;
+                    dropped[i / 8] |= 0xfu << (4 * (i % 8));
+                }
         }
         __syncwarp();
-        bool listed = NI <= 8 && k > 4 && k <= 16;
+        bool listed = k > 4 && k <= 16;
         if (listed) {
             float h0, h1;                            // the lane's two half maxima
             if (NI == 1) {
@@ -374,30 +413,39 @@ gate_kernel(const Params p) {
                 h0 = top[0];
                 h1 = top[NI / 2];
 #pragma unroll
-                for (int i = 1; i < NI / 2; ++i) {
-                    h0 = fmaxf(h0, top[i]);
-                    h1 = fmaxf(h1, top[NI / 2 + i]);
-                }
+                for (int i = 1; i < NI / 2; ++i) h0 = fmaxf(h0, top[i]);
+#pragma unroll
+                for (int i = NI / 2 + 1; i < NI; ++i) h1 = fmaxf(h1, top[i]);
             }
-            int above0 = 0, above1 = 0;              // how many of the sixteen are larger
+            float above0 = 0.f, above1 = 0.f;        // how many of the sixteen are larger
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 const float o0 = __shfl_sync(0xffffffffu, h0, (lane & 24) + q), o1 = __shfl_sync(0xffffffffu, h1, (lane & 24) + q);
-                above0 += (o0 > h0 ? 1 : 0) + (o1 > h0 ? 1 : 0);
-                above1 += (o0 > h1 ? 1 : 0) + (o1 > h1 ? 1 : 0);
+                above0 += one_if_above(o0, h0) + one_if_above(o1, h0);
+                above1 += one_if_above(o0, h1) + one_if_above(o1, h1);
             }
-            float reach = fminf(above0 < k ? h0 : INFINITY, above1 < k ? h1 : INFINITY);
+            float reach = fminf(above0 < (float)k ? h0 : INFINITY, above1 < (float)k ? h1 : INFINITY);
 #pragma unroll
             for (int off = 1; off < 8; off <<= 1) reach = fminf(reach, __shfl_xor_sync(0xffffffffu, reach, off));
-            unsigned mask = 0u;                      // bit 4 i + j: value j of piece i
+            // bit 4 i + j of the words: value j of piece i.  The sign of a difference is shifted in, one comparison's work for
+            // two; the difference of equal infinities, NaN, has none (+inf; with -inf there is no list).
+            unsigned mask[WORDS];
+            int mine = 0;
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                if (NI <= 8 && top[i] >= reach) {    // (pieces of other groups have lost their maximum)
+            for (int w = 0; w < WORDS; ++w) {
+                constexpr unsigned ALL = 0xffffffffu;
+                const int pieces = NI - 8 * w < 8 ? NI - 8 * w : 8;
+                mask[w] = 0u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) mask |= (c[i][j] >= reach ? 1u : 0u) << (4 * i + j);
-                }
+                for (int i = 7; i >= 0; --i)
+                    if (i < pieces) {
+#pragma unroll
+                        for (int j = 3; j >= 0; --j)
+                            mask[w] = __funnelshift_l(__float_as_uint(c[(8 * w + i) % NI][j] - reach), mask[w], 1);
+                    }
+                mask[w] = ~mask[w] & ~dropped[w] & (ALL >> (32 - 4 * pieces));
+                mine += __popc(mask[w]);
             }
-            const int mine = __popc(mask);
             int upto = mine;
 #pragma unroll
             for (int off = 1; off < 8; off <<= 1) {
@@ -410,27 +458,52 @@ gate_kernel(const Params p) {
             listed = __all_sync(0xffffffffu, listed);
             if (listed) {
                 int at = upto - mine;
-                while (mask) {
-                    const int b = __ffs(mask) - 1, e = (sub + 8 * (b >> 2)) * 4 + (b & 3);
-                    mask &= mask - 1;
-                    list[at++] = make_float2(vals[e], __int_as_float(e));
-                }
-                for (int q = sub; q < most; q += 8)
-                    if (q >= n) list[q] = make_float2(-INFINITY, 0.f);
-                __syncwarp();
-                for (int q0 = 0; q0 < most; q0 += 16) {      // two values per lane
-                    const float2 a = q0 + sub < n ? list[q0 + sub] : make_float2(-INFINITY, 0.f);
-                    const float2 b = q0 + 8 + sub < n ? list[q0 + 8 + sub] : make_float2(-INFINITY, 0.f);
-                    const int ia = __float_as_int(a.y), ib = __float_as_int(b.y);
-                    int ra = 0, rb = 0;
-                    for (int x = 0; x < most; ++x) {
-                        const float2 o = list[x];
-                        const int io = __float_as_int(o.y);
-                        ra += (o.x > a.x || (o.x == a.x && io < ia)) ? 1 : 0;
-                        rb += (o.x > b.x || (o.x == b.x && io < ib)) ? 1 : 0;
+#pragma unroll
+                for (int w = 0; w < WORDS; ++w)
+                    while (mask[w]) {
+                        const int b = __ffs(mask[w]) - 1, e = (sub + 8 * (8 * w + (b >> 2))) * 4 + (b & 3);
+                        mask[w] &= mask[w] - 1;
+                        list[at] = vals[e];
+                        list_id[at++] = e;
                     }
-                    if (q0 + sub < n && ra < k) chosen[ra] = ia;
-                    if (q0 + 8 + sub < n && rb < k) chosen[rb] = ib;
+                for (int q = n + sub; q < ((most + 3) & ~3); q += 8) list[q] = -INFINITY;
+                __syncwarp();
+                // The values alone give each its place, unless two are equal; then the places, which should be 0 .. n - 1, add
+                // up to less.  Of 16-bit logits without a bias some mostly are.
+                bool equals = sizeof(L) == 2 && !p.bias;
+                if (!equals) {
+                    float places = 0.f;
+                    for (int q0 = 0; q0 < most; q0 += 16) {  // two values per lane
+                        const bool is_a = q0 + sub < n, is_b = q0 + 8 + sub < n;
+                        const float a = is_a ? list[q0 + sub] : INFINITY, b = is_b ? list[q0 + 8 + sub] : INFINITY;
+                        float ra = 0.f, rb = 0.f;
+                        for (int x = 0; x < most; x += 4) {
+                            const float4 o = *reinterpret_cast<const float4*>(list + x);
+                            ra += (one_if_above(o.x, a) + one_if_above(o.y, a)) + (one_if_above(o.z, a) + one_if_above(o.w, a));
+                            rb += (one_if_above(o.x, b) + one_if_above(o.y, b)) + (one_if_above(o.z, b) + one_if_above(o.w, b));
+                        }
+                        places += ra + rb;                   // (none is above infinity)
+                        if (is_a && ra < (float)k) chosen[(int)ra] = list_id[q0 + sub];
+                        if (is_b && rb < (float)k) chosen[(int)rb] = list_id[q0 + 8 + sub];
+                    }
+                    equals = __any_sync(0xffffffffu, sum8(places) != (float)(n * (n - 1) / 2));
+                }
+                if (equals) {
+                    __syncwarp();
+                    for (int q0 = 0; q0 < most; q0 += 16) {
+                        const bool is_a = q0 + sub < n, is_b = q0 + 8 + sub < n;
+                        const float a = is_a ? list[q0 + sub] : INFINITY, b = is_b ? list[q0 + 8 + sub] : INFINITY;
+                        const int ia = is_a ? list_id[q0 + sub] : 0, ib = is_b ? list_id[q0 + 8 + sub] : 0;
+                        int ra = 0, rb = 0;
+                        for (int x = 0; x < n; ++x) {
+                            const float o = list[x];
+                            const int io = list_id[x];
+                            ra += (o > a || (o == a && io < ia)) ? 1 : 0;
+                            rb += (o > b || (o == b && io < ib)) ? 1 : 0;
+                        }
+                        if (is_a && ra < k) chosen[ra] = ia;
+                        if (is_b && rb < k) chosen[rb] = ib;
+                    }
                 }
             }
         }
@@ -662,7 +735,9 @@ static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
         if (n <= 1) return launch_four<L, 1>(p, s);
         if (n <= 2) return launch_four<L, 2>(p, s);
         if (n <= 4) return launch_four<L, 4>(p, s);
+        if (n <= 6) return launch_four<L, 6>(p, s);
         if (n <= 8) return launch_four<L, 8>(p, s);
+        if (n <= 12) return launch_four<L, 12>(p, s);
         return launch_four<L, 16>(p, s);
     }
     long long blocks = ((long long)p.T + WARPS - 1) / WARPS;
