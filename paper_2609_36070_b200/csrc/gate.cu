@@ -722,7 +722,7 @@ static cudaError_t launch_four(const Params& p, cudaStream_t s) {
                      (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0;
     // one wave of blocks with the same number of rounds each
     const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * gate_blocks(NI);
-    const long long rounds = (units + wave - 1) / wave, blocks = (units + rounds - 1) / rounds;
+    const long long blocks = units < wave ? units : wave;
     const size_t smem = sizeof(float) * WARPS * GATE_FLOATS<NI>;
     const dim3 grid((unsigned)blocks), block(32 * WARPS);
     return vec ? launch_pdl(gate_kernel<L, NI, true>, grid, block, smem, s, p) : launch_pdl(gate_kernel<L, NI, false>, grid, block, smem, s, p);
