@@ -13,7 +13,7 @@
 // memory traffic), so the common case, no groups or groups of a multiple of four experts, puts FOUR tokens into a warp,
 // eight lanes each: every step across lanes then serves four tokens.  Lane p of a token holds pieces p, p + 8, ... of four
 // consecutive experts and the largest value of each piece.  Two ways to the k largest:
-//   - lists (k = 5 .. 16): the k-th largest of the sixteen half-lane maxima is a lower bound of the k-th largest value; the
+//   - lists (k = 5 .. 16): the k-th largest of the lanes' two largest piece maxima is a lower bound of the k-th largest value; the
 //     values that reach it, a few more than k, are listed in shared memory, and a value's place is the number of listed
 //     values before it.
 //   - rounds (small k, where they are cheaper; large k; and tokens with more than 32 values in reach, which equal values can
@@ -62,6 +62,11 @@ __device__ __forceinline__ float one_if_above(float a, float b) {
 __device__ __forceinline__ float next_below(float v) {
     const int u = __float_as_int(v);
     return __int_as_float(v > 0.f ? u - 1 : v == 0.f ? (int)0x80000001u : u + 1);
+}
+// For a 16-bit logit, whose last bits are free in fp32: expert e's place there sorts equals by their ids.  Finite v.
+__device__ __forceinline__ float with_id(float v, int e) {
+    const unsigned u = __float_as_uint(v + 0.f);
+    return __uint_as_float(u | (unsigned)((u >> 31) ? e : MAX_E - 1 - e));
 }
 // Keys that compare as the values do: absent or taken experts 0, NaN 1, then -inf ... +inf.  -0 counts as 0.
 __device__ __forceinline__ unsigned choice_key(float v) {
@@ -405,17 +410,13 @@ gate_kernel(const Params p) {
         __syncwarp();
         bool listed = k > 4 && k <= 16;
         if (listed) {
-            float h0, h1;                            // the lane's two half maxima
-            if (NI == 1) {
-                h0 = fmaxf(c[0][0], c[0][1]);
-                h1 = fmaxf(c[0][2], c[0][3]);
-            } else {
-                h0 = top[0];
-                h1 = top[NI / 2];
+            float h0 = top[0], h1 = -INFINITY;       // the two largest maxima of the lane's pieces
+            if (NI == 1 && h0 > -INFINITY)           // (or values of its only one)
+                h1 = fmaxf(fminf(fmaxf(c[0][0], c[0][1]), fmaxf(c[0][2], c[0][3])), fmaxf(fminf(c[0][0], c[0][1]), fminf(c[0][2], c[0][3])));
 #pragma unroll
-                for (int i = 1; i < NI / 2; ++i) h0 = fmaxf(h0, top[i]);
-#pragma unroll
-                for (int i = NI / 2 + 1; i < NI; ++i) h1 = fmaxf(h1, top[i]);
+            for (int i = 1; i < NI; ++i) {
+                h1 = fmaxf(h1, fminf(h0, top[i]));
+                h0 = fmaxf(h0, top[i]);
             }
             float above0 = 0.f, above1 = 0.f;        // how many of the sixteen are larger
 #pragma unroll
@@ -457,20 +458,21 @@ gate_kernel(const Params p) {
             listed = most <= 32 && reach > -INFINITY && __all_sync(0xffffffffu, n >= k);
             listed = __all_sync(0xffffffffu, listed);
             if (listed) {
+                const bool keyed = sizeof(L) == 2 && !by_score && __all_sync(0xffffffffu, ordinary);
                 int at = upto - mine;
 #pragma unroll
                 for (int w = 0; w < WORDS; ++w)
                     while (mask[w]) {
                         const int b = __ffs(mask[w]) - 1, e = (sub + 8 * (8 * w + (b >> 2))) * 4 + (b & 3);
                         mask[w] &= mask[w] - 1;
-                        list[at] = vals[e];
+                        list[at] = keyed ? with_id(vals[e], e) : vals[e];
                         list_id[at++] = e;
                     }
                 for (int q = n + sub; q < ((most + 3) & ~3); q += 8) list[q] = -INFINITY;
                 __syncwarp();
                 // The values alone give each its place, unless two are equal; then the places, which should be 0 .. n - 1, add
-                // up to less.  Of 16-bit logits without a bias some mostly are.
-                bool equals = sizeof(L) == 2 && !p.bias;
+                // up to less.  Of scores of 16-bit logits without a bias some mostly are.
+                bool equals = sizeof(L) == 2 && !p.bias && !keyed;
                 if (!equals) {
                     float places = 0.f;
                     for (int q0 = 0; q0 < most; q0 += 16) {  // two values per lane
