@@ -19,8 +19,10 @@
 //   - rounds (small k, where they are cheaper; large k; and tokens with more than 32 values in reach, which equal values can
 //     bring): a maximum over the lane's pieces, three shuffles across the eight lanes, and a refill of the one piece that
 //     lost its largest value.
-// 260 instructions per token (256 experts, k = 8; 440 with groups and a bias) against 610 (1300) with a warp per token: 14 (24)
-// us for 32768 tokens against 25 (53).  Other groupings, and batches that do not fill the GPU (up to some 2300 tokens: 4.7
+// 214 instructions per token (256 experts, k = 8; 379 with groups and a bias) against 610 (1300) with a warp per token: 11.5
+// (19.4) us for 32768 tokens against 25 (53).  Issue slots are 55 % used, the pipe of comparisons 45 %; the rest is the latency of
+// its steps, with the 20 warps per SM that the registers allow (more warps and spilled values, or the next rows copied ahead
+// into shared memory, were 5 % slower).  Other groupings, and batches that do not fill the GPU (up to some 2300 tokens: 4.7
 // against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
 #include "mok_internal.cuh"
 #include <cuda_fp16.h>
@@ -264,8 +266,10 @@ constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOW
 
 template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      // shared memory of a warp
 
-// Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.
-constexpr int gate_blocks(int NI) { return NI <= 4 ? 8 : NI <= 6 ? 6 : NI <= 8 ? 5 : NI <= 12 ? 3 : 2; }
+// Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.  (7 of the small ones, not 8:
+// 32768 tokens of 128 experts 9.5 -> 8.6 us, 8192 of 64 5.0 -> 3.8, 40000 of 30 8.2 -> 9.2; 5 for NI = 8, not 4 or 6: 19.4 against
+// 21.3 and 20.5.)
+constexpr int gate_blocks(int NI) { return NI <= 4 ? 7 : NI <= 6 ? 6 : NI <= 8 ? 5 : NI <= 12 ? 3 : 2; }
 
 // No groups, or groups of whole pieces of four experts: four tokens per warp.  NI pieces of four experts per lane (E <= 32 NI).
 template <class L, int NI, bool VEC>
