@@ -592,11 +592,11 @@ struct BwdParams {
 // Only the last one is non-zero outside the chosen experts (and reads all logits).  1 - s is sigmoid(-l), without the
 // cancellation.  Four tokens per warp, eight lanes each, as in the forward kernel; a token's row is put together in shared
 // memory and written once, in 16-byte pieces.  Chosen ids outside 0 .. E-1 (routes that were dropped) have no part in it.
-// NI: pieces of four experts per lane, as in the forward kernel; 0 where only the chosen experts have a gradient.  SLOTS: of a
-// token's k routes per lane.
-template <class L, int NI, bool VEC, int SLOTS>
+// NI: pieces of four experts per lane, as in the forward kernel; 0 where only the chosen experts have a gradient.
+template <class L, int NI, bool VEC>
 __global__ void __launch_bounds__(32 * WARPS)
 gate_backward_kernel(const BwdParams p) {
+    constexpr int SLOTS = MAX_K / 8;                 // of a token's k routes per lane
     extern __shared__ __align__(16) float s_row[];   // [WARPS][4][E rounded up to 8], zero between tokens
     constexpr int PER = 16 / sizeof(L);
     pdl_enter();
@@ -665,7 +665,7 @@ gate_backward_kernel(const BwdParams p) {
                         store_f(v + j + 2, f.z);
                         store_f(v + j + 3, f.w);
                     }
-                    *reinterpret_cast<uint4*>(out + i * PER) = o;
+                    __stcs(reinterpret_cast<uint4*>(out + i * PER), o);
                 }
             } else {
                 for (int i = sub; i < E; i += 8) store_f(out + i, mine[i]);
@@ -726,7 +726,7 @@ template <class L, int NI>
 static cudaError_t launch_four(const Params& p, cudaStream_t s) {
     const bool vec = p.E % 4 == 0 && (p.T == 1 || p.stride % 4 == 0) && (reinterpret_cast<uintptr_t>(p.logits) & (4 * sizeof(L) - 1)) == 0 &&
                      (reinterpret_cast<uintptr_t>(p.bias) & 15u) == 0;
-    // one wave of blocks with the same number of rounds each
+    // one wave of blocks
     const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), wave = 148 * gate_blocks(NI);
     const long long blocks = units < wave ? units : wave;
     const size_t smem = sizeof(float) * WARPS * GATE_FLOATS<NI>;
@@ -757,30 +757,28 @@ static cudaError_t launch_gate(const Params& p, cudaStream_t s) {
     return launch_pdl(gate_warp_kernel<L, 16>, grid, block, smem, s, p);
 }
 
-template <class L, int NI, int SLOTS>
+template <class L, int NI>
 static cudaError_t launch_backward_four(const BwdParams& p, cudaStream_t s) {
     const bool vec = p.E % 4 == 0 && (p.T == 1 || p.stride % 4 == 0) && (reinterpret_cast<uintptr_t>(p.logits) & (4 * sizeof(L) - 1)) == 0;
-    // a block's chain of dependent loads is its time, so the blocks are many and short
+    // A block's chain of dependent loads is its time, so the blocks are many and short.  The rows are written past the caches'
+    // usual order: where they and the logits exceed L2 the next loads do not wait for them to be evicted (32768 tokens of 256
+    // experts, sigmoid, inputs and outputs beyond L2: 11.0 us; two rounds of blocks and plain stores 12.0; one slot per lane for
+    // small k, which leaves more room on an SM, 12.3: the next call's blocks then crowd on the SMs that are done first).
     const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), most = 148 * 64;
     const size_t smem = sizeof(float) * WARPS * 4 * ((p.E + 7) & ~7);
     const dim3 grid((unsigned)(units < most ? units : most)), block(32 * WARPS);
-    return NI > 0 && vec ? launch_pdl(gate_backward_kernel<L, NI, true, SLOTS>, grid, block, smem, s, p)
-                         : launch_pdl(gate_backward_kernel<L, NI, false, SLOTS>, grid, block, smem, s, p);
-}
-
-template <class L, int SLOTS>
-static cudaError_t launch_backward_slots(const BwdParams& p, cudaStream_t s) {
-    if (!p.softmax || p.renormalise) return launch_backward_four<L, 0, SLOTS>(p, s);
-    const int n = (p.E + 31) / 32;
-    if (n <= 2) return launch_backward_four<L, 2, SLOTS>(p, s);
-    if (n <= 4) return launch_backward_four<L, 4, SLOTS>(p, s);
-    if (n <= 8) return launch_backward_four<L, 8, SLOTS>(p, s);
-    return launch_backward_four<L, 16, SLOTS>(p, s);
+    return NI > 0 && vec ? launch_pdl(gate_backward_kernel<L, NI, true>, grid, block, smem, s, p)
+                         : launch_pdl(gate_backward_kernel<L, NI, false>, grid, block, smem, s, p);
 }
 
 template <class L>
 static cudaError_t launch_backward(const BwdParams& p, cudaStream_t s) {
-    return p.k <= 8 ? launch_backward_slots<L, 1>(p, s) : launch_backward_slots<L, MAX_K / 8>(p, s);
+    if (!p.softmax || p.renormalise) return launch_backward_four<L, 0>(p, s);
+    const int n = (p.E + 31) / 32;
+    if (n <= 2) return launch_backward_four<L, 2>(p, s);
+    if (n <= 4) return launch_backward_four<L, 4>(p, s);
+    if (n <= 8) return launch_backward_four<L, 8>(p, s);
+    return launch_backward_four<L, 16>(p, s);
 }
 
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
