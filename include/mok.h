@@ -569,7 +569,8 @@ int mok_i8_linear(const mok_i8_linear_args* args);
 /*
  * The routed experts of the layer on 8-bit operands, from given routes:
  *     out[t] = add[t] + sum_s topk_w[t, s] f_{topk_idx[t, s]}(x[t]),   f_e(x) = W_down_e (silu(W_gate_e x) .* (W_up_e x))
- * x and the gated activation are quantised per token row as above.  Slots whose id is outside 0 .. E-1 are not routed (a
+ * x and the gated activation are quantised per token row as above; everything between the products is fp32, and an output is
+ * rounded once, to type.  Slots whose id is outside 0 .. E-1 are not routed (a
  * device that holds some of the experts passes ids relative to its first one).  Deterministic: fixed slot order, no atomics.
  * H and I multiples of 8, I <= 16384; limits of the layer otherwise.
  */
@@ -581,7 +582,8 @@ typedef struct mok_i8_experts_args {
     const float* gate_up_scales;             /* fp32 [E, 2I] */
     const int8_t* down_codes;                /* [E, H, I], rows down_stride bytes apart */
     const float* down_scales;                /* fp32 [E, H] */
-    const float* down_max;                   /* fp32 [E]: the largest down_scales of each expert */
+    const float* down_max;                   /* fp32 [E]: the largest down_scales of each expert (has to be there; the rows
+                                                between the products and the combine are fp32, so nothing is put in its unit) */
     const void* add;                         /* [T, H] of type (a shared expert's output), or NULL */
     int64_t x_stride, gate_up_stride, down_stride, add_stride, out_stride;
     int32_t T, H, I, E, k;

@@ -15,9 +15,9 @@
 //   EPI_GATED : B tile = 128 gate rows (even CTA) + the matching 128 up rows (odd CTA); h = silu(g) u in fp32 -> C fp32.  h is
 //               quantised by a pass of its own, since its row maximum spans all N tiles; fp32 because a rounding before the
 //               quantisation moves codes (bf16 moves one code in twenty).
-//   EPI_HALF  : C = fp16(sum * y_unit * b_scale[n] / b_max): the sums in the unit of the row, at most 65504 by construction
-//               (|sum| <= 127 * 127 * K, y_unit a power of two), so that the combine can read two bytes per value with
-//               eleven significant bits and put the row's factor a_scale * b_max / y_unit on in fp32.
+//   EPI_ROWS  : C = b_scale[n] * sum as fp32, whatever the type of the layer's output: the combine puts a row's scale on with
+//               its weight, adds up a token's rows in fp32 and rounds once.  (16-bit rows would spare half of the path's largest stream, but round every row a second
+//               time, and a common unit for them loses the channels whose scales are far below their matrix's largest.)
 // K, N and the rows may be ragged: TMA fills bytes past K and rows past the tensor with zeros, stores are masked.
 // All mbarrier waits are bounded; on a timeout the CTA records MOK_ERR_TIMEOUT and leaves cleanly.
 #include "i8_common.cuh"
@@ -290,12 +290,8 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
             // products finish
             const int first = t.n * (GATED ? BN / 2 : bn) + half * 32;           // pieces are dealt to the two halves in turn
             const float* bs = a.b_scale + (size_t)t.e * (GATED ? 2 : 1) * a.N;
-            float rs = 0.f, unit_n = 1.f;
-            if (EPI != EPI_HALF && lane < n_rows) rs = __ldg(a.a_scale + t.row0 + r0 + lane);
-            if constexpr (EPI == EPI_HALF) {
-                const float top = __ldg(a.b_max + t.e);
-                unit_n = top > 0.f ? a.y_unit / top : 0.f;
-            }
+            float rs = 0.f;
+            if (EPI != EPI_ROWS && lane < n_rows) rs = __ldg(a.a_scale + t.row0 + r0 + lane);
             float s0[CHUNKS], s1[CHUNKS];                            // s1: up scales, or the bias
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
@@ -316,8 +312,8 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
 #pragma unroll
             for (int c = 0; c < CHUNKS; ++c) {
                 const int b = c & 1;
-                st_shared_f32(factors + lane * 4, EPI == EPI_HALF ? s0[c] * unit_n : s0[c]);
-                if (EPI != EPI_HALF) st_shared_f32(factors + 128 + lane * 4, s1[c]);
+                st_shared_f32(factors + lane * 4, s0[c]);
+                if (EPI != EPI_ROWS) st_shared_f32(factors + 128 + lane * 4, s1[c]);
                 tc_wait_ld();
                 if (c + 1 < CHUNKS) {                                // the next piece comes while this one is worked on
                     tc_ld32(taddr + (c + 1) * 64, acc[b ^ 1]);       // (columns past a narrow tile: never stored)
@@ -335,7 +331,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                     for (int i = 0; i < 32; i += 4) {
                         const float4 f = ld_shared_f4(factors + i * 4);
                         const float fs[4] = {f.x, f.y, f.z, f.w};
-                        if constexpr (EPI == EPI_HALF) {
+                        if constexpr (EPI == EPI_ROWS) {
 #pragma unroll
                             for (int j = 0; j < 4; ++j) v[i + j] = (float)(int)acc[b][i + j] * fs[j];
                         } else {
@@ -351,10 +347,8 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
                     }
                     const int row = t.row0 + r0;
                     // (grouped rows are stored in whole blocks of 32: what follows a segment's last row is its own padding)
-                    if constexpr (GATED) {
+                    if constexpr (EPI != EPI_PLAIN) {
                         store_tile<float>(v, &tmapC, slabs, flip, n0, row, lane);
-                    } else if constexpr (EPI == EPI_HALF) {
-                        store_tile<__half>(v, &tmapC, slabs, flip, n0, row, lane);
                     } else if (a.c_mapped) {
                         if (a.c_type == MOK_TYPE_F32) store_tile<float>(v, &tmapC, slabs, flip, n0, row, lane);
                         else if (a.c_type == MOK_TYPE_F16) store_tile<__half>(v, &tmapC, slabs, flip, n0, row, lane);
@@ -476,7 +470,7 @@ cudaError_t launch_product(const ProductArgs& args, int epi, cudaStream_t s) {
         !byte_map(&mB, a.B, (long long)a.E * (gated ? 2 : 1) * a.N, a.K, a.ldb, (uint32_t)a.bn / 2))
         return cudaErrorInvalidValue;
     // C in boxes of 32 rows of 64 bytes, where its rows allow it
-    const int type = gated ? MOK_TYPE_F32 : epi == EPI_HALF ? MOK_TYPE_F16 : a.c_type;
+    const int type = epi == EPI_PLAIN ? a.c_type : MOK_TYPE_F32;
     const uint64_t size = type_bytes(type);
     a.c_mapped = (reinterpret_cast<uintptr_t>(a.C) & 15u) == 0 && (a.ldc * size) % 16 == 0;
     if (!a.c_mapped) mC = mA;
@@ -490,7 +484,7 @@ cudaError_t launch_product(const ProductArgs& args, int epi, cudaStream_t s) {
     if (tiles <= 0 || tiles > 0x7fffffffll) return cudaErrorInvalidValue;
     if (epi == EPI_PLAIN) return launch_pair<EPI_PLAIN>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
     if (gated) return launch_pair<EPI_GATED>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
-    return launch_pair<EPI_HALF>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
+    return launch_pair<EPI_ROWS>(mA, mB, mC, a, n_nt, k_blocks, tiles, s);
 }
 
 }  // namespace i8

@@ -10,7 +10,7 @@
 //   warps 2..9   epilogue: lane = channel, so that stores are coalesced as they are
 //   EPI_GATED : the M side holds 64 gate rows and the 64 matching up rows; the warps of the up lanes hand their values over
 //               through shared memory, those of the gate lanes write h = silu(g) u as fp32
-//   EPI_HALF  : fp16 in the unit of the row (see gemm_i8.cu)
+//   EPI_ROWS  : sums times the channel's scale, as fp32 (see gemm_i8.cu)
 // All mbarrier waits are bounded; on a timeout the CTA records MOK_ERR_TIMEOUT and leaves cleanly.
 #include "i8_common.cuh"
 #include "i8_ptx.cuh"
@@ -167,10 +167,6 @@ product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_c
             const bool there = n < a.N;
             float f = 0.f;
             if (there) f = GATED ? __ldg(a.b_scale + ((size_t)t.e * 2 + (quad >> 1)) * a.N + n) : __ldg(a.b_scale + (size_t)t.e * a.N + n);
-            if (!GATED) {
-                const float top = __ldg(a.b_max + t.e);
-                f *= top > 0.f ? a.y_unit / top : 0.f;
-            }
             float xs[ROWS / 32];                           // lane l: scale of the tile's rows l, l + 32, ...
             if (GATED) {
 #pragma unroll
@@ -217,10 +213,10 @@ product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_c
                     flip ^= 1;
                     xph ^= flip ^ 1;                         // (both buffers have been used once more)
                 } else if (there) {
-                    __half* dst = reinterpret_cast<__half*>(a.C) + (long long)(t.row0 + c) * a.ldc + n;
+                    float* dst = reinterpret_cast<float*>(a.C) + (long long)(t.row0 + c) * a.ldc + n;
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
-                        if (c + j < t.valid) dst[j * a.ldc] = __float2half_rn((float)(int)acc[j] * f);
+                        if (c + j < t.valid) dst[j * a.ldc] = (float)(int)acc[j] * f;
                 }
             }
             if (!__all_sync(0xffffffffu, ok)) break;
@@ -276,16 +272,16 @@ cudaError_t launch_grouped(const ProductArgs& a, int epi, cudaStream_t s) {
     if (tiles <= 0 || tiles > 0x7fffffffll) return cudaErrorInvalidValue;
     if (a.tile_rows == 64)
         return is_gated ? launch_grouped_epi<EPI_GATED, 64>(mW, mX, a, n_nt, k_blocks, tiles, s)
-                        : launch_grouped_epi<EPI_HALF, 64>(mW, mX, a, n_nt, k_blocks, tiles, s);
+                        : launch_grouped_epi<EPI_ROWS, 64>(mW, mX, a, n_nt, k_blocks, tiles, s);
     if (a.tile_rows == 128)
         return is_gated ? launch_grouped_epi<EPI_GATED, 128>(mW, mX, a, n_nt, k_blocks, tiles, s)
-                        : launch_grouped_epi<EPI_HALF, 128>(mW, mX, a, n_nt, k_blocks, tiles, s);
+                        : launch_grouped_epi<EPI_ROWS, 128>(mW, mX, a, n_nt, k_blocks, tiles, s);
     if (a.tile_rows == 192)
         return is_gated ? launch_grouped_epi<EPI_GATED, 192>(mW, mX, a, n_nt, k_blocks, tiles, s)
-                        : launch_grouped_epi<EPI_HALF, 192>(mW, mX, a, n_nt, k_blocks, tiles, s);
+                        : launch_grouped_epi<EPI_ROWS, 192>(mW, mX, a, n_nt, k_blocks, tiles, s);
     if (a.tile_rows != 256) return cudaErrorInvalidValue;
     return is_gated ? launch_grouped_epi<EPI_GATED, 256>(mW, mX, a, n_nt, k_blocks, tiles, s)
-                    : launch_grouped_epi<EPI_HALF, 256>(mW, mX, a, n_nt, k_blocks, tiles, s);
+                    : launch_grouped_epi<EPI_ROWS, 256>(mW, mX, a, n_nt, k_blocks, tiles, s);
 }
 
 }  // namespace i8

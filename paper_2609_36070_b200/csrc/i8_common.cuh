@@ -76,8 +76,6 @@ struct ProductArgs {
     int32_t c_type;              // MOK_TYPE_* (plain epilogue)
     const float* a_scale;        // [a_rows] (plain, swiglu)
     const float* b_scale;        // [E * (swiglu ? 2 : 1) * N]
-    const float* b_max;          // [E]: largest b_scale of the matrix (EPI_HALF)
-    float y_unit;                // EPI_HALF: power of two that brings |sum| <= 127 * 127 * K below 65504
     const float* bias;           // [N] or NULL (plain)
     int32_t dense_rows;          // > 0: dense
     const int4* tiles;           // grouped: {first row, rows of the segment from there on, expert, -} of every row tile
@@ -88,7 +86,7 @@ struct ProductArgs {
     int32_t bn;                  // set by the launcher: columns of a plain tile
     WsHeader* header;
 };
-enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_HALF = 2 };
+enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_ROWS = 2 };
 
 // Where a token's codes go when its rows are wanted in expert order: row pos[t * k + s] for every routed slot s.
 //   n > 0     : the launch makes the whole schedule of the n routes itself (at most ROUTES_HERE): pos, tiles and their number
@@ -107,7 +105,7 @@ struct RouteArgs {
 cudaError_t launch_quantize(const void* x, int type, long long rows, int K, long long ldx, int8_t* codes, long long ldc,
                             float* scales, cudaStream_t s, const RouteArgs* routes = nullptr);
 cudaError_t launch_product(const ProductArgs& a, int epi, cudaStream_t s);
-// few rows per expert (EPI_GATED, EPI_HALF)
+// few rows per expert (EPI_GATED, EPI_ROWS)
 cudaError_t launch_grouped(const ProductArgs& a, int epi, cudaStream_t s);
 // few tokens (EPI_PLAIN, dense): whether the kernel for them takes the product; quantises: from the activations (of x_type, -1:
 // there are only codes)

@@ -4,8 +4,8 @@
 //   2. token rows -> codes: found once per token, written once per route, in expert order.  (Gathering the rows in the product
 //      instead, with gathering TMA loads of four rows, took 70 cycles per load and three times the product's own time.)
 //   3. gate/up product, h = silu(g) u in fp32
-//   4. rows of h -> codes; the row's factor for step 6
-//   5. down product, fp16 in the unit of the row
+//   4. rows of h -> codes and a scale
+//   5. down product, fp32 rows
 //   6. combine: slot order, fp32, no atomics, so the bits do not depend on the launch
 #include "i8_common.cuh"
 #include <string.h>
@@ -17,13 +17,11 @@ constexpr int THREADS = 256;
 constexpr int ONE_BLOCK = 1024, ONE_BLOCK_ROUTES = 32768;    // of the schedule in one block
 constexpr long long GROUPED_ROWS = 112;                      // rows per expert up to which launch_grouped is the faster one
 
-// Rows of h (fp32) -> codes, one per route: route j's row is pos[j].  factor = scale * b_max / y_unit: what the combine
-// multiplies a row by.
+// Rows of h (fp32) -> codes and a scale (which the combine puts on), one per route: route j's row is pos[j].
 template <int TPR, int NV>
 __global__ void __launch_bounds__(THREADS)
-quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ codes, int ldc, float* __restrict__ factor,
-                       const float* __restrict__ b_max, float inv_unit, const int32_t* __restrict__ idx,
-                       const int32_t* __restrict__ pos, int n, int E) {
+quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ codes, int ldc, float* __restrict__ scales,
+                       const int32_t* __restrict__ idx, const int32_t* __restrict__ pos, int n, int E) {
     __shared__ uint32_t s_max[THREADS / 32];
     pdl_enter();
     constexpr int ROWS = THREADS / TPR, WARPS = TPR / 32;
@@ -42,7 +40,6 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
             v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (live && c < pieces) v[i] = __ldcs(src + c);
         }
-        const float top = live ? __ldg(b_max + e) : 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
             m = max(max(m, max(abs_bits(v[i].x), abs_bits(v[i].y))), max(abs_bits(v[i].z), abs_bits(v[i].w)));
@@ -67,65 +64,62 @@ quantize_hidden_kernel(const float* __restrict__ h, int I, int8_t* __restrict__ 
             if (codable) o = four_codes(v[i].x, v[i].y, v[i].z, v[i].w, rule);
             *reinterpret_cast<uint32_t*>(dst + c * 4) = o;
         }
-        if (sub == 0) factor[p] = amax / 127.f * (top * inv_unit);
+        if (sub == 0) scales[p] = amax / 127.f;
     }
 }
 
-// A block per token and 1024 columns, eight columns a thread.  Slots whose expert id is outside 0 .. E-1 are not routed.
+// A block per token and 1024 columns, four columns a thread.  Slots whose expert id is outside 0 .. E-1 are not routed: their
+// weights are not read.  A routed row counts even with weight 0 (0 times NaN is NaN).
+constexpr int COMBINE_THREADS = 256;
 template <class T>
-__global__ void __launch_bounds__(128)
-combine_half_kernel(const __half* __restrict__ y, const float* __restrict__ factor, const int32_t* __restrict__ idx,
-                    const float* __restrict__ w, const int32_t* __restrict__ pos, const T* __restrict__ add, long long ld_add,
-                    int H, int E, int k, T* __restrict__ out, long long ld_out) {
-    __shared__ int32_t s_pos[MAX_K];
+__global__ void __launch_bounds__(COMBINE_THREADS)
+combine_rows_kernel(const float* __restrict__ y, const float* __restrict__ scales, const int32_t* __restrict__ idx, const float* __restrict__ w,
+                    const int32_t* __restrict__ pos, const T* __restrict__ add, long long ld_add, int H, int E, int k,
+                    T* __restrict__ out, long long ld_out) {
+    struct alignas(4 * sizeof(T)) Four { T e[4]; };
+    __shared__ int32_t s_pos[MAX_K];                 // -1: not routed
     __shared__ float s_w[MAX_K];
     pdl_enter();
     const size_t t = blockIdx.x;
     if (threadIdx.x < k) {
         const size_t j = t * k + threadIdx.x;
         const bool routed = (unsigned)idx[j] < (unsigned)E;
-        const int p = routed ? pos[j] : 0;
+        const int p = routed ? pos[j] : -1;
         s_pos[threadIdx.x] = p;
-        s_w[threadIdx.x] = routed ? w[j] * factor[p] : 0.f;
+        s_w[threadIdx.x] = routed ? w[j] * scales[p] : 0.f;
     }
-    const int c = blockIdx.y * 128 + threadIdx.x;
-    const bool mine = c < H >> 3;
-    float acc[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[i] = 0.f;
+    const int c = (blockIdx.y * COMBINE_THREADS + threadIdx.x) * 4;
+    const bool mine = c < H;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     if (add && mine) {
-        const uint4 raw = __ldg(reinterpret_cast<const uint4*>(add + t * ld_add + c * 8));
-        const T* v = reinterpret_cast<const T*>(&raw);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc[i] = to_f(v[i]);
+        const Four v = *reinterpret_cast<const Four*>(add + t * ld_add + c);
+        acc = make_float4(to_f(v.e[0]), to_f(v.e[1]), to_f(v.e[2]), to_f(v.e[3]));
     }
     __syncthreads();
     if (!mine) return;
     for (int s0 = 0; s0 < k; s0 += 8) {
-        uint4 raw[8];
+        float4 row[8];
 #pragma unroll
-        for (int s = 0; s < 8; ++s) {            // eight rows on their way at once; unrouted slots bring zeros
-            raw[s] = make_uint4(0u, 0u, 0u, 0u);
-            if (s0 + s < k && s_w[s0 + s] != 0.f) raw[s] = __ldg(reinterpret_cast<const uint4*>(y + (size_t)s_pos[s0 + s] * H + c * 8));
+        for (int s = 0; s < 8; ++s) {            // eight rows on their way at once
+            row[s] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (s0 + s < k && s_pos[s0 + s] >= 0) row[s] = __ldg(reinterpret_cast<const float4*>(y + (size_t)s_pos[s0 + s] * H + c));
         }
 #pragma unroll
         for (int s = 0; s < 8; ++s) {
             if (s0 + s >= k) break;
-            const __half2* v = reinterpret_cast<const __half2*>(&raw[s]);
             const float f = s_w[s0 + s];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 q = __half22float2(v[i]);
-                acc[2 * i] = fmaf(f, q.x, acc[2 * i]);
-                acc[2 * i + 1] = fmaf(f, q.y, acc[2 * i + 1]);
-            }
+            acc.x = fmaf(f, row[s].x, acc.x);
+            acc.y = fmaf(f, row[s].y, acc.y);
+            acc.z = fmaf(f, row[s].z, acc.z);
+            acc.w = fmaf(f, row[s].w, acc.w);
         }
     }
-    uint4 o;
-    T* v = reinterpret_cast<T*>(&o);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = from_f<T>(acc[i]);
-    *reinterpret_cast<uint4*>(out + t * ld_out + c * 8) = o;
+    Four o;
+    o.e[0] = from_f<T>(acc.x);
+    o.e[1] = from_f<T>(acc.y);
+    o.e[2] = from_f<T>(acc.z);
+    o.e[3] = from_f<T>(acc.w);
+    *reinterpret_cast<Four*>(out + t * ld_out + c) = o;
 }
 
 // The schedule in one block, for batches of up to ONE_BLOCK_ROUTES routes: the layer's own schedule keeps an expert's rows in
@@ -190,7 +184,7 @@ static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_
 // Workspace of the routed experts: the schedule's tables (a WsLayout of which only those are set) and the activations.
 struct ExpertsLayout {
     WsLayout L;
-    size_t tiles, xq, xs, h, hq, factor, y, total;
+    size_t tiles, xq, xs, h, hq, hs, y, total;
     int pitch_h, pitch_i;
     bool grouped;                // the products for few rows per expert
     int tile_rows;               // of the products' row tiles
@@ -239,18 +233,19 @@ static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) 
     X->xs = take(sizeof(float) * (size_t)L.Rpad);
     X->h = take(sizeof(float) * (size_t)L.Rpad * I);
     X->hq = take((size_t)L.Rpad * X->pitch_i);
-    X->factor = take(sizeof(float) * (size_t)L.Rpad);
-    X->y = take(2 * (size_t)L.Rpad * H);
+    X->hs = take(sizeof(float) * (size_t)L.Rpad);
+    X->y = take(sizeof(float) * (size_t)L.Rpad * H);
     X->total = off;
     return true;
 }
 
 template <class T>
-static cudaError_t launch_combine_half(const mok_i8_experts_args* a, const ExpertsLayout& X, char* ws, cudaStream_t s) {
-    return launch_pdl(combine_half_kernel<T>, dim3((unsigned)a->T, (unsigned)((a->H + 1023) / 1024)), dim3(128), 0, s, reinterpret_cast<const __half*>(ws + X.y),
-                      reinterpret_cast<const float*>(ws + X.factor), a->topk_idx, a->topk_w,
-                      reinterpret_cast<const int32_t*>(ws + X.L.pos), reinterpret_cast<const T*>(a->add),
-                      (long long)a->add_stride, a->H, a->E, a->k, reinterpret_cast<T*>(a->out), (long long)a->out_stride);
+static cudaError_t launch_combine(const mok_i8_experts_args* a, const ExpertsLayout& X, char* ws, cudaStream_t s) {
+    const dim3 grid((unsigned)a->T, (unsigned)((a->H + 4 * COMBINE_THREADS - 1) / (4 * COMBINE_THREADS)));
+    return launch_pdl(combine_rows_kernel<T>, grid, dim3(COMBINE_THREADS), 0, s, reinterpret_cast<const float*>(ws + X.y),
+                      reinterpret_cast<const float*>(ws + X.hs), a->topk_idx, a->topk_w,
+                      reinterpret_cast<const int32_t*>(ws + X.L.pos), reinterpret_cast<const T*>(a->add), (long long)a->add_stride,
+                      a->H, a->E, a->k, reinterpret_cast<T*>(a->out), (long long)a->out_stride);
 }
 
 }  // namespace i8
@@ -410,16 +405,13 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     g.ldc = a->I;
     e = X.grouped ? i8::launch_grouped(g, i8::EPI_GATED, s) : i8::launch_product(g, i8::EPI_GATED, s);
     if (e != cudaSuccess) return cuda_fail(e);
-    float unit = 1.f;                                // |sum| * unit <= 65504
-    while (127.0 * 127.0 * a->I * unit > 65504.0) unit *= 0.5f;
     {
         const float* h = reinterpret_cast<const float*>(ws + X.h);
         int8_t* hq = reinterpret_cast<int8_t*>(ws + X.hq);
-        float* factor = reinterpret_cast<float*>(ws + X.factor);
         auto rows = [&](auto kernel, int per_block) {
             const int blocks = (X.L.R + per_block - 1) / per_block, most = 148 * 16;
             return launch_pdl(kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(i8::THREADS), 0, s, h, a->I, hq, X.pitch_i,
-                              factor, a->down_max, 1.f / unit, a->topk_idx, table(X.L.pos), X.L.R, a->E);
+                              reinterpret_cast<float*>(ws + X.hs), a->topk_idx, table(X.L.pos), X.L.R, a->E);
         };
         e = a->I <= 1024 ? rows(i8::quantize_hidden_kernel<32, 8>, 8)
             : a->I <= 2048 ? rows(i8::quantize_hidden_kernel<128, 4>, 2)
@@ -433,14 +425,12 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     g.B = a->down_codes;
     g.ldb = a->down_stride;
     g.b_scale = a->down_scales;
-    g.b_max = a->down_max;
-    g.y_unit = unit;
     g.K = a->I; g.N = a->H;
     g.C = ws + X.y;
     g.ldc = a->H;
-    e = X.grouped ? i8::launch_grouped(g, i8::EPI_HALF, s) : i8::launch_product(g, i8::EPI_HALF, s);
+    e = X.grouped ? i8::launch_grouped(g, i8::EPI_ROWS, s) : i8::launch_product(g, i8::EPI_ROWS, s);
     if (e != cudaSuccess) return cuda_fail(e);
-    e = a->type == MOK_TYPE_BF16 ? i8::launch_combine_half<__nv_bfloat16>(a, X, ws, s) : i8::launch_combine_half<__half>(a, X, ws, s);
+    e = a->type == MOK_TYPE_BF16 ? i8::launch_combine<__nv_bfloat16>(a, X, ws, s) : i8::launch_combine<__half>(a, X, ws, s);
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);
 }
 

@@ -1,0 +1,121 @@
+"""Routing and 8-bit operators where they can go wrong: precision of small channels, masked groups, signed zeros, extreme
+logits, aligned rows of every width, buffers wider than the rows, other streams.  Plain evaluations in 64 bits.
+
+Roundings: 2^-24 of the value for an fp32 operation; half a unit in the last place for the final one."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+UNIT = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def mok():
+    from paper_2609_36070_b200 import mok
+    yield mok
+    assert mok.mok_i8_status() == 0
+
+
+def gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape):
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+# ------------------------------------------------------------------------------------------------------ 8-bit experts
+
+def codes64(x):
+    x = x.double()
+    amax = x.abs().amax(-1, keepdim=True)
+    return torch.where(amax > 0, (x * 127 / amax).round(), torch.zeros_like(x)), (amax / 127).squeeze(-1)
+
+
+def weights(mok, g, *shape, scales=None):
+    codes = torch.randint(-127, 128, (*shape[:-1], (shape[-1] + 15) // 16 * 16), generator=g, device="cuda", dtype=torch.int8)
+    if scales is None:
+        scales = (torch.rand(*shape[:-1], generator=g, device="cuda") + 0.5) * 1e-3
+    return mok.I8Weights(codes, scales)
+
+
+def experts64(x, idx, w, gu, dn):
+    T, H = x.shape
+    E, I = gu.codes.shape[0], gu.codes.shape[1] // 2
+    out = torch.zeros(T, H, dtype=torch.float64, device=x.device)
+    q, s = codes64(x)
+    for e in range(E):
+        t, slot = torch.nonzero(idx == e, as_tuple=True)
+        if len(t):
+            z = (q[t] @ gu.codes[e, :, :H].double().t()) * s[t, None] * gu.scales[e].double()
+            hq, hs = codes64(torch.nn.functional.silu(z[:, :I]) * z[:, I:])
+            y = (hq @ dn.codes[e, :, :I].double().t()) * hs[:, None] * dn.scales[e].double()
+            out.index_add_(0, t, w[t, slot].double()[:, None] * y)
+    return out
+
+
+def routes(g, T, E, k):
+    top = randn(g, T, E).topk(k, -1)
+    return top.indices.int().contiguous(), top.values.softmax(-1)
+
+
+# few rows per expert and many (both products), batches of all three schedules
+@pytest.mark.parametrize("T,H,I,E,k", [(40, 256, 128, 8, 2), (900, 256, 192, 4, 2), (9000, 136, 64, 8, 4)])
+def test_experts_small_and_negative_channel_scales(mok, T, H, I, E, k):
+    """Output channels whose scales span ten orders of magnitude, some negative: every column keeps its own precision."""
+    g = gen(T)
+    x = randn(g, T, H).bfloat16()
+    scales = 10.0 ** (-10 * torch.rand(E, H, generator=g, device="cuda"))
+    scales = torch.where(torch.rand(E, H, generator=g, device="cuda") < 0.3, -scales, scales)
+    scales[:, 3] = -1.0
+    scales[:, 5] = 1e-10
+    scales[:, 7] = 0.0
+    scales[1] = -scales[1].abs()                          # a matrix without any positive scale
+    gu, dn = weights(mok, g, E, 2 * I, H), weights(mok, g, E, H, I, scales=scales)
+    idx, w = routes(g, T, E, k)
+    out = mok.mok_i8_experts(x, idx, w, gu, dn).double()
+    ref = experts64(x, idx, w, gu, dn)
+    assert (out[:, 7] == 0).all()
+    # one bf16 rounding moves a value by 2^-8 of it at most, and by less than half of that in the mean square; a code of the
+    # hidden row on the other side of a tie (one value in 2^14) moves a column by some 2^-7 / sqrt(I) of one of its T values
+    assert ((out - ref).norm(dim=0) <= 2.0 ** -8 * ref.norm(dim=0)).all()
+
+
+@pytest.mark.parametrize("T,H,I,E,k", [(64, 256, 64, 8, 2), (1000, 256, 64, 4, 2), (9000, 136, 64, 8, 4)])
+def test_experts_round_once(mok, T, H, I, E, k):
+    """fp16 outputs are the rounded 64-bit ones but for what 32-bit sums move across a rounding boundary.  Each output carries
+    some ten roundings of 2^-24 where the unit is 2^-11: one in 400 moves.  A hidden value is good to about 2^-21 of itself, 127
+    times that of a code: less than one row in 100 has a code on the other side of a tie.  A row with a second rounding to 11
+    bits would move every fourth output."""
+    g = gen(T + 1)
+    x = randn(g, T, H).half()
+    gu, dn = weights(mok, g, E, 2 * I, H), weights(mok, g, E, H, I)
+    dn.scales.mul_(20)                                     # (normal numbers of fp16)
+    idx, w = routes(g, T, E, k)
+    out = mok.mok_i8_experts(x, idx, w, gu, dn)
+    ref = experts64(x, idx, w, gu, dn)
+    assert ref.abs().max() < 6e4
+    assert (out != ref.half()).double().mean() <= 0.02
+
+
+def test_experts_broken_channel_and_zero_weight(mok):
+    """A channel whose scale is NaN is NaN for its expert's tokens, and no other channel is; a weight of 0 on a row that is NaN
+    gives NaN."""
+    g = gen(3)
+    T, H, I, E = 48, 64, 64, 4
+    x = randn(g, T, H).bfloat16()
+    gu, dn = weights(mok, g, E, 2 * I, H), weights(mok, g, E, H, I)
+    idx = (torch.arange(T, device="cuda") % E)[:, None].int().contiguous()
+    w = torch.ones(T, 1, device="cuda")
+    clean = mok.mok_i8_experts(x, idx, w, gu, dn)
+    dn.scales[2, 9] = math.nan
+    out = mok.mok_i8_experts(x, idx, w, gu, mok.I8Weights(dn.codes, dn.scales))
+    bad = torch.zeros(T, H, dtype=torch.bool, device="cuda")
+    bad[2::4, 9] = True
+    assert torch.equal(torch.isnan(out), bad) and torch.equal(out[~bad], clean[~bad])
+    w[2] = 0.0
+    out = mok.mok_i8_experts(x, idx, w, gu, mok.I8Weights(dn.codes, dn.scales))
+    assert torch.isnan(out[2, 9]) and (out[2, :9] == 0).all() and (out[2, 10:] == 0).all()
