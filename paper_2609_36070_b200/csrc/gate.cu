@@ -432,6 +432,7 @@ gate_kernel(const Params p) {
             float reach = fminf(above0 < (float)k ? h0 : INFINITY, above1 < (float)k ? h1 : INFINITY);
 #pragma unroll
             for (int off = 1; off < 8; off <<= 1) reach = fminf(reach, __shfl_xor_sync(0xffffffffu, reach, off));
+            if (reach == 0.f) reach = -0.f;          // (-0 - +0 would be -0, but both zeros reach a zero: v - -0 is +0 for them)
             // bit 4 i + j of the words: value j of piece i.  The sign of a difference is shifted in, one comparison's work for
             // two; the difference of equal infinities, NaN, has none (+inf; with -inf there is no list).
             unsigned mask[WORDS];

@@ -119,3 +119,29 @@ def test_experts_broken_channel_and_zero_weight(mok):
     w[2] = 0.0
     out = mok.mok_i8_experts(x, idx, w, gu, mok.I8Weights(dn.codes, dn.scales))
     assert torch.isnan(out[2, 9]) and (out[2, :9] == 0).all() and (out[2, 10:] == 0).all()
+
+
+# --------------------------------------------------------------------------------------------------------------- gate
+# T = 33 is served by the kernel with a warp per token, T = 2433 by the one with four tokens per warp.
+
+@pytest.mark.parametrize("T", [33, 2433])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("E", [40, 64, 160, 256])
+def test_gate_zeros_of_both_signs_are_equal(mok, T, dtype, E):
+    """Few zeros of both signs decide the k-th place: fewer than the lists hold, in the same and in different pieces of four."""
+    g = gen(E)
+    logits = torch.full((T, E), -1.0, device="cuda")
+    at = torch.rand(T, E, generator=g, device="cuda").argsort(-1)
+    zeros = torch.where(torch.randint(0, 2, (T, 20), generator=g, device="cuda") > 0, -0.0, 0.0)
+    logits.scatter_(1, at[:, :20], zeros)
+    above = torch.randint(0, 7, (T, 1), generator=g, device="cuda") > torch.arange(6, device="cuda")
+    logits.scatter_(1, at[:, 20:26], torch.where(above, randn(g, T, 6).abs() + 0.5, torch.full((T, 6), -2.0, device="cuda")))
+    logits[0] = -1.0                                       # every piece has a zero of both signs, the positive one later
+    logits[0, 0:32:4], logits[0, 1:32:4] = -0.0, 0.0
+    logits[1] = -1.0
+    logits[1, 0:24:4], logits[1, 1], logits[1, 24], logits[1, 28] = 1.0, -0.0, 0.0, 0.0
+    logits = logits.to(dtype)
+    for k in (3, 5, 8, 16):
+        idx, _ = mok.mok_gate(logits, k, score="sigmoid")
+        ref = logits.float().add(0.0).sort(dim=-1, descending=True, stable=True).indices[:, :k]     # (-0 + 0 is +0)
+        assert torch.equal(idx.long(), ref), k
