@@ -559,16 +559,18 @@ gate_kernel(const Params p) {
                 sum += s[q];
             }
         }
-        float times = p.scale;
         if (p.renormalise) {
+            // (the scores are divided first: scale / sum is infinite for a sum of subnormal scores)
             sum = sum8(sum);
-            times = sum == 0.f ? 0.f : p.scale / sum;
+#pragma unroll
+            for (int q = 0; q < MAX_K / 8; ++q)
+                if (8 * q < k) s[q] = sum == 0.f ? 0.f : s[q] / sum;
         }
 #pragma unroll
         for (int q = 0; q < MAX_K / 8; ++q) {
             if (8 * q + sub < k && t0 + own < p.T) {
                 p.idx[(size_t)t * k + 8 * q + sub] = chosen[8 * q + sub];
-                p.w[(size_t)t * k + 8 * q + sub] = s[q] * times;
+                p.w[(size_t)t * k + 8 * q + sub] = s[q] * p.scale;
             }
         }
         __syncwarp();                                // vals and chosen are rewritten by the next tokens

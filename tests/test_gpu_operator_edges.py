@@ -145,3 +145,19 @@ def test_gate_zeros_of_both_signs_are_equal(mok, T, dtype, E):
         idx, _ = mok.mok_gate(logits, k, score="sigmoid")
         ref = logits.float().add(0.0).sort(dim=-1, descending=True, stable=True).indices[:, :k]     # (-0 + 0 is +0)
         assert torch.equal(idx.long(), ref), k
+
+
+@pytest.mark.parametrize("T", [33, 2433])
+@pytest.mark.parametrize("k", [1, 2, 8])
+def test_gate_weights_of_subnormal_scores(mok, T, k):
+    """Sigmoid scores of logits around -88 are subnormal numbers of 32 bits, good to 2^-149: their renormalised weights are
+    finite and right to that."""
+    E = 16
+    logits = -87.5 - 1.2 * torch.rand(T, E, generator=gen(k), device="cuda")               # scores of 3e-39 .. 1e-38
+    for scale in (1.0, 2.5, 40.0):
+        idx, w = mok.mok_gate(logits, k, score="sigmoid", scale=scale)
+        s = torch.sigmoid(logits.double()).gather(1, idx.long())
+        ref = scale * s / s.sum(-1, keepdim=True)
+        # a score is off by 2^-22 of itself (exponential, quotient) and half of 2^-149; so is the sum, k times
+        off = 2.0 ** -22 + 2.0 ** -150 / s.min()
+        assert ((w.double() - ref).abs() <= 4 * off * ref).all()
