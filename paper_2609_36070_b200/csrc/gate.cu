@@ -642,18 +642,19 @@ gate_backward_kernel(const BwdParams p) {
                 s[q] = 0.f;
                 if (e[q] >= 0) s[q] = p.softmax ? exp_below(l[q], m) : sigmoid(l[q]);
                 total += s[q];
-                dot += g[q] * s[q];
             }
-            total = sum8(total);
-            dot = sum8(dot);
-            const float inv = total > 0.f ? 1.f / total : 0.f;
-            const float mean = dot * inv;
+            if (p.renormalise) {                     // (the scores are divided, not their sum inverted: it may be subnormal)
+                total = sum8(total);
 #pragma unroll
-            for (int q = 0; q < SLOTS; ++q) {
-                if (e[q] < 0) continue;
-                mine[e[q]] = p.softmax ? s[q] * inv * (g[q] - mean)
-                             : p.renormalise ? s[q] * sigmoid(-l[q]) * inv * (g[q] - mean) : g[q] * s[q] * sigmoid(-l[q]);
+                for (int q = 0; q < SLOTS; ++q) {
+                    if (8 * q < k) s[q] = total == 0.f ? 0.f : s[q] / total;
+                    dot += g[q] * s[q];
+                }
+                dot = sum8(dot);
             }
+#pragma unroll
+            for (int q = 0; q < SLOTS; ++q)
+                if (e[q] >= 0) mine[e[q]] = s[q] * (g[q] - dot) * (p.softmax ? 1.f : sigmoid(-l[q]));
             __syncwarp();
             if (!live) {
             } else if (vec) {

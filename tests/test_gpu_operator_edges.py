@@ -161,3 +161,19 @@ def test_gate_weights_of_subnormal_scores(mok, T, k):
         # a score is off by 2^-22 of itself (exponential, quotient) and half of 2^-149; so is the sum, k times
         off = 2.0 ** -22 + 2.0 ** -150 / s.min()
         assert ((w.double() - ref).abs() <= 4 * off * ref).all()
+
+
+@pytest.mark.parametrize("k", [1, 2, 8])
+def test_gate_gradient_of_subnormal_scores(mok, k):
+    T, E = 300, 16
+    logits = -87.5 - 1.2 * torch.rand(T, E, generator=gen(k), device="cuda")
+    idx, _ = mok.mok_gate(logits, k, score="sigmoid")
+    dw = randn(gen(k + 1), T, k)
+    d = mok.mok_gate_backward(logits, idx, dw, score="sigmoid", scale=2.5)
+    s = torch.sigmoid(logits.double()).gather(1, idx.long())
+    r, g = s / s.sum(-1, keepdim=True), 2.5 * dw.double()
+    ref = torch.zeros(T, E, dtype=torch.float64, device="cuda")
+    ref.scatter_(1, idx.long(), r * (1 - s) * (g - (g * r).sum(-1, keepdim=True)))
+    # r is off by 4 (2^-22 + 2^-150 / s) of itself, as the weights are, and multiplies differences of the largest |g|
+    off = 4 * (2.0 ** -22 + 2.0 ** -150 / s.min())
+    assert ((d.double() - ref).abs() <= 4 * off * g.abs().amax(-1, keepdim=True)).all()
