@@ -70,9 +70,14 @@ __device__ __forceinline__ float with_id(float v, int e) {
     const unsigned u = __float_as_uint(v + 0.f);
     return __uint_as_float(u | (unsigned)((u >> 31) ? e : MAX_E - 1 - e));
 }
-// Keys that compare as the values do: absent or taken experts 0, NaN 1, then -inf ... +inf.  -0 counts as 0.
+// What a choice value is compared as.  -inf stands for "not there", so NaN and -inf take the place of the lowest finite values,
+// in this order; finite values that low count as AT_LOWEST, so that both kernels order all values alike.
+constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOWEST = -3.40282306e38f;
+__device__ __forceinline__ float ranked(float v) {
+    return v != v ? AT_NAN : v == -INFINITY ? AT_MINUS_INF : fmaxf(v, AT_LOWEST);
+}
+// Keys that compare as ranked values do; absent or taken experts are 0.  -0 counts as 0.
 __device__ __forceinline__ unsigned choice_key(float v) {
-    if (v != v) return 1u;
     const unsigned u = __float_as_uint(v + 0.f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
@@ -147,6 +152,9 @@ gate_warp_kernel(const Params p) {
                 c[j] = c[j] == -INFINITY ? -INFINITY : s + bias[j];    // (absent, or not to be used whatever its bias)
             }
         }
+#pragma unroll
+        for (int j = 0; j < VPL; ++j)
+            if (lane + 32 * j < E) c[j] = ranked(c[j]);
         unsigned kept = 0xffffffffu;
         if (G > 1) {
             float* mine = s_choice + warp * E;
@@ -172,7 +180,7 @@ gate_warp_kernel(const Params p) {
                 b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
                 b1 = fmaxf(b1, o1);
             }
-            const unsigned value = choice_key(p.group_top == 2 ? b1 + b2 : b1);
+            const unsigned value = choice_key(fmaxf(p.group_top == 2 ? b1 + b2 : b1, -FLT_MAX));      // (two AT_ values)
             int rank = 0;
             for (int q = 0; q < G; ++q) {
                 const unsigned other = __shfl_sync(0xffffffffu, value, q * per);
@@ -261,9 +269,6 @@ __device__ __forceinline__ float sum8(float v) {
     return v;
 }
 
-// Values that compare below every other one, so that -inf can stand for "not there": NaN, then -inf, then the finite ones.
-constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOWEST = -3.40282306e38f;
-
 template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      // shared memory of a warp
 
 // Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.  (7 of the small ones, not 8:
@@ -294,21 +299,24 @@ gate_kernel(const Params p) {
         float c[NI][4];
 #pragma unroll
         for (int i = 0; i < NI; ++i) load4<VEC>(row, (sub + 8 * i) * 4, E, c[i]);
-        // a sum that is finite holds no NaN and no infinity
-        auto finite = [&]() {
+        // a finite sum of magnitudes holds no NaN and no infinity; one below LOW nothing near the lowest finite values either, so
+        // that ranked() changes nothing
+        constexpr float LOW = 1e38f;
+        auto magnitude = [&]() {
             float sum = 0.f;
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
                 const int e = (sub + 8 * i) * 4;
-                if (e + 3 < E) sum += (c[i][0] + c[i][1]) + (c[i][2] + c[i][3]);
+                if (e + 3 < E) sum += (fabsf(c[i][0]) + fabsf(c[i][1])) + (fabsf(c[i][2]) + fabsf(c[i][3]));
                 else if (!VEC) {
 #pragma unroll
-                    for (int j = 0; j < 3; ++j) sum += e + j < E ? c[i][j] : 0.f;
+                    for (int j = 0; j < 3; ++j) sum += e + j < E ? fabsf(c[i][j]) : 0.f;
                 }
             }
-            return fabsf(sum) < INFINITY;
+            return sum;
         };
-        bool ordinary = finite();
+        float size = magnitude();
+        const bool finite = size < INFINITY;
         float m = -INFINITY, total = 1.f;
         if (p.softmax) {
 #pragma unroll
@@ -343,7 +351,7 @@ gate_kernel(const Params p) {
                     c[i][j] = p.bias ? s + b[j] : s;
                 }
             }
-            ordinary = ordinary && finite();
+            size = magnitude();
             if (E < 32 * NI) {
 #pragma unroll
                 for (int i = 0; i < NI; ++i)
@@ -352,6 +360,7 @@ gate_kernel(const Params p) {
                         if ((sub + 8 * i) * 4 + j >= E) c[i][j] = -INFINITY;
             }
         }
+        const bool ordinary = size < LOW && finite;
         if (!ordinary) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) {
@@ -360,8 +369,7 @@ gate_kernel(const Params p) {
                 load4<VEC>(row, e, E, l);            // (an expert masked by -inf is not to be used whatever its bias)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float v = l[j] == -INFINITY ? -INFINITY : c[i][j];
-                    c[i][j] = e + j >= E ? -INFINITY : v != v ? AT_NAN : v == -INFINITY ? AT_MINUS_INF : fmaxf(v, AT_LOWEST);
+                    c[i][j] = e + j >= E ? -INFINITY : ranked(l[j] == -INFINITY ? -INFINITY : c[i][j]);
                 }
             }
         }

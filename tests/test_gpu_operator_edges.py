@@ -177,3 +177,29 @@ def test_gate_gradient_of_subnormal_scores(mok, k):
     # r is off by 4 (2^-22 + 2^-150 / s) of itself, as the weights are, and multiplies differences of the largest |g|
     off = 4 * (2.0 ** -22 + 2.0 ** -150 / s.min())
     assert ((d.double() - ref).abs() <= 4 * off * g.abs().amax(-1, keepdim=True)).all()
+
+
+@pytest.mark.parametrize("T", [33, 2433])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("E,k", [(40, 8), (64, 3), (60, 16), (256, 8), (300, 20)])
+def test_gate_order_of_extreme_logits(mok, T, dtype, E, k):
+    """+inf, finite values down to the type's lowest, -inf, NaN: in this order, equals by their ids, for tokens that have fewer
+    ordinary experts than k."""
+    g = gen(E + k)
+    kind = torch.randint(0, 40, (T, E), generator=g, device="cuda")
+    low = torch.finfo(dtype).min
+    logits = torch.full((T, E), -math.inf, device="cuda")
+    for at, v in ((0, 1.0), (1, -2.0), (2, low), (3, low / 2), (4, math.nan), (5, -low)):
+        logits[kind == at] = v
+    logits[T // 2:][kind[T // 2:] >= 20] = low             # half of the tokens: mostly the lowest value
+    logits[3:6] = -math.inf
+    logits[3, E - 1], logits[4, 1], logits[5, E // 2] = low, low, 0.0
+    logits[6:9] = math.nan
+    logits[6, E - 1], logits[7, 1] = -math.inf, low
+    logits[9, :] = low
+    logits[9, 5] = -math.inf
+    logits = logits.to(dtype)
+    idx, _ = mok.mok_gate(logits, k, score="sigmoid")
+    order = logits.double()
+    order = torch.where(torch.isnan(order), -1e40, torch.where(order == -math.inf, -1e39, order))
+    assert torch.equal(idx.long(), order.sort(dim=-1, descending=True, stable=True).indices[:, :k])
