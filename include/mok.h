@@ -492,7 +492,8 @@ int mok_ep_bwd_combine(const mok_ep_bwd_combine_args* args);
  * layers of this kind were extended with since).  Per token, in fp32:
  *     s = softmax(logits) or sigmoid(logits);   c = s + bias          (bias: selection only; NULL = none)
  *     the E experts form n_groups groups of consecutive ids; a group's value is its largest c (group_top = 1) or the sum of
- *     its two largest (2); the topk_groups groups of largest value stay (n_groups = topk_groups = 1: no groups)
+ *     its two largest (2); experts that may not be used (c of -inf or NaN) add nothing to it, and a group without any other
+ *     is below all groups; the topk_groups groups of largest value stay (n_groups = topk_groups = 1: no groups)
  *     topk_idx = the k largest c among them, descending; all ties go to the lowest id
  *     topk_w   = scale * s_i / sum_j s_j over the chosen (renormalise != 0; 0 where that sum is 0), or scale * s_i
  * Without a bias, and unless sums of two scores are compared, the logits themselves are compared.  Logits of -inf are

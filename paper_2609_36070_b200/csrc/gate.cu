@@ -2,7 +2,8 @@
 //
 //   s = sigmoid(l) or softmax(l) over the E experts of a token (fp32 whatever the logits' type)
 //   c = s + bias                     the choice value; the bias decides the selection only, never a weight
-//   groups of E / n_groups consecutive experts: a group's value is its best c, or the sum of its two best; the
+//   groups of E / n_groups consecutive experts: a group's value is its best c, or the sum of its two best; experts that may
+//   not be used (c of -inf or NaN) add nothing to it, and a group of such experts only is below all others.  The
 //   topk_groups best groups stay.  The k best c among them are the token's experts, in descending order; every tie (of
 //   groups and of experts) goes to the lowest id.
 //   w_i = scale * s_i / sum_j s_j over the chosen (renormalise; 0 where the sum is 0), or scale * s_i
@@ -26,7 +27,6 @@
 // against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
 #include "mok_internal.cuh"
 #include <cuda_fp16.h>
-#include <float.h>
 
 namespace mok {
 namespace gate {
@@ -75,6 +75,11 @@ __device__ __forceinline__ float with_id(float v, int e) {
 constexpr float AT_NAN = -3.40282347e38f, AT_MINUS_INF = -3.40282326e38f, AT_LOWEST = -3.40282306e38f;
 __device__ __forceinline__ float ranked(float v) {
     return v != v ? AT_NAN : v == -INFINITY ? AT_MINUS_INF : fmaxf(v, AT_LOWEST);
+}
+// A group's value from its two best ranked values, or its best one
+__device__ __forceinline__ float group_value(float b1, float b2, bool two) {
+    if (b1 <= AT_MINUS_INF) return AT_NAN;
+    return two && b2 > AT_MINUS_INF ? fmaxf(b1 + b2, AT_LOWEST) : b1;
 }
 // Keys that compare as ranked values do; absent or taken experts are 0.  -0 counts as 0.
 __device__ __forceinline__ unsigned choice_key(float v) {
@@ -180,7 +185,7 @@ gate_warp_kernel(const Params p) {
                 b2 = fmaxf(fminf(b1, o1), fmaxf(b2, o2));
                 b1 = fmaxf(b1, o1);
             }
-            const unsigned value = choice_key(fmaxf(p.group_top == 2 ? b1 + b2 : b1, -FLT_MAX));      // (two AT_ values)
+            const unsigned value = choice_key(group_value(b1, b2, p.group_top == 2));
             int rank = 0;
             for (int q = 0; q < G; ++q) {
                 const unsigned other = __shfl_sync(0xffffffffu, value, q * per);
@@ -399,7 +404,7 @@ gate_kernel(const Params p) {
                     b2 = fmaxf(fmaxf(b2, second), fminf(b1, h));
                     b1 = fmaxf(b1, h);
                 }
-                value[g] = fmaxf(p.group_top == 2 ? b1 + b2 : b1, -FLT_MAX) + 0.f;      // (two AT_ values; no -0)
+                value[g] = group_value(b1, b2, p.group_top == 2) + 0.f;     // (no -0)
             }
             __syncwarp();
             unsigned kept = 0u;

@@ -203,3 +203,47 @@ def test_gate_order_of_extreme_logits(mok, T, dtype, E, k):
     order = logits.double()
     order = torch.where(torch.isnan(order), -1e40, torch.where(order == -math.inf, -1e39, order))
     assert torch.equal(idx.long(), order.sort(dim=-1, descending=True, stable=True).indices[:, :k])
+
+
+@pytest.mark.parametrize("T", [33, 2433])
+@pytest.mark.parametrize("score,with_bias", [("sigmoid", False), ("sigmoid", True), ("softmax", False)])
+@pytest.mark.parametrize("group_top", [1, 2])
+@pytest.mark.parametrize("E,G,top_groups,k", [(64, 8, 4, 6), (64, 16, 5, 8), (160, 8, 3, 3), (60, 5, 2, 5), (54, 6, 3, 4)])
+def test_gate_groups_with_masked_experts(mok, T, score, with_bias, group_top, E, G, top_groups, k):
+    """Groups of which a token may use no, one, two or more experts: the value of a group is that of its usable ones."""
+    g = gen(E + G)
+    gs = E // G
+    logits = randn(g, T, E)
+    usable = torch.randint(0, 5, (T, G), generator=g, device="cuda")                       # 4: all
+    place = torch.rand(T, G, gs, generator=g, device="cuda").argsort(-1)
+    masked = ((place >= usable[..., None]) & (usable < 4)[..., None]).view(T, E)
+    logits[masked] = -math.inf
+    if score == "sigmoid":                                                                 # (a NaN breaks a whole softmax)
+        logits[masked & (torch.rand(T, E, generator=g, device="cuda") < 0.2)] = math.nan
+    logits[0] = -math.inf                                                                  # the seventh expert alone is left
+    logits[0, 7] = -3.0
+    logits[1, :gs] = -math.inf
+    logits[1, gs:] = randn(g, E - gs)
+    logits[1, -gs:] = -math.inf                                                            # one left of the last group ...
+    logits[1, -2] = 4.0
+    logits[1, gs:2 * gs] = -math.inf                                                       # ... and none of the first two
+    bias = randn(g, E) * 0.1 if with_bias else None
+    idx, w = mok.mok_gate(logits, k, bias=bias, score=score, n_groups=G, topk_groups=top_groups, group_top=group_top)
+    z = logits.double()
+    dead = torch.isnan(z) | (z == -math.inf)
+    s = torch.sigmoid(z) if score == "sigmoid" else torch.softmax(z, -1)
+    c = (s if bias is not None or group_top == 2 else z) + (0 if bias is None else bias.double())
+    c = torch.where(dead, -1e30, c)
+    best = c.view(T, G, gs).topk(min(2, gs), -1).values
+    value = torch.where((best[..., 1] > -1e29) & (group_top == 2), best.sum(-1), best[..., 0])
+    order = value.sort(dim=-1, descending=True, stable=True)
+    clear = (order.values[:, top_groups - 1] - order.values[:, top_groups] > 1e-6) | (order.values[:, top_groups] < -1e29)
+    keep = torch.zeros(T, G, dtype=torch.bool, device="cuda").scatter_(1, order.indices[:, :top_groups], True)
+    c = torch.where(torch.isnan(z), -2e30, c).masked_fill(~keep.repeat_interleave(gs, 1), -math.inf)
+    order = c.sort(dim=-1, descending=True, stable=True)
+    gaps = order.values[:, :k] - order.values[:, 1:k + 1]
+    clear &= ((gaps > 1e-6) | (order.values[:, :k] < -1e29)).all(-1)
+    assert clear.float().mean() > 0.97 and clear[:2].all()
+    assert torch.equal(idx.long()[clear], order.indices[:, :k][clear])
+    alive = (~dead).any(-1)
+    assert not dead.gather(1, idx.long())[alive, 0].any()                                  # no masked expert before a usable one
