@@ -32,6 +32,7 @@ namespace mok {
 namespace gate {
 
 constexpr int WARPS = 4;
+static_assert(MAX_K == 32, "the kernels add up the chosen scores of four slots per lane, or of one");
 
 __device__ __forceinline__ float load_f(const float* p) { return __ldg(p); }
 __device__ __forceinline__ float load_f(const __nv_bfloat16* p) { return __bfloat162float(*p); }
@@ -42,7 +43,8 @@ __device__ __forceinline__ void store_f(__half* p, float v) { *p = __float2half_
 
 __device__ __forceinline__ float sigmoid(float l) { return 1.f / (1.f + expf(-l)); }
 
-// For the comparison of scores: within 2^-22 of the exact value, which is what an fp32 score is worth.
+// For the comparison of scores: within 2^-21 of the exact value, absolutely, as scores near 1 are in fp32.  (Relatively the
+// exponent's rounding counts as well: 2^-24 |l|, 1e-6 of the score for l = -20.)  Weights are not made of it.
 __device__ __forceinline__ float exp2_near(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
@@ -86,14 +88,27 @@ __device__ __forceinline__ unsigned choice_key(float v) {
     const unsigned u = __float_as_uint(v + 0.f);
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
+// (Pairs of neighbours first.  The order of the sums is the one of the four-token kernel, where lane l's experts l, l + 32, ...
+// are element l % 4 of the pieces of lane l / 4: a token's weights have the same bits in any batch.)
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
-    for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
+    for (int off = 1; off < 32; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
 }
 __device__ __forceinline__ float warp_max(float v) {
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+    return v;
+}
+// Reductions over the eight lanes of a token.
+__device__ __forceinline__ float max8(float v) {
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
+    return v;
+}
+__device__ __forceinline__ float sum8(float v) {
+#pragma unroll
+    for (int off = 1; off < 8; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
 }
 // exp(l - m), 0 where everything is masked (m = -inf)
@@ -146,15 +161,15 @@ gate_warp_kernel(const Params p) {
         if (full_sum) {
             float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) sum += (lane + 32 * j < E) ? exp_below(c[j], m) : 0.f;
+            for (int j = 0; j < VPL; ++j) sum += exp_below(c[j], m);
             total = m == -INFINITY ? 1.f : warp_sum(sum);
         }
         if (by_score) {
             const float inv = 1.f / total;
 #pragma unroll
             for (int j = 0; j < VPL; ++j) {
-                const float s = p.softmax ? (m == -INFINITY ? 0.f : __expf(c[j] - m) * inv) : sigmoid_near(c[j]);
-                c[j] = c[j] == -INFINITY ? -INFINITY : s + bias[j];    // (absent, or not to be used whatever its bias)
+                const float s = p.softmax ? __fmul_rn(exp_below(c[j], m), inv) : sigmoid_near(c[j]);
+                c[j] = c[j] == -INFINITY ? -INFINITY : __fadd_rn(s, bias[j]);  // (absent, or not to be used whatever its bias)
             }
         }
 #pragma unroll
@@ -224,8 +239,9 @@ gate_warp_kernel(const Params p) {
             s = !p.softmax ? sigmoid(l) : full_sum ? exp_below(l, m) / total : exp_below(l, m);
         }
         if (p.renormalise) {
-            const float sum = warp_sum(s);
-            s = sum > 0.f || sum != sum ? s / sum : 0.f;
+            float sum = s + __shfl_xor_sync(0xffffffffu, s, 8);      // (the order of the four-token kernel again)
+            sum = sum8(sum + __shfl_xor_sync(0xffffffffu, sum, 16));
+            s = sum == 0.f ? 0.f : s / sum;
         }
         if (lane < k) {
             p.idx[(size_t)t * k + lane] = my_e;
@@ -262,18 +278,6 @@ __device__ __forceinline__ void load4(const H* row, int e, int E, float (&v)[4])
         for (int j = 0; j < 4; ++j) v[j] = e + j < E ? load_f(row + e + j) : -INFINITY;
     }
 }
-// Reductions over the eight lanes of a token.
-__device__ __forceinline__ float max8(float v) {
-#pragma unroll
-    for (int off = 1; off < 8; off <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, off));
-    return v;
-}
-__device__ __forceinline__ float sum8(float v) {
-#pragma unroll
-    for (int off = 1; off < 8; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
-    return v;
-}
-
 template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      // shared memory of a warp
 
 // Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.  (7 of the small ones, not 8:
@@ -329,18 +333,16 @@ gate_kernel(const Params p) {
             m = max8(m);
         }
         if (full_sum) {
-            // (a term's error, 2^-22 of it and 2^-24 of its exponent, is below the sum's rounding)
-            const float from = m == -INFINITY ? 0.f : m;
-            float sum = 0.f;
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float x = exp2_near((c[i][j] - from) * LOG2_E);
-                    sum += x;
+                    const float x = exp_below(c[i][j], m);
+                    part[j] += x;
                     if (by_score) c[i][j] = x;
                 }
-            sum = sum8(sum);
+            const float sum = sum8((part[0] + part[1]) + (part[2] + part[3]));
             total = m == -INFINITY ? 1.f : sum;
         }
         if (by_score) {
@@ -352,8 +354,8 @@ gate_kernel(const Params p) {
                 if (p.bias) load4<VEC>(p.bias, e, E, b);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float s = p.softmax ? c[i][j] * inv : sigmoid_near(c[i][j]);
-                    c[i][j] = p.bias ? s + b[j] : s;
+                    const float s = p.softmax ? __fmul_rn(c[i][j], inv) : sigmoid_near(c[i][j]);
+                    c[i][j] = p.bias ? __fadd_rn(s, b[j]) : s;
                 }
             }
             size = magnitude();
@@ -562,19 +564,18 @@ gate_kernel(const Params p) {
         }
         __syncwarp();
         // the chosen experts' weights, slots sub, sub + 8, ...
-        float s[MAX_K / 8], sum = 0.f;
+        float s[MAX_K / 8];
 #pragma unroll
         for (int q = 0; q < MAX_K / 8; ++q) {
             s[q] = 0.f;
             if (8 * q + sub < k) {
                 const float l = load_f(row + chosen[8 * q + sub]);
                 s[q] = !p.softmax ? sigmoid(l) : full_sum ? exp_below(l, m) / total : exp_below(l, m);
-                sum += s[q];
             }
         }
         if (p.renormalise) {
             // (the scores are divided first: scale / sum is infinite for a sum of subnormal scores)
-            sum = sum8(sum);
+            const float sum = sum8((s[0] + s[1]) + (s[2] + s[3]));
 #pragma unroll
             for (int q = 0; q < MAX_K / 8; ++q)
                 if (8 * q < k) s[q] = sum == 0.f ? 0.f : s[q] / sum;

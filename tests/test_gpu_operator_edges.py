@@ -247,3 +247,29 @@ def test_gate_groups_with_masked_experts(mok, T, score, with_bias, group_top, E,
     assert torch.equal(idx.long()[clear], order.indices[:, :k][clear])
     alive = (~dead).any(-1)
     assert not dead.gather(1, idx.long())[alive, 0].any()                                  # no masked expert before a usable one
+
+
+@pytest.mark.parametrize("score,with_bias,renorm", [("sigmoid", True, True), ("sigmoid", False, False), ("softmax", False, True),
+                                                    ("softmax", True, False), ("softmax", False, False)])
+@pytest.mark.parametrize("E,G,top_groups,k,dtype", [(8, 1, 1, 2, torch.float32), (60, 1, 1, 4, torch.float16), (64, 8, 3, 6, torch.bfloat16),
+                                                    (160, 8, 3, 6, torch.float32), (256, 8, 4, 8, torch.float32), (256, 1, 1, 8, torch.bfloat16),
+                                                    (384, 1, 1, 10, torch.float32), (384, 4, 2, 32, torch.bfloat16), (511, 1, 1, 17, torch.float32),
+                                                    (512, 16, 5, 16, torch.float32)])
+@pytest.mark.parametrize("pitch", [0, 3])
+def test_gate_gives_a_token_the_same_bits_in_any_batch(mok, score, with_bias, renorm, E, G, top_groups, k, dtype, pitch):
+    g = gen(E + k)
+    T = 2900
+    logits = (randn(g, T, E + pitch) * 2).to(dtype)[:, :E]
+    logits[5:40][torch.rand(35, E, generator=g, device="cuda") < 0.7] = -math.inf
+    logits[40:60][torch.rand(20, E, generator=g, device="cuda") < 0.7] = torch.finfo(dtype).min
+    logits[60] = -math.inf
+    logits[61, 3] = math.nan
+    logits[62, 3] = math.inf
+    logits[63:90] -= 80.0
+    bias = randn(g, E) * 0.1 if with_bias else None
+    kw = dict(bias=bias, score=score, n_groups=G, topk_groups=top_groups, group_top=2, renormalise=renorm, scale=1.7)
+    idx, w = mok.mok_gate(logits, k, **kw)
+    for some in (slice(0, 1), slice(0, 100), slice(900, 2900)):
+        i, v = mok.mok_gate(logits[some], k, **kw)
+        assert torch.equal(i, idx[some]) and ((v == w[some]) | (torch.isnan(v) & torch.isnan(w[some]))).all()
+    assert torch.isfinite(w[63:]).all() and (w[60] == 0).all()
