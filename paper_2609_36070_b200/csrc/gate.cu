@@ -828,7 +828,7 @@ int mok_gate(const mok_gate_args* a) {
     const gate::Params p = {a->logits, a->bias, a->logits_stride, a->T, a->E, a->k, a->score == MOK_SCORE_SOFTMAX,
                             a->n_groups, a->topk_groups, a->group_top, a->renormalise != 0, a->scale, a->topk_idx, a->topk_w};
     cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
-    g_pdl = true;
+    const DependentLaunches dependent;
     cudaError_t e = a->logits_type == MOK_TYPE_F32 ? gate::launch_gate<float>(p, s)
                     : a->logits_type == MOK_TYPE_BF16 ? gate::launch_gate<__nv_bfloat16>(p, s) : gate::launch_gate<__half>(p, s);
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);
@@ -849,7 +849,7 @@ int mok_gate_backward(const mok_gate_bwd_args* a) {
     const gate::BwdParams p = {a->logits, a->topk_idx, a->dw, a->logits_stride, a->dlogits_stride, a->T, a->E, a->k,
                                a->score == MOK_SCORE_SOFTMAX, a->renormalise != 0, a->scale, a->dlogits};
     cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
-    g_pdl = true;
+    const DependentLaunches dependent;
     cudaError_t e = a->logits_type == MOK_TYPE_F32 ? gate::launch_backward<float>(p, s)
                     : a->logits_type == MOK_TYPE_BF16 ? gate::launch_backward<__nv_bfloat16>(p, s)
                                                       : gate::launch_backward<__half>(p, s);

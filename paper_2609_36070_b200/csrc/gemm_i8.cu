@@ -439,7 +439,7 @@ static cudaError_t launch_pair(const CUtensorMap& mA, const CUtensorMap& mB, con
     });
     if (e != cudaSuccess) return e;
     cfg.gridDim = dim3((unsigned)(2 * (tiles < units ? tiles : units)));
-    cfg.numAttrs = 2;
+    cfg.numAttrs = g_pdl ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, mA, mB, mC, a, n_nt, k_blocks);
 }
 

@@ -324,7 +324,7 @@ static cudaError_t launch_narrow_typed(const CUtensorMap& mW, const CUtensorMap&
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cfg.attrs = attr;
-    cfg.numAttrs = 2;
+    cfg.numAttrs = g_pdl ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, mW, mX, a);
 }
 

@@ -262,7 +262,7 @@ int mok_i8_quantize(const void* x, int type, long long rows, int K, long long x_
     if (rows == 0) return MOK_OK;
     if (!x || !codes || !scales) return MOK_ERR_NULL;
     if (!i8::aligned(x, i8::type_bytes(type)) || !i8::aligned(scales, 4)) return MOK_ERR_ALIGN;
-    g_pdl = true;
+    const DependentLaunches dependent;
     const cudaError_t e = i8::launch_quantize(x, type, rows, K, x_stride, codes, codes_stride > K ? codes_stride : K, scales,
                                               reinterpret_cast<cudaStream_t>(stream));
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);
@@ -296,7 +296,7 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
               : !i8::aligned(a->x, i8::type_bytes(a->x_type)))
         return MOK_ERR_ALIGN;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
-    g_pdl = true;
+    const DependentLaunches dependent;
     i8::ProductArgs g = {};
     cudaError_t e = i8::status_header(&g.header);
     if (e != cudaSuccess) return cuda_fail(e);
@@ -362,7 +362,7 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
     char* ws = reinterpret_cast<char*>(a->workspace);
     WsHeader* hdr = reinterpret_cast<WsHeader*>(ws + X.L.header);
-    g_pdl = true;
+    const DependentLaunches dependent;
     i8::ProductArgs g = {};
     cudaError_t e = i8::status_header(&g.header);
     if (e != cudaSuccess) return cuda_fail(e);

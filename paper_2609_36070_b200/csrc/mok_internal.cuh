@@ -194,6 +194,12 @@ __device__ __forceinline__ void pdl_enter() {
 #endif
 }
 extern thread_local bool g_pdl;       // set per forward call from config.serial_launches
+// For the time of a call that has no such option: dependent launches, and afterwards what the thread had before.
+struct DependentLaunches {
+    const bool before;
+    DependentLaunches() : before(g_pdl) { g_pdl = true; }
+    ~DependentLaunches() { g_pdl = before; }
+};
 template <class... P, class... A>
 inline cudaError_t launch_pdl(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, A&&... args) {
     cudaLaunchConfig_t cfg = {};

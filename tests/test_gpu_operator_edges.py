@@ -273,3 +273,27 @@ def test_gate_gives_a_token_the_same_bits_in_any_batch(mok, score, with_bias, re
         i, v = mok.mok_gate(logits[some], k, **kw)
         assert torch.equal(i, idx[some]) and ((v == w[some]) | (torch.isnan(v) & torch.isnan(w[some]))).all()
     assert torch.isfinite(w[63:]).all() and (w[60] == 0).all()
+
+
+# ------------------------------------------------------------------------------------------------- what a call leaves
+
+@pytest.mark.parametrize("dependent", [False, True])
+def test_calls_leave_the_threads_launch_mode(mok, dependent):
+    """The layer's serial_launches sets how the later entry points that read the mode launch; these operators put it back."""
+    import ctypes
+    from paper_2609_36070_b200 import build
+    mode = ctypes.c_bool.in_dll(ctypes.CDLL(build.LIB), "_ZN3mok5g_pdlE")
+    g = gen(1)
+    logits, x = randn(g, 12, 16), randn(g, 12, 64).bfloat16()
+    gu, dn = weights(mok, g, 16, 32, 64), weights(mok, g, 16, 64, 16)
+    lin = mok.I8Weights(gu.codes[0], gu.scales[0])
+    before = mode.value
+    try:
+        for call in (lambda: mok.mok_gate(logits, 2), lambda: mok.mok_i8_quantize(x), lambda: mok.mok_i8_linear(x, lin),
+                     lambda: mok.mok_gate_backward(logits, *mok.mok_gate(logits, 2)),
+                     lambda: mok.mok_i8_experts(x, *mok.mok_gate(logits, 2), gu, dn)):
+            mode.value = dependent
+            call()
+            assert mode.value == dependent
+    finally:
+        mode.value = before
