@@ -13,7 +13,10 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmok.so"
 if not os.path.exists(_LIB_PATH):
     raise ImportError(f"{_LIB_PATH} is missing: build it with `python -m paper_2609_36070_b200.build`")
 _lib = ctypes.CDLL(_LIB_PATH)
-from . import _binding  # noqa: E402  (needs torch and the library; fails as loudly)
+try:
+    from . import _binding  # noqa: E402  (needs torch and the library)
+except ImportError as _e:   # the layer works without it; the operators bound there say what to do
+    _binding, _binding_error = None, _e
 
 MOK_OK = 0
 MOK_ERR_NULL, MOK_ERR_SHAPE, MOK_ERR_ALIGN, MOK_ERR_WORKSPACE = -1, -2, -3, -4
@@ -216,12 +219,23 @@ def _check(status):
         raise MokError(status)
 
 
-_binding.set_error(MokError)
 # routing from logits, 8-bit products and 8-bit experts: bound in C++ (csrc/binding.cpp), since their smallest calls take as
 # long as the host does
-mok_gate, mok_gate_backward = _binding.mok_gate, _binding.mok_gate_backward
-mok_i8_quantize, mok_i8_linear, mok_i8_matmul = _binding.mok_i8_quantize, _binding.mok_i8_linear, _binding.mok_i8_matmul
-mok_i8_experts = _binding.mok_i8_experts
+def _bound(name):
+    if _binding is not None:
+        return getattr(_binding, name)
+
+    def missing(*args, **kwargs):
+        raise ImportError(f"{name} is bound in _binding.so, which does not load ({_binding_error}): build it with "
+                          "`python -m paper_2609_36070_b200.build --force`") from _binding_error
+    return missing
+
+
+if _binding is not None:
+    _binding.set_error(MokError)
+mok_gate, mok_gate_backward = _bound("mok_gate"), _bound("mok_gate_backward")
+mok_i8_quantize, mok_i8_linear, mok_i8_matmul = _bound("mok_i8_quantize"), _bound("mok_i8_linear"), _bound("mok_i8_matmul")
+mok_i8_experts = _bound("mok_i8_experts")
 
 
 def _p(t):

@@ -1,0 +1,40 @@
+"""Host side of the routing and 8-bit operators: a missing extension module, scratch sizes, arguments that are refused before
+anything is allocated or launched."""
+import os
+import shutil
+import subprocess
+import sys
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def mok():
+    from paper_2609_36070_b200 import build
+    build.build()
+    from paper_2609_36070_b200 import mok
+    return mok
+
+
+def test_the_layer_imports_without_the_extension_module(mok, tmp_path):
+    """... and the operators bound in it say how to build it."""
+    from paper_2609_36070_b200 import build
+    package = tmp_path / "paper_2609_36070_b200"
+    package.mkdir()
+    for name in os.listdir(build.PKG):
+        if name.endswith(".py") or name == "libmok.so":
+            shutil.copy(os.path.join(build.PKG, name), package)
+    code = """
+from paper_2609_36070_b200 import mok
+assert mok.mok_i8_experts_workspace_bytes(4, 64, 64, 4, 2) > 0 and callable(mok.mok_moe_forward)
+for call in (mok.mok_gate, mok.mok_gate_backward, mok.mok_i8_quantize, mok.mok_i8_linear, mok.mok_i8_matmul, mok.mok_i8_experts):
+    try:
+        call(None, 1)
+    except ImportError as e:
+        assert "paper_2609_36070_b200.build" in str(e)
+    else:
+        raise AssertionError(call)
+"""
+    env = {**os.environ, "PYTHONPATH": str(tmp_path)}
+    done = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, env=env, capture_output=True, text=True)
+    assert done.returncode == 0, done.stderr
