@@ -4,6 +4,7 @@ tensors) with g++.
 `python -m paper_2609_36070_b200.build [--force] [--verbose]`.  nvcc cross-compiles without a GPU.
 """
 import glob
+import importlib.metadata
 import os
 import subprocess
 import sys
@@ -15,6 +16,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmok.so")
 BINDING = os.path.join(PKG, "_binding.so")
 BINDING_SRC = os.path.join(CSRC, "binding.cpp")
+BINDING_FOR = os.path.join(PKG, "build", "binding.torch")       # the torch and Python that _binding.so was compiled against
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
@@ -36,7 +38,13 @@ def _stale():
 def build_binding(force: bool = False) -> str:
     """The Python extension module, linked against libmok.so beside it and against torch's libraries (loaded by torch)."""
     deps = [BINDING_SRC, os.path.join(ROOT, "include", "mok.h")]
-    if not force and os.path.exists(BINDING) and all(os.path.getmtime(d) <= os.path.getmtime(BINDING) for d in deps):
+    wanted = f"torch {importlib.metadata.version('torch')}, Python {sys.version.split()[0]}"
+    built = ""
+    if os.path.exists(BINDING_FOR):
+        with open(BINDING_FOR) as f:
+            built = f.read()
+    if (not force and built == wanted and os.path.exists(BINDING) and
+            all(os.path.getmtime(d) <= os.path.getmtime(BINDING) for d in deps)):
         return BINDING
     import torch
     site = os.path.join(os.path.dirname(torch.__file__), "")
@@ -48,6 +56,9 @@ def build_binding(force: bool = False) -> str:
                     *(f"-I{d}" for d in include), BINDING_SRC, "-o", BINDING + ".tmp", f"-L{site}lib", *(f"-l{n}" for n in libs),
                     f"-L{PKG}", "-l:libmok.so", "-Wl,-rpath,$ORIGIN"], check=True)
     os.replace(BINDING + ".tmp", BINDING)
+    os.makedirs(os.path.dirname(BINDING_FOR), exist_ok=True)
+    with open(BINDING_FOR, "w") as f:
+        f.write(wanted)
     return BINDING
 
 

@@ -38,3 +38,23 @@ for call in (mok.mok_gate, mok.mok_gate_backward, mok.mok_i8_quantize, mok.mok_i
     env = {**os.environ, "PYTHONPATH": str(tmp_path)}
     done = subprocess.run([sys.executable, "-c", code], cwd=tmp_path, env=env, capture_output=True, text=True)
     assert done.returncode == 0, done.stderr
+
+
+def test_the_extension_module_is_rebuilt_for_another_torch(mok, tmp_path, monkeypatch):
+    from paper_2609_36070_b200 import build
+    calls = []
+
+    def compiler(cmd, check):
+        calls.append(cmd)
+        open(cmd[cmd.index("-o") + 1], "w").close()
+
+    monkeypatch.setattr(build, "BINDING", str(tmp_path / "_binding.so"))
+    monkeypatch.setattr(build, "BINDING_FOR", str(tmp_path / "build" / "binding.torch"))
+    monkeypatch.setattr(build.subprocess, "run", compiler)
+    build.build_binding()
+    build.build_binding()
+    assert len(calls) == 1                                # up to date
+    monkeypatch.setattr("importlib.metadata.version", lambda name: "0.0.1")
+    build.build_binding()
+    build.build_binding()
+    assert len(calls) == 2
