@@ -228,7 +228,7 @@ static bool experts_layout(int T, int H, int I, int E, int k, ExpertsLayout* X) 
     L.pos = take(r1);
     L.blk_hist = take(sizeof(int32_t) * (size_t)L.n_blk * E);
     L.row_token = take(sizeof(int32_t) * (size_t)L.Rpad);
-    X->tiles = take(sizeof(int4) * (size_t)(X->max_tiles > 0 ? X->max_tiles : 1));
+    X->tiles = take(sizeof(int4) * (size_t)(R / 64 + nonempty + 1));      // (of the smallest tiles: no size falls as T grows)
     X->xq = take((size_t)L.Rpad * X->pitch_h);
     X->xs = take(sizeof(float) * (size_t)L.Rpad);
     X->h = take(sizeof(float) * (size_t)L.Rpad * I);

@@ -58,3 +58,14 @@ def test_the_extension_module_is_rebuilt_for_another_torch(mok, tmp_path, monkey
     build.build_binding()
     build.build_binding()
     assert len(calls) == 2
+
+
+@pytest.mark.parametrize("E,k", [(300, 8), (62, 6), (11, 8), (511, 1), (128, 8), (1, 1), (512, 32)])
+@pytest.mark.parametrize("H,I", [(2048, 768), (8, 8)])
+def test_experts_scratch_never_shrinks_with_the_batch(mok, E, k, H, I):
+    """A workspace for T tokens serves every smaller batch, over the thresholds of the tile sizes and of the schedules."""
+    sizes = [mok.mok_i8_experts_workspace_bytes(T, H, I, E, k) for T in range(0, 120 * E // k + 40)]
+    assert sizes[0] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+    T = 32768 // k
+    near = [mok.mok_i8_experts_workspace_bytes(t, H, I, E, k) for t in range(T - 40, T + 40)]
+    assert all(a <= b for a, b in zip(near, near[1:]))
