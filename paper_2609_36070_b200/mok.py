@@ -699,7 +699,9 @@ class I8Weights:
     @classmethod
     def quantize(cls, W, stream=None):
         """From floating-point weights [N, K] or [E, N, K]."""
-        return cls(*mok_i8_quantize(W, stream=stream))
+        codes, scales = mok_i8_quantize(W, stream=stream)
+        with torch.cuda.stream(stream):         # (None: as it is) the largest scales are found where the scales are written
+            return cls(codes, scales)
 
 
 def alloc_i8_workspace(T, H, I, E, k, device="cuda"):

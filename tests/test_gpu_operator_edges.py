@@ -297,3 +297,20 @@ def test_calls_leave_the_threads_launch_mode(mok, dependent):
             assert mode.value == dependent
     finally:
         mode.value = before
+
+
+def test_weights_quantised_on_another_stream(mok):
+    """Codes, scales and the largest scales all belong to the stream that is named."""
+    g = gen(2)
+    W = randn(g, 5, 64, 96)
+    ref = mok.I8Weights.quantize(W)
+    side = torch.cuda.Stream()
+    for n in range(3):
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)                   # the stream is busy when the call is made
+            late = W.clone()
+        q = mok.I8Weights.quantize(late, stream=side)
+        side.synchronize()
+        assert torch.equal(q.codes, ref.codes) and torch.equal(q.scales, ref.scales) and torch.equal(q.max, ref.scales.amax(-1))
+        del q, late
+        torch.full((5,), 7.0, device="cuda")
