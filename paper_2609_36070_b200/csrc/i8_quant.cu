@@ -120,7 +120,7 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
     __shared__ int32_t s_place[ROUTED ? MAX_K : 1];
     pdl_enter();
     if (ROUTED && routes.n == 0 && routes.tiles) write_tiles(routes);
-    const int sub = threadIdx.x % TPR, pieces = K / PER;
+    const int sub = threadIdx.x % TPR, pieces = K / PER, padded = (K + 15) & ~15;
     constexpr int ROWS = BLOCK / TPR;
     for (long long r0 = (long long)blockIdx.x * ROWS; r0 < rows; r0 += (long long)gridDim.x * ROWS) {
         const long long r = r0 + threadIdx.x / TPR;
@@ -172,7 +172,7 @@ quantize_vec_kernel(const T* __restrict__ x, long long rows, int K, long long ld
                 else *reinterpret_cast<uint32_t*>(dst + c * 4) = raw[i].x;
             }
             if (sub == 0) scales[row] = amax / 127.f;
-            for (int c = K + sub; c < ldc && c < K + 16; c += TPR) dst[c] = 0;     // the pitch's tail
+            if (K + sub < padded && K + sub < ldc) dst[K + sub] = 0;               // (fewer than 16 bytes)
         }
     }
 }
@@ -186,6 +186,7 @@ quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ld
     __shared__ int32_t s_place[ROUTED ? MAX_K : 1];
     pdl_enter();
     if (ROUTED && routes.n == 0 && routes.tiles) write_tiles(routes);
+    const int padded = (K + 15) & ~15;
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const T* src = x + r * ldx;
         if constexpr (ROUTED) {
@@ -205,7 +206,7 @@ quantize_any_kernel(const T* __restrict__ x, long long rows, int K, long long ld
             for (int c = threadIdx.x; c < K; c += THREADS)
                 dst[c] = codable ? (int8_t)(code_bits(to_f(src[c]), rule) & 0xffu) : (int8_t)0;
             if (threadIdx.x == 0) scales[row] = amax / 127.f;
-            for (int c = K + threadIdx.x; c < ldc && c < K + 16; c += THREADS) dst[c] = 0;
+            if (K + (int)threadIdx.x < padded && K + (int)threadIdx.x < ldc) dst[K + threadIdx.x] = 0;
         }
     }
 }

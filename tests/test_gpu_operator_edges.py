@@ -314,3 +314,24 @@ def test_weights_quantised_on_another_stream(mok):
         assert torch.equal(q.codes, ref.codes) and torch.equal(q.scales, ref.scales) and torch.equal(q.max, ref.scales.amax(-1))
         del q, late
         torch.full((5,), 7.0, device="cuda")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows", [1, 3, 1300])
+@pytest.mark.parametrize("K,stride", [(16, 64), (16, 48), (20, 64), (20, 24), (24, 48), (7, 16), (7, 7), (2048, 2080), (2056, 2096), (17000, 17040)])
+def test_quantised_rows_of_a_wider_buffer(mok, dtype, rows, K, stride):
+    """Codes as a column range of a wider buffer: what follows the next multiple of 16 columns is not written."""
+    import ctypes
+    from paper_2609_36070_b200 import build
+    f = ctypes.CDLL(build.LIB).mok_i8_quantize
+    f.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_int, ctypes.c_longlong, ctypes.c_void_p,
+                  ctypes.c_longlong, ctypes.c_void_p, ctypes.c_void_p]
+    x = randn(gen(K), rows, K).to(dtype)
+    want, _ = mok.mok_i8_quantize(x)
+    buffer = torch.full((rows + 2, stride), 77, dtype=torch.int8, device="cuda")           # (a row before and one behind)
+    scales = torch.empty(rows, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+    assert f(x.data_ptr(), 2 if dtype == torch.float32 else 0, rows, K, K, buffer[1].data_ptr(), stride, scales.data_ptr(), stream) == 0
+    end = min(stride, (K + 15) // 16 * 16)
+    assert torch.equal(buffer[1:-1, :K], want[:, :K]) and (buffer[1:-1, K:end] == 0).all()
+    assert (buffer[1:-1, end:] == 77).all() and (buffer[0] == 77).all() and (buffer[-1] == 77).all()
