@@ -143,8 +143,8 @@ gate_warp_kernel(const Params p) {
     }
     int per = 1;                                     // lanes that share a group's experts: G * per <= 32
     while (G * per * 2 <= 32) per *= 2;
-    for (int t = blockIdx.x * WARPS + warp; t < p.T; t += gridDim.x * WARPS) {
-        const L* row = reinterpret_cast<const L*>(p.logits) + (long long)t * p.stride;
+    for (long long t = (long long)blockIdx.x * WARPS + warp; t < p.T; t += (long long)gridDim.x * WARPS) {
+        const L* row = reinterpret_cast<const L*>(p.logits) + t * p.stride;
         float c[VPL];
         float m = -INFINITY, total = 1.f;
 #pragma unroll

@@ -335,3 +335,15 @@ def test_quantised_rows_of_a_wider_buffer(mok, dtype, rows, K, stride):
     end = min(stride, (K + 15) // 16 * 16)
     assert torch.equal(buffer[1:-1, :K], want[:, :K]) and (buffer[1:-1, K:end] == 0).all()
     assert (buffer[1:-1, end:] == 77).all() and (buffer[0] == 77).all() and (buffer[-1] == 77).all()
+
+
+def test_gate_of_the_largest_number_of_tokens(mok):
+    """2^31 - 1 tokens: the step past the last one does not fit 32 bits (two experts in two groups: a warp per token)."""
+    T = 2 ** 31 - 1
+    logits = torch.zeros(T, 2, dtype=torch.bfloat16, device="cuda")
+    logits[-1, 1] = logits[T // 2, 1] = logits[0, 1] = 1.0
+    idx, w = mok.mok_gate(logits, 1, n_groups=2, group_top=1, renormalise=False)
+    torch.cuda.synchronize()
+    at = torch.tensor([0, 1, T // 2, T - 2, T - 1], device="cuda")
+    assert idx[at, 0].tolist() == [1, 0, 1, 0, 1]
+    assert (w[at, 0].double() - torch.tensor([1.0, 0.0, 1.0, 0.0, 1.0], device="cuda", dtype=torch.float64).sigmoid()).abs().max() < 1e-6
