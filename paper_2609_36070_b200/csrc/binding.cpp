@@ -20,6 +20,14 @@ namespace {
 PyObject* g_error = nullptr;             // mok.MokError
 
 // ------------------------------------------------------------------------------------------------- arguments of a call
+// A string for a message (there are Python strings that have no UTF-8 form)
+std::string text(PyObject* o) {
+    const char* s = PyUnicode_AsUTF8(o);
+    if (s) return s;
+    PyErr_Clear();
+    return "?";
+}
+
 // Positional and keyword arguments by name; `required` of them have to be there.
 template <int N>
 struct Call {
@@ -33,7 +41,7 @@ struct Call {
             int at = -1;
             for (int i = 0; i < N && at < 0; ++i)
                 if (PyUnicode_CompareWithASCIIString(name, names[i]) == 0) at = i;
-            if (at < 0) throw_type(function, std::string("unexpected argument ") + PyUnicode_AsUTF8(name));
+            if (at < 0) throw_type(function, std::string("unexpected argument ") + text(name));
             if (v[at]) throw_type(function, std::string("argument given twice: ") + names[at]);
             v[at] = args[n_args + q];
         }
@@ -79,7 +87,7 @@ int32_t score(PyObject* o) {
     TORCH_CHECK_TYPE(PyUnicode_Check(o), "score: expected a string");
     if (PyUnicode_CompareWithASCIIString(o, "softmax") == 0) return MOK_SCORE_SOFTMAX;
     if (PyUnicode_CompareWithASCIIString(o, "sigmoid") == 0) return MOK_SCORE_SIGMOID;
-    TORCH_CHECK_VALUE(false, "score: expected \"softmax\" or \"sigmoid\", got \"", PyUnicode_AsUTF8(o), "\"");
+    TORCH_CHECK_VALUE(false, "score: expected \"softmax\" or \"sigmoid\", got \"", text(o), "\"");
 }
 int32_t type_of(const char* name, at::ScalarType t) {
     if (t == at::kBFloat16) return MOK_TYPE_BF16;

@@ -69,3 +69,18 @@ def test_experts_scratch_never_shrinks_with_the_batch(mok, E, k, H, I):
     T = 32768 // k
     near = [mok.mok_i8_experts_workspace_bytes(t, H, I, E, k) for t in range(T - 40, T + 40)]
     assert all(a <= b for a, b in zip(near, near[1:]))
+
+
+def test_argument_names_without_a_utf8_form_are_refused(mok):
+    code = """
+from paper_2609_36070_b200 import mok
+try:
+    mok.mok_gate(1, 2, **{chr(0xd800): 3})
+except TypeError as e:
+    assert "unexpected argument" in str(e)
+else:
+    raise AssertionError
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
+    assert done.returncode == 0, (done.returncode, done.stderr)
