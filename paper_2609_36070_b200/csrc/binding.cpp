@@ -221,7 +221,7 @@ PyObject* gate(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
     a.renormalise = truth(c.v[7], true);
     a.scale = (float)number(c.v[8], 1.0);
     TORCH_CHECK_VALUE(logits.size(0) <= INT32_MAX && logits.size(1) <= INT32_MAX, "logits: too large");
-    if (a.k < 0) check(MOK_ERR_SHAPE);
+    if (a.k < 1 || a.k > a.E) check(MOK_ERR_SHAPE);     // (before outputs of that size are allocated)
     at::Tensor idx = make({a.T, a.k}, at::kInt, w.device), weight = make({a.T, a.k}, at::kFloat, w.device);
     a.topk_idx = static_cast<int32_t*>(idx.data_ptr());
     a.topk_w = static_cast<float*>(weight.data_ptr());

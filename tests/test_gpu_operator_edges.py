@@ -347,3 +347,14 @@ def test_gate_of_the_largest_number_of_tokens(mok):
     at = torch.tensor([0, 1, T // 2, T - 2, T - 1], device="cuda")
     assert idx[at, 0].tolist() == [1, 0, 1, 0, 1]
     assert (w[at, 0].double() - torch.tensor([1.0, 0.0, 1.0, 0.0, 1.0], device="cuda", dtype=torch.float64).sigmoid()).abs().max() < 1e-6
+
+
+def test_gate_refuses_k_before_it_allocates(mok):
+    logits = torch.zeros(1 << 16, 8, device="cuda")
+    for k in (9, 1 << 30, 2 ** 31 - 1, 0, -1):
+        with pytest.raises(mok.MokError) as e:
+            mok.mok_gate(logits, k)
+        assert e.value.status == mok.MOK_ERR_SHAPE
+    for k in (2 ** 31, -2 ** 31 - 1):
+        with pytest.raises(ValueError):
+            mok.mok_gate(logits, k)
