@@ -355,7 +355,7 @@ PyObject* matmul(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
     const Weights weights("weights", c.v[2]);
     TORCH_CHECK_VALUE(weights.codes.defined() && weights.codes.dim() == 2 && codes.dim() == 2 && codes.scalar_type() == at::kChar,
                       "codes: expected int8 [M, K] and weights [N, K]");
-    const int64_t K = integer(c.v[3], weights.codes.size(1));
+    const int64_t K = small("K", c.v[3], weights.codes.size(1));
     mok_i8_linear_args a = {};
     a.codes_stride = rows("codes", codes, K, w.device);
     a.x_codes = static_cast<const int8_t*>(codes.data_ptr());

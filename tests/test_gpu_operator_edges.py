@@ -358,3 +358,16 @@ def test_gate_refuses_k_before_it_allocates(mok):
     for k in (2 ** 31, -2 ** 31 - 1):
         with pytest.raises(ValueError):
             mok.mok_gate(logits, k)
+
+
+def test_matmul_refuses_a_contraction_out_of_range(mok):
+    g = gen(1)
+    w = weights(mok, g, 24, 32)
+    codes, scales = torch.zeros(1, 16, dtype=torch.int8, device="cuda"), torch.ones(1, device="cuda")
+    for K in (-2 ** 32 + 32, 2 ** 32 + 16, 2 ** 31, 2 ** 63 - 1, 33, 17):
+        with pytest.raises(ValueError):
+            mok.mok_i8_matmul(codes, scales, w, K=K)
+    for K in (0, -1, -2 ** 31):
+        with pytest.raises(mok.MokError) as e:
+            mok.mok_i8_matmul(codes, scales, w, K=K)
+        assert e.value.status == mok.MOK_ERR_SHAPE
