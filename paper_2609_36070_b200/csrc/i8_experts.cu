@@ -356,7 +356,8 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
         return MOK_ERR_NULL;
     if (!i8::aligned(a->x, 2) || !i8::aligned(a->out, 16) || !i8::aligned(a->add, 16) || !i8::aligned(a->gate_up_codes, 16) ||
         !i8::aligned(a->down_codes, 16) || (a->gate_up_stride % 16) || (a->down_stride % 16) || (a->out_stride % 8) ||
-        (a->add && a->add_stride % 8) || !i8::aligned(a->topk_idx, 4) || !i8::aligned(a->topk_w, 4))
+        (a->add && a->add_stride % 8) || !i8::aligned(a->topk_idx, 4) || !i8::aligned(a->topk_w, 4) ||
+        !i8::aligned(a->gate_up_scales, 4) || !i8::aligned(a->down_scales, 4) || !i8::aligned(a->down_max, 4))
         return MOK_ERR_ALIGN;
     if (!a->workspace || !i8::aligned(a->workspace, 256) || a->workspace_bytes < X.total) return MOK_ERR_WORKSPACE;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);

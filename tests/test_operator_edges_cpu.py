@@ -1,5 +1,6 @@
 """Host side of the routing and 8-bit operators: a missing extension module, scratch sizes, arguments that are refused before
 anything is allocated or launched."""
+import ctypes
 import os
 import shutil
 import subprocess
@@ -84,3 +85,21 @@ else:
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     done = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True)
     assert done.returncode == 0, (done.returncode, done.stderr)
+
+
+class Experts(ctypes.Structure):
+    _fields_ = ([(n, ctypes.c_void_p) for n in ("x", "idx", "w", "gu", "gu_scales", "dn", "dn_scales", "dn_max", "add")] +
+                [(n, ctypes.c_int64) for n in ("x_stride", "gu_stride", "dn_stride", "add_stride", "out_stride")] +
+                [(n, ctypes.c_int32) for n in ("T", "H", "I", "E", "k", "type")] +
+                [("out", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t), ("stream", ctypes.c_void_p)])
+
+
+def test_scales_that_are_not_aligned_are_refused(mok):
+    """(No workspace is given, so that nothing is launched whatever the check of the scales says.)"""
+    from paper_2609_36070_b200 import build
+    lib, A = ctypes.CDLL(build.LIB), 1 << 20              # A stands for an address
+    good = dict(x=A, idx=A, w=A, gu=A, gu_scales=A, dn=A, dn_scales=A, dn_max=A, x_stride=64, gu_stride=64, dn_stride=32, out_stride=64,
+                T=8, H=64, I=32, E=4, k=2, type=0, out=A, workspace=None, workspace_bytes=0)
+    assert lib.mok_i8_experts(ctypes.byref(Experts(**good))) == mok.MOK_ERR_WORKSPACE
+    for name in ("gu_scales", "dn_scales", "dn_max"):
+        assert lib.mok_i8_experts(ctypes.byref(Experts(**{**good, name: A + 2}))) == mok.MOK_ERR_ALIGN, name
