@@ -540,7 +540,7 @@ int mok_gate_backward(const mok_gate_bwd_args* args);
 /*
  * Products in 8-bit integers, one scale per token and one per output channel (the paper's low-precision mode is MXFP8,
  * Section 3.4; this is the form that weight-and-activation quantised checkpoints come in).
- *   codes   : int8 in -127 .. 127, rows of `stride` bytes (a multiple of 16 for the products; bytes past K are not read).
+ *   codes   : int8 in -127 .. 127, rows of `stride` bytes (a multiple of 16 where a product has several; bytes past K are not read).
  *             mok_i8_quantize sets the bytes from K up to the next multiple of 16 to 0, as far as codes_stride reaches, and
  *             leaves what follows alone
  *   quantise: scale = amax / 127, code = round(127 x / amax) in fp32, ties to even; a row of zeros has scale 0, a row with

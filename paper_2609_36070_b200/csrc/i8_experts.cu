@@ -285,14 +285,15 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
     if (a->M < 0 || a->K < 1 || a->K > i8::MAX_CONTRACTION || a->N < 1 || !i8::type_ok(a->out_type) ||
         (!coded && !i8::type_ok(a->x_type)))
         return MOK_ERR_SHAPE;
-    if ((a->M > 1 && ((coded ? a->codes_stride : a->x_stride) < a->K || a->out_stride < a->N)) || a->w_stride < a->K)
+    // (strides of single rows do not count)
+    if ((a->M > 1 && ((coded ? a->codes_stride : a->x_stride) < a->K || a->out_stride < a->N)) || (a->N > 1 && a->w_stride < a->K))
         return MOK_ERR_SHAPE;
     if (a->M == 0) return MOK_OK;
     if ((!a->x && !a->x_codes) || (coded && !a->x_scales) || !a->W_codes || !a->W_scales || !a->out) return MOK_ERR_NULL;
-    if (!i8::aligned(a->W_codes, 16) || (a->w_stride % 16) || !i8::aligned(a->W_scales, 4) || !i8::aligned(a->bias, 4) ||
+    if (!i8::aligned(a->W_codes, 16) || (a->N > 1 && a->w_stride % 16) || !i8::aligned(a->W_scales, 4) || !i8::aligned(a->bias, 4) ||
         !i8::aligned(a->out, i8::type_bytes(a->out_type)))
         return MOK_ERR_ALIGN;
-    if (coded ? !i8::aligned(a->x_codes, 16) || (a->codes_stride % 16) || !i8::aligned(a->x_scales, 4)
+    if (coded ? !i8::aligned(a->x_codes, 16) || (a->M > 1 && a->codes_stride % 16) || !i8::aligned(a->x_scales, 4)
               : !i8::aligned(a->x, i8::type_bytes(a->x_type)))
         return MOK_ERR_ALIGN;
     cudaStream_t s = reinterpret_cast<cudaStream_t>(a->stream);
@@ -302,7 +303,7 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
     if (e != cudaSuccess) return cuda_fail(e);
     g.a_rows = a->M;
     g.B = a->W_codes;
-    g.ldb = a->w_stride;
+    g.ldb = a->N > 1 ? a->w_stride : i8::pitch_of(a->K);
     g.b_scale = a->W_scales;
     g.bias = a->bias;
     g.K = a->K; g.N = a->N; g.E = 1;
@@ -315,7 +316,7 @@ int mok_i8_linear(const mok_i8_linear_args* a) {
     const bool narrow = i8::narrow_product(a->M, a->K, a->N, coded ? -1 : a->x_type, x_alignment(a), &quantises);
     if (coded) {
         g.A = a->x_codes;
-        g.lda = a->codes_stride;
+        g.lda = a->M > 1 ? a->codes_stride : i8::pitch_of(a->K);
         g.a_scale = a->x_scales;
     } else {
         if (narrow && quantises) {

@@ -371,3 +371,16 @@ def test_matmul_refuses_a_contraction_out_of_range(mok):
         with pytest.raises(mok.MokError) as e:
             mok.mok_i8_matmul(codes, scales, w, K=K)
         assert e.value.status == mok.MOK_ERR_SHAPE
+
+
+@pytest.mark.parametrize("K", [16, 100, 2049])
+def test_products_of_single_rows(mok, K):
+    """One token's codes, or one channel's, need no pitch of whole 16 bytes."""
+    g = gen(K)
+    for M, N in ((1, 40), (1, 1), (300, 1)):
+        codes = torch.randint(-127, 128, (M, K if M == 1 else (K + 15) // 16 * 16), generator=g, device="cuda", dtype=torch.int8)
+        wide = torch.randint(-127, 128, (N, K if N == 1 else (K + 15) // 16 * 16), generator=g, device="cuda", dtype=torch.int8)
+        s, ws = torch.rand(M, generator=g, device="cuda"), torch.rand(N, generator=g, device="cuda")
+        out = mok.mok_i8_matmul(codes, s, mok.I8Weights(wide, ws), K=K, out_dtype=torch.float32)
+        ref = (codes[:, :K].double() @ wide[:, :K].double().t()) * s.double()[:, None] * ws.double()
+        assert ((out.double() - ref).abs() <= 4 * UNIT[torch.float32] * ref.abs()).all()
