@@ -384,3 +384,74 @@ def test_products_of_single_rows(mok, K):
         out = mok.mok_i8_matmul(codes, s, mok.I8Weights(wide, ws), K=K, out_dtype=torch.float32)
         ref = (codes[:, :K].double() @ wide[:, :K].double().t()) * s.double()[:, None] * ws.double()
         assert ((out.double() - ref).abs() <= 4 * UNIT[torch.float32] * ref.abs()).all()
+
+
+# ------------------------------------------------------------------------------ aligned rows of every width, large batches
+
+@pytest.mark.parametrize("T", [70, 2500])
+@pytest.mark.parametrize("E,G,top_groups,k", [(28, 1, 1, 6), (64, 1, 1, 6), (128, 1, 1, 8), (160, 8, 3, 6), (192, 1, 1, 12), (256, 8, 4, 8),
+                                              (256, 1, 1, 8), (256, 1, 1, 2), (256, 1, 1, 20), (320, 10, 4, 9), (384, 1, 1, 8), (384, 4, 2, 8),
+                                              (512, 1, 1, 10), (512, 16, 6, 8)])
+@pytest.mark.parametrize("dtype,score,with_bias,renorm", [(torch.float32, "sigmoid", True, True), (torch.bfloat16, "softmax", False, True),
+                                                          (torch.float16, "softmax", True, False), (torch.float32, "softmax", False, False)])
+def test_gate_of_aligned_rows(mok, T, E, G, top_groups, k, dtype, score, with_bias, renorm):
+    g = gen(E + k)
+    logits = (randn(g, T, E) * 1.5).to(dtype)
+    bias = randn(g, E) * 0.05 if with_bias else None
+    idx, w = mok.mok_gate(logits, k, bias=bias, score=score, n_groups=G, topk_groups=top_groups, group_top=2, renormalise=renorm, scale=2.5)
+    z = logits.double()
+    s = torch.sigmoid(z) if score == "sigmoid" else torch.softmax(z, -1)
+    by_score = with_bias or G > 1
+    c = s + bias.double() if with_bias else s if by_score else z
+    grouped = torch.ones(T, dtype=torch.bool, device="cuda")                               # tokens whose groups fp32 cannot mistake
+    if G > 1:
+        value = c.view(T, G, E // G).topk(2, -1).values.sum(-1)
+        order = value.sort(dim=-1, descending=True, stable=True)
+        grouped = order.values[:, top_groups - 1] - order.values[:, top_groups] > 1e-6
+        keep = torch.zeros(T, G, dtype=torch.bool, device="cuda").scatter_(1, order.indices[:, :top_groups], True)
+        c = c.masked_fill(~keep.repeat_interleave(E // G, 1), -math.inf)
+    order = c.sort(dim=-1, descending=True, stable=True)
+    assert grouped.float().mean() > 0.97
+    assert (c.gather(1, idx.long()) - order.values[:, :k])[grouped].abs().max() <= 1e-6
+    clear = grouped                                        # logits are compared as they are, fp32 decides closer scores
+    if by_score:
+        clear = grouped & (order.values[:, :k] - order.values[:, 1:k + 1] > 1e-6).all(-1)
+    assert torch.equal(idx.long()[clear], order.indices[:, :k][clear])
+    ref = s.gather(1, idx.long())
+    ref = 2.5 * (ref / ref.sum(-1, keepdim=True) if renorm else ref)
+    # exponentials, sums of up to 512 terms in lanes of 16 and a tree, quotients: less than 64 roundings
+    assert ((w.double() - ref).abs() <= 64 * UNIT[torch.float32] * ref).all()
+
+
+@pytest.mark.parametrize("T,E,k", [(300, 64, 4), (301, 128, 8), (302, 256, 8), (303, 384, 6), (304, 512, 16), (200_001, 8, 2), (160_000, 36, 4)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("score,renorm", [("softmax", False), ("softmax", True), ("sigmoid", True), ("sigmoid", False)])
+def test_gate_gradient_of_aligned_rows(mok, T, E, k, dtype, score, renorm):
+    g = gen(E + k)
+    logits = randn(g, T, E).to(dtype)
+    idx, _ = mok.mok_gate(logits, k, score=score, renormalise=renorm)
+    dw = randn(g, T, k)
+    d = mok.mok_gate_backward(logits, idx, dw, score=score, renormalise=renorm, scale=1.7)
+    z = logits.double().requires_grad_()
+    s = torch.sigmoid(z) if score == "sigmoid" else torch.softmax(z, -1)
+    w = s.gather(1, idx.long())
+    ref, = torch.autograd.grad((w / w.sum(-1, keepdim=True) if renorm else w) * 1.7, z, dw.double())
+    # as for rows of any alignment: 64 roundings of the token's largest |g|
+    room = 64 * UNIT[torch.float32] * 1.7 * dw.abs().amax(-1, keepdim=True).double()
+    assert ((d.double() - ref).abs() <= UNIT[dtype] * ref.abs() + room).all()
+
+
+@pytest.mark.parametrize("M,K,N", [(2049, 256, 520), (2305, 130, 1000), (4100, 384, 72), (7000, 64, 300), (16384, 512, 256)])
+@pytest.mark.parametrize("dtype,out_dtype", [(torch.bfloat16, torch.bfloat16), (torch.float32, torch.float32)])
+def test_linear_of_many_rows(mok, M, K, N, dtype, out_dtype):
+    """Row tiles past the first group of 2048 rows, with and without a bias."""
+    g = gen(M)
+    x, w, bias = randn(g, M, K).to(dtype), weights(mok, g, N, K), randn(g, N)
+    codes, scales = mok.mok_i8_quantize(x)
+    for b in (None, bias):
+        out = mok.mok_i8_linear(x, w, bias=b, out_dtype=out_dtype)
+        ref = (codes[:, :K].double() @ w.codes[:, :K].double().t()) * scales.double()[:, None] * w.scales.double()
+        room = 4 * UNIT[torch.float32] * ref.abs()
+        if b is not None:
+            ref, room = ref + b.double(), room + 4 * UNIT[torch.float32] * b.double().abs()
+        assert ((out.double() - ref).abs() <= UNIT[out_dtype] * ref.abs() + room).all()
