@@ -604,6 +604,10 @@ int mok_i8_experts(const mok_i8_experts_args* args);
 /* Status word of the 8-bit products on the current device (one for all of them, kept until it is read): synchronises
  * `stream`, returns MOK_OK or MOK_ERR_TIMEOUT (a bounded wait ran out) and clears it. */
 int mok_i8_status(void* stream);
+/* Test hook.  wait_limit_us > 0: the products that this thread launches from now on load nothing, and waits on the current device
+ * run out after that time, so that the calls end without a result and leave MOK_ERR_TIMEOUT; 0: both as usual.  Synchronises
+ * `stream`. */
+int mok_i8_starve(int wait_limit_us, void* stream);
 
 /*
  * Reads the device-side status word of a workspace after synchronising `stream` -- the only call besides

@@ -217,7 +217,7 @@ product_pair_kernel(const __grid_constant__ CUtensorMap tmapA, const __grid_cons
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
-        if (lane == 0) {
+        if (lane == 0 && !a.starve) {
             int s = 0;
             uint32_t ph = 0;
             PairTile next = {};
@@ -465,6 +465,7 @@ cudaError_t launch_product(const ProductArgs& args, int epi, cudaStream_t s) {
     ProductArgs a = args;
     const bool gated = epi == EPI_GATED;
     a.bn = epi == EPI_PLAIN ? pair_columns(a.dense_rows, a.N) : BN;
+    a.starve = g_starve;
     CUtensorMap mA, mB, mC;
     if (!byte_map(&mA, a.A, a.a_rows, a.K, a.lda, BM) ||
         !byte_map(&mB, a.B, (long long)a.E * (gated ? 2 : 1) * a.N, a.K, a.ldb, (uint32_t)a.bn / 2))

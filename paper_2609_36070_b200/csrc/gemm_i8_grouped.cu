@@ -93,7 +93,7 @@ product_grouped_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_c
     const int total = n_mt * n_nt;
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (lane == 0 && !a.starve) {
             int s = 0;
             uint32_t ph = 0;
             RowTile next = {};
@@ -256,7 +256,9 @@ static cudaError_t launch_grouped_epi(const CUtensorMap& mW, const CUtensorMap (
                       mX[1], mX[2], mX[3], a, n_nt, k_blocks);
 }
 
-cudaError_t launch_grouped(const ProductArgs& a, int epi, cudaStream_t s) {
+cudaError_t launch_grouped(const ProductArgs& args, int epi, cudaStream_t s) {
+    ProductArgs a = args;
+    a.starve = g_starve;
     const bool is_gated = epi == EPI_GATED;
     CUtensorMap mW, mX[4];
     auto map = [&](CUtensorMap* m, const void* p, long long rows, long long pitch, uint32_t box) {

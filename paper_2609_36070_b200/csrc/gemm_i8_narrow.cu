@@ -66,6 +66,7 @@ struct NarrowArgs {
     int32_t M, K, N;
     int32_t bn;                  // columns of the MMA: 16, 32, 64, 128 or 256
     int32_t stages;
+    int32_t starve;              // (see ProductArgs)
     const float* w_scale;
     const float* bias;
     void* out;
@@ -184,6 +185,7 @@ product_narrow_kernel(const __grid_constant__ CUtensorMap tmapW, const __grid_co
     // the first stages of the weights are on their way before the tokens are looked at
     const int ahead = n_kb < a.stages ? n_kb : a.stages;
     auto load = [&](int s, int kb) {
+        if (a.starve) return;
         const uint32_t full = smem_u32(&ctrl->full[s]);
         mbar_expect_tx(full, stage_bytes);
         tma_load_2d(base + s * stage_bytes, &tmapW, full, (kb0 + kb) * 128, tile * 128);
@@ -422,6 +424,7 @@ cudaError_t launch_narrow(const ProductArgs& g, const void* x, int x_type, long 
     const size_t smem = shape.smem;
     a.bn = shape.bn;
     a.stages = shape.stages;
+    a.starve = g_starve;
     a.x = x;
     a.ldx = ldx;
     a.scales = g.a_scale;

@@ -84,6 +84,7 @@ struct ProductArgs {
     int32_t max_mt;              // at most
     int32_t c_mapped;            // set by the launcher: C is stored through a tensor map
     int32_t bn;                  // set by the launcher: columns of a plain tile
+    int32_t starve;              // test hook (set by the launchers): nothing is loaded, so the waits run out
     WsHeader* header;
 };
 enum { EPI_PLAIN = 0, EPI_GATED = 1, EPI_ROWS = 2 };
@@ -112,6 +113,7 @@ cudaError_t launch_grouped(const ProductArgs& a, int epi, cudaStream_t s);
 bool narrow_product(int M, int K, int N, int x_type, unsigned long long x_align, bool* quantises);
 cudaError_t launch_narrow(const ProductArgs& a, const void* x, int x_type, long long ldx, cudaStream_t s);
 cudaError_t status_header(WsHeader** out);
+extern thread_local bool g_starve;    // this thread's launches of products load nothing (mok_i8_starve)
 
 }  // namespace i8
 }  // namespace mok

@@ -179,6 +179,8 @@ schedule_one_kernel(const int32_t* __restrict__ idx, int n, int E, int tile_rows
     }
 }
 
+thread_local bool g_starve = false;
+
 static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // Workspace of the routed experts: the schedule's tables (a WsLayout of which only those are set) and the activations.
@@ -434,6 +436,20 @@ int mok_i8_experts(const mok_i8_experts_args* a) {
     if (e != cudaSuccess) return cuda_fail(e);
     e = a->type == MOK_TYPE_BF16 ? i8::launch_combine<__nv_bfloat16>(a, X, ws, s) : i8::launch_combine<__half>(a, X, ws, s);
     return e == cudaSuccess ? MOK_OK : cuda_fail(e);
+}
+
+int mok_i8_starve(int wait_limit_us, void* stream) {
+    if (wait_limit_us < 0) return MOK_ERR_SHAPE;
+    WsHeader* hdr = nullptr;
+    cudaError_t e = i8::status_header(&hdr);
+    if (e != cudaSuccess) return cuda_fail(e);
+    cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
+    const uint32_t limit = (uint32_t)wait_limit_us;
+    if ((e = cudaMemcpyAsync(&hdr->wait_limit_us, &limit, sizeof(limit), cudaMemcpyHostToDevice, s)) != cudaSuccess ||
+        (e = cudaStreamSynchronize(s)) != cudaSuccess)
+        return cuda_fail(e);
+    i8::g_starve = wait_limit_us > 0;
+    return MOK_OK;
 }
 
 int mok_i8_status(void* stream) {

@@ -33,7 +33,7 @@ EXPORTS = ["mok_moe_forward", "mok_workspace_bytes", "mok_workspace_bytes_ring",
            "mok_ep_expert_bwd", "mok_ep_bwd_combine", "mok_selftest_per_device",
            "mok_router_prepared_bytes", "mok_router_prepare", "mok_gate", "mok_gate_backward", "mok_i8_quantize",
            "mok_i8_linear_workspace_bytes", "mok_i8_linear", "mok_i8_experts_workspace_bytes", "mok_i8_experts",
-           "mok_i8_status"]
+           "mok_i8_status", "mok_i8_starve"]
 MOK_PRECISION_BF16, MOK_PRECISION_MXFP8 = 0, 1
 MOK_H_RING_MIN_TILES = 24
 MOK_MAX_RANKS = 16
@@ -136,6 +136,8 @@ _lib.mok_i8_experts_workspace_bytes.restype = ctypes.c_size_t
 _lib.mok_i8_experts_workspace_bytes.argtypes = [ctypes.c_int] * 5
 _lib.mok_i8_status.restype = ctypes.c_int
 _lib.mok_i8_status.argtypes = [ctypes.c_void_p]
+_lib.mok_i8_starve.restype = ctypes.c_int
+_lib.mok_i8_starve.argtypes = [ctypes.c_int, ctypes.c_void_p]
 _lib.mok_bwd_workspace_bytes.restype = ctypes.c_size_t
 _lib.mok_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 6
 _lib.mok_moe_backward.restype = ctypes.c_int
@@ -719,6 +721,11 @@ def mok_i8_experts_workspace_bytes(T, H, I, E, k):
 def mok_i8_status(stream=None):
     """Status of the 8-bit products on the current device since it was last read (synchronises the stream)."""
     return int(_lib.mok_i8_status(_stream(stream)))
+
+
+def mok_i8_starve(wait_limit_us, stream=None):
+    """Test hook: products that load nothing and give up after that time; 0: as usual."""
+    _check(_lib.mok_i8_starve(wait_limit_us, _stream(stream)))
 
 
 DEBUG_COUNTERS = ["mma_wait_operands", "mma_wait_peer_operands", "mma_wait_accumulator", "mma_total", "k_blocks",

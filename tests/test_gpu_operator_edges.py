@@ -455,3 +455,36 @@ def test_linear_of_many_rows(mok, M, K, N, dtype, out_dtype):
         if b is not None:
             ref, room = ref + b.double(), room + 4 * UNIT[torch.float32] * b.double().abs()
         assert ((out.double() - ref).abs() <= UNIT[out_dtype] * ref.abs() + room).all()
+
+
+# ------------------------------------------------------------------------------------------------------ bounded waits
+
+def test_waits_of_the_products_run_out(mok):
+    """Products whose loads never come end with a status, and the next calls are as before: few tokens (quantised in the kernel,
+    and codes), pairs of CTAs, experts with few and with many rows, of all tile sizes."""
+    g = gen(5)
+    lin, wide = weights(mok, g, 640, 512), weights(mok, g, 4096, 1024)
+    gu, dn = weights(mok, g, 4, 128, 512), weights(mok, g, 4, 512, 64)
+    x = {T: randn(g, T, 512).bfloat16() for T in (3, 100, 150, 600)}
+    many = randn(g, 1500, 1024).bfloat16()
+    r = {T: routes(g, T, 4, 2) for T in x}
+
+    def calls():
+        yield lambda: mok.mok_i8_linear(x[3], lin)
+        yield lambda: mok.mok_i8_linear(x[150], lin)
+        yield lambda: mok.mok_i8_linear(many, wide)
+        for T in (3, 100, 150, 600):
+            yield lambda: mok.mok_i8_experts(x[T], *r[T], gu, dn)
+
+    good = [call() for call in calls()]
+    assert mok.mok_i8_status() == mok.MOK_OK
+    try:
+        for call in calls():
+            mok.mok_i8_starve(20_000)
+            call()
+            assert mok.mok_i8_status() == mok.MOK_ERR_TIMEOUT
+            assert mok.mok_i8_status() == mok.MOK_OK       # read once
+    finally:
+        mok.mok_i8_starve(0)
+    assert all(torch.equal(a, call()) for a, call in zip(good, calls()))
+    assert mok.mok_i8_status() == mok.MOK_OK
