@@ -39,7 +39,7 @@ constexpr int SCALE_REGION = SLAB_REGION + EPI_WARPS * 2 * SLAB_BYTES;      // p
 constexpr int CTRL_REGION = SCALE_REGION + EPI_WARPS * 256;
 constexpr int SMEM_BYTES = CTRL_REGION + 256;
 constexpr int TMEM_COLS = 512;
-constexpr int THREADS = 64 + 32 * EPI_WARPS;     // + one gather warp
+constexpr int THREADS = 64 + 32 * EPI_WARPS;
 constexpr int GROUP_ROWS = 2048;
 
 struct Ctrl {

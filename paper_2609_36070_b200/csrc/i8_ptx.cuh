@@ -22,8 +22,10 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, uint32_t (&r)[16]) {
         : "r"(taddr) : "memory");
 }
 
-// silu(g) u.  The exponential and the quotient are good to about 2^-21: what follows is a rounding to 8-bit codes, which an
-// 11-bit tanh would move in one case of fifty.
+// silu(g) u.  The exponential is off by (2 + 1.2 |g|) 2^-23 of itself, the quotient by 2^-22: no more than what the three
+// roundings of g to fp32 leave open (|g| 2^-22 of silu(g) for negative g, where it counts), and far below the rounding to 8-bit
+// codes that follows, which an 11-bit tanh would move in one case of fifty.  (expf and an exact division: 131072 rows of 768
+// from 2048 in 403 instead of 312 us.)
 __device__ __forceinline__ float gated(float g, float u) { return __fdividef(g, 1.f + __expf(-g)) * u; }
 
 }  // namespace i8
