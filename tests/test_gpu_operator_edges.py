@@ -488,3 +488,25 @@ def test_waits_of_the_products_run_out(mok):
         mok.mok_i8_starve(0)
     assert all(torch.equal(a, call()) for a, call in zip(good, calls()))
     assert mok.mok_i8_status() == mok.MOK_OK
+
+
+@pytest.mark.parametrize("H,I,E,k", [(256, 64, 4, 2), (136, 200, 16, 4)])
+def test_experts_give_a_token_the_same_bits_in_any_batch(mok, H, I, E, k):
+    g = gen(H)
+    T = 9000
+    x, (idx, w) = randn(g, T, H).half(), routes(g, T, E, k)
+    idx[::7, 0] = -1
+    gu, dn = weights(mok, g, E, 2 * I, H), weights(mok, g, E, H, I)
+    whole = mok.mok_i8_experts(x, idx, w, gu, dn)
+    for n in (1, 40, 100, 300, 900, 4000):
+        assert torch.equal(mok.mok_i8_experts(x[:n], idx[:n].contiguous(), w[:n].contiguous(), gu, dn), whole[:n]), n
+
+
+@pytest.mark.parametrize("K,N", [(1040, 520), (256, 2000)])
+def test_linear_gives_a_token_the_same_bits_in_any_batch(mok, K, N):
+    g = gen(K)
+    x, w, bias = randn(g, 6000, K).bfloat16(), weights(mok, g, N, K), randn(g, N)
+    for b in (None, bias):
+        whole = mok.mok_i8_linear(x, w, bias=b, out_dtype=torch.float32)
+        for n in (1, 16, 40, 128, 256, 400, 2500):
+            assert torch.equal(mok.mok_i8_linear(x[:n], w, bias=b, out_dtype=torch.float32), whole[:n]), n
