@@ -111,8 +111,8 @@ __device__ __forceinline__ float sum8(float v) {
     for (int off = 1; off < 8; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
 }
-// exp(l - m), 0 where everything is masked (m = -inf)
-__device__ __forceinline__ float exp_below(float l, float m) { return m == -INFINITY ? 0.f : expf(l - m); }
+// What a row's exponentials are taken from: its maximum, 0 where everything is masked (so that they are 0), or NaN.
+__device__ __forceinline__ float exp_from(float m) { return m == -INFINITY ? 0.f : m; }
 
 struct Params {
     const void* logits;
@@ -156,19 +156,20 @@ gate_warp_kernel(const Params p) {
         if (p.softmax) {
 #pragma unroll
             for (int j = 0; j < VPL; ++j) m = fmaxf(m, c[j]);
-            m = warp_max(m);
+            m = exp_from(warp_max(m));
         }
         if (full_sum) {
             float sum = 0.f;
 #pragma unroll
-            for (int j = 0; j < VPL; ++j) sum += exp_below(c[j], m);
-            total = m == -INFINITY ? 1.f : warp_sum(sum);
+            for (int j = 0; j < VPL; ++j) sum += expf(c[j] - m);
+            sum = warp_sum(sum);
+            total = sum == 0.f ? 1.f : sum;
         }
         if (by_score) {
             const float inv = 1.f / total;
 #pragma unroll
             for (int j = 0; j < VPL; ++j) {
-                const float s = p.softmax ? __fmul_rn(exp_below(c[j], m), inv) : sigmoid_near(c[j]);
+                const float s = p.softmax ? __fmul_rn(expf(c[j] - m), inv) : sigmoid_near(c[j]);
                 c[j] = c[j] == -INFINITY ? -INFINITY : __fadd_rn(s, bias[j]);  // (absent, or not to be used whatever its bias)
             }
         }
@@ -236,7 +237,7 @@ gate_warp_kernel(const Params p) {
         float s = 0.f;
         if (lane < k) {
             const float l = load_f(row + my_e);
-            s = !p.softmax ? sigmoid(l) : full_sum ? exp_below(l, m) / total : exp_below(l, m);
+            s = !p.softmax ? sigmoid(l) : full_sum ? expf(l - m) / total : expf(l - m);
         }
         if (p.renormalise) {
             float sum = s + __shfl_xor_sync(0xffffffffu, s, 8);      // (the order of the four-token kernel again)
@@ -330,7 +331,7 @@ gate_kernel(const Params p) {
         if (p.softmax) {
 #pragma unroll
             for (int i = 0; i < NI; ++i) m = fmaxf(m, fmaxf(fmaxf(c[i][0], c[i][1]), fmaxf(c[i][2], c[i][3])));
-            m = max8(m);
+            m = exp_from(max8(m));
         }
         if (full_sum) {
             float part[4] = {0.f, 0.f, 0.f, 0.f};
@@ -338,12 +339,12 @@ gate_kernel(const Params p) {
             for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float x = exp_below(c[i][j], m);
+                    const float x = expf(c[i][j] - m);
                     part[j] += x;
                     if (by_score) c[i][j] = x;
                 }
             const float sum = sum8((part[0] + part[1]) + (part[2] + part[3]));
-            total = m == -INFINITY ? 1.f : sum;
+            total = sum == 0.f ? 1.f : sum;
         }
         if (by_score) {
             const float inv = 1.f / total;
@@ -570,7 +571,7 @@ gate_kernel(const Params p) {
             s[q] = 0.f;
             if (8 * q + sub < k) {
                 const float l = load_f(row + chosen[8 * q + sub]);
-                s[q] = !p.softmax ? sigmoid(l) : full_sum ? exp_below(l, m) / total : exp_below(l, m);
+                s[q] = !p.softmax ? sigmoid(l) : full_sum ? expf(l - m) / total : expf(l - m);
             }
         }
         if (p.renormalise) {
@@ -649,12 +650,12 @@ gate_backward_kernel(const BwdParams p) {
             if (p.softmax) {
 #pragma unroll
                 for (int q = 0; q < SLOTS; ++q) m = fmaxf(m, e[q] >= 0 ? l[q] : -INFINITY);
-                m = max8(m);
+                m = exp_from(max8(m));
             }
 #pragma unroll
             for (int q = 0; q < SLOTS; ++q) {
                 s[q] = 0.f;
-                if (e[q] >= 0) s[q] = p.softmax ? exp_below(l[q], m) : sigmoid(l[q]);
+                if (e[q] >= 0) s[q] = p.softmax ? expf(l[q] - m) : sigmoid(l[q]);
                 total += s[q];
             }
             if (p.renormalise) {                     // (the scores are divided, not their sum inverted: it may be subnormal)
@@ -695,20 +696,20 @@ gate_backward_kernel(const BwdParams p) {
             for (int i = 0; i < NI; ++i) load4<VEC>(row, (sub + 8 * i) * 4, E, c[i]);
 #pragma unroll
             for (int i = 0; i < NI; ++i) m = fmaxf(m, fmaxf(fmaxf(c[i][0], c[i][1]), fmaxf(c[i][2], c[i][3])));
-            m = max8(m);
+            m = exp_from(max8(m));
 #pragma unroll
             for (int i = 0; i < NI; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    c[i][j] = exp_below(c[i][j], m);
+                    c[i][j] = expf(c[i][j] - m);
                     sum += c[i][j];
                 }
             sum = sum8(sum);
-            const float inv = sum > 0.f ? 1.f / sum : 0.f;
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
             for (int q = 0; q < SLOTS; ++q) {
                 if (e[q] < 0) continue;
-                dot += g[q] * exp_below(l[q], m) * inv;
+                dot += g[q] * expf(l[q] - m) * inv;
                 mine[e[q]] = g[q];
             }
             dot = sum8(dot);

@@ -510,3 +510,28 @@ def test_linear_gives_a_token_the_same_bits_in_any_batch(mok, K, N):
         whole = mok.mok_i8_linear(x, w, bias=b, out_dtype=torch.float32)
         for n in (1, 16, 40, 128, 256, 400, 2500):
             assert torch.equal(mok.mok_i8_linear(x[:n], w, bias=b, out_dtype=torch.float32), whole[:n]), n
+
+
+@pytest.mark.parametrize("T", [33, 2433])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("with_bias", [False, True])
+@pytest.mark.parametrize("E,G", [(40, 1), (64, 8)])
+def test_gate_nan_rows_are_not_taken_for_masked_ones(mok, T, score, with_bias, E, G):
+    """A NaN reaches its token's weights and gradients, also where nothing but NaN and masks is left."""
+    k = 6
+    logits = randn(gen(E), T, E)
+    logits[0] = math.nan
+    logits[1], logits[1, 1::2] = math.nan, -math.inf
+    logits[2, 11] = math.nan
+    logits[3] = -math.inf
+    bias = torch.zeros(E, device="cuda") if with_bias else None
+    for renorm in (True, False):
+        kw = dict(score=score, renormalise=renorm)
+        idx, w = mok.mok_gate(logits, k, bias=bias, n_groups=G, topk_groups=G, **kw)
+        assert torch.equal(idx[0], torch.arange(k, device="cuda", dtype=torch.int32)) and torch.isnan(w[0]).all()
+        assert (w[3] == 0).all() and torch.isfinite(w[4:]).all()
+        every = torch.arange(k, device="cuda", dtype=torch.int32).expand(T, k).contiguous()
+        d = mok.mok_gate_backward(logits, every, torch.ones(T, k, device="cuda") * torch.arange(k, device="cuda"), **kw)
+        assert torch.isnan(d[0, 1:k]).all() and torch.isfinite(d[3:]).all()
+        if score == "softmax" and not renorm:
+            assert torch.isnan(w[2]).all() and torch.isnan(d[:3]).all()
