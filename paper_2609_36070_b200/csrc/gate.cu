@@ -111,6 +111,10 @@ __device__ __forceinline__ float sum8(float v) {
     for (int off = 1; off < 8; off <<= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
 }
+// 1 / sum where that is finite: a sum of subnormal scores, and the scores, are multiplied by lift(sum) first.  (One quotient for
+// all scores: a quotient for each was 3 to 12 % slower.)
+__device__ __forceinline__ float lift(float sum) { return sum < 0x1p-64f ? 0x1p+64f : 1.f; }
+__device__ __forceinline__ float inverse(float sum, float up) { return sum == 0.f ? 0.f : 1.f / (sum * up); }
 // What a row's exponentials are taken from: its maximum, 0 where everything is masked (so that they are 0), or NaN.
 __device__ __forceinline__ float exp_from(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -242,7 +246,8 @@ gate_warp_kernel(const Params p) {
         if (p.renormalise) {
             float sum = s + __shfl_xor_sync(0xffffffffu, s, 8);      // (the order of the four-token kernel again)
             sum = sum8(sum + __shfl_xor_sync(0xffffffffu, sum, 16));
-            s = sum == 0.f ? 0.f : s / sum;
+            const float up = lift(sum);
+            s = s * up * inverse(sum, up);
         }
         if (lane < k) {
             p.idx[(size_t)t * k + lane] = my_e;
@@ -575,11 +580,10 @@ gate_kernel(const Params p) {
             }
         }
         if (p.renormalise) {
-            // (the scores are divided first: scale / sum is infinite for a sum of subnormal scores)
             const float sum = sum8((s[0] + s[1]) + (s[2] + s[3]));
+            const float up = lift(sum), inv = inverse(sum, up);
 #pragma unroll
-            for (int q = 0; q < MAX_K / 8; ++q)
-                if (8 * q < k) s[q] = sum == 0.f ? 0.f : s[q] / sum;
+            for (int q = 0; q < MAX_K / 8; ++q) s[q] = s[q] * up * inv;
         }
 #pragma unroll
         for (int q = 0; q < MAX_K / 8; ++q) {
@@ -658,11 +662,12 @@ gate_backward_kernel(const BwdParams p) {
                 if (e[q] >= 0) s[q] = p.softmax ? expf(l[q] - m) : sigmoid(l[q]);
                 total += s[q];
             }
-            if (p.renormalise) {                     // (the scores are divided, not their sum inverted: it may be subnormal)
+            if (p.renormalise) {
                 total = sum8(total);
+                const float up = lift(total), inv = inverse(total, up);
 #pragma unroll
                 for (int q = 0; q < SLOTS; ++q) {
-                    if (8 * q < k) s[q] = total == 0.f ? 0.f : s[q] / total;
+                    s[q] = s[q] * up * inv;
                     dot += g[q] * s[q];
                 }
                 dot = sum8(dot);
