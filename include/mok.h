@@ -498,7 +498,7 @@ int mok_ep_bwd_combine(const mok_ep_bwd_combine_args* args);
  *     topk_w   = scale * s_i / sum_j s_j over the chosen (renormalise != 0; 0 where that sum is 0), or scale * s_i
  * Without a bias, and unless sums of two scores are compared, the logits themselves are compared.  Logits of -inf are
  * experts that a token may not use, whatever their bias (a token whose logits are all -inf gets weights of 0); NaN logits rank below -inf
- * and reach their own token's weights only; fp32 logits below -3.402823e38 count as equal.  The ids are always k distinct
+ * and reach their own token's weights (and gradients) only; fp32 logits below -3.402823e38 count as equal.  The ids are always k distinct
  * ones in 0 .. E-1.  A token's ids and weights have the same bits in any batch.  Scores are compared in fp32, each within
  * 2^-21 of its exact value.
  * Limits: E <= 512, k <= 32, n_groups <= 32 and a divisor of E, k <= topk_groups * E / n_groups.

@@ -199,7 +199,8 @@ const char GATE_DOC[] =
     "mok_gate(logits, k, bias=None, score='softmax', n_groups=1, topk_groups=1, group_top=2, renormalise=True, scale=1.0, stream=None)\n"
     "--\n\n"
     "Routing from logits [T, E] (bf16, fp16 or fp32): returns (topk_idx int32 [T, k], topk_w fp32 [T, k]).  score: 'softmax' or\n"
-    "'sigmoid'; bias fp32 [E] takes part in the selection only; see include/mok.h for groups and weights.";
+    "'sigmoid'; bias fp32 [E] takes part in the selection only; see include/mok.h for groups and weights.  Outside of autograd,\n"
+    "like the layer's own calls: logits that require a gradient get theirs from mok_gate_backward.";
 PyObject* gate(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
     HANDLE_TH_ERRORS
     static const char* const names[] = {"logits", "k", "bias", "score", "n_groups", "topk_groups", "group_top", "renormalise", "scale", "stream"};
@@ -238,7 +239,8 @@ PyObject* gate(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
 const char GATE_BACKWARD_DOC[] =
     "mok_gate_backward(logits, topk_idx, dw, score='softmax', renormalise=True, scale=1.0, stream=None)\n"
     "--\n\n"
-    "dL/dlogits [T, E] (in the logits' type) from dL/dtopk_w (dw) and the chosen experts of mok_gate.";
+    "dL/dlogits [T, E] (in the logits' type) from dL/dtopk_w (dw) and the chosen experts of mok_gate.\n"
+    "In a torch.autograd.Function it is the backward of mok_gate's weights.";
 PyObject* gate_backward(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
     HANDLE_TH_ERRORS
     static const char* const names[] = {"logits", "topk_idx", "dw", "score", "renormalise", "scale", "stream"};

@@ -20,10 +20,11 @@
 //   - rounds (small k, where they are cheaper; large k; and tokens with more than 32 values in reach, which equal values can
 //     bring): a maximum over the lane's pieces, three shuffles across the eight lanes, and a refill of the one piece that
 //     lost its largest value.
-// 214 instructions per token (256 experts, k = 8; 379 with groups and a bias) against 610 (1300) with a warp per token: 11.5
-// (19.4) us for 32768 tokens against 25 (53).  Issue slots are 55 % used, the pipe of comparisons 45 %; the rest is the latency of
+// 229 instructions per token (256 experts, k = 8; 395 with groups and a bias) against 610 (1300) with a warp per token: 12.2
+// (20.7) us for 32768 tokens against 25 (53), one call after the other on rows that stay in L2; 23.2 with groups on changing rows.
+// Issue slots are 55 % used, the pipe of comparisons 46 to 50 %; the rest is the latency of
 // its steps, with the 20 warps per SM that the registers allow (more warps and spilled values, or the next rows copied ahead
-// into shared memory, were 5 % slower).  Other groupings, and batches that do not fill the GPU (up to some 2300 tokens: 4.7
+// into shared memory, were 2 to 7 % slower).  Other groupings, and batches that do not fill the GPU (up to some 2300 tokens: 4.7
 // against 7.4 us for 512 tokens), take the warp-per-token kernel, whose chain of steps is shorter.
 #include "mok_internal.cuh"
 #include <cuda_fp16.h>
@@ -287,8 +288,8 @@ __device__ __forceinline__ void load4(const H* row, int e, int E, float (&v)[4])
 template <int NI> constexpr int GATE_FLOATS = 4 * (32 * NI + MAX_K + 64);      // shared memory of a warp
 
 // Blocks of an SM: what the registers of 4 NI values and NI maxima per thread leave room for.  (7 of the small ones, not 8:
-// 32768 tokens of 128 experts 9.5 -> 8.6 us, 8192 of 64 5.0 -> 3.8, 40000 of 30 8.2 -> 9.2; 5 for NI = 8, not 4 or 6: 19.4 against
-// 21.3 and 20.5.)
+// 32768 tokens of 128 experts 8.9 us against 10.0, 8192 of 64 3.9 against 5.1, but 40000 of 30 9.5 against 8.4; 5 for NI = 8, not 4
+// or 6: 32768 tokens of 256 experts in groups 20.7 against 22.3 and 21.1.)
 constexpr int gate_blocks(int NI) { return NI <= 4 ? 7 : NI <= 6 ? 6 : NI <= 8 ? 5 : NI <= 12 ? 3 : 2; }
 
 // No groups, or groups of whole pieces of four experts: four tokens per warp.  NI pieces of four experts per lane (E <= 32 NI).
@@ -786,7 +787,7 @@ static cudaError_t launch_backward_four(const BwdParams& p, cudaStream_t s) {
     const bool vec = p.E % 4 == 0 && (p.T == 1 || p.stride % 4 == 0) && (reinterpret_cast<uintptr_t>(p.logits) & (4 * sizeof(L) - 1)) == 0;
     // A block's chain of dependent loads is its time, so the blocks are many and short.  The rows are written past the caches'
     // usual order: where they and the logits exceed L2 the next loads do not wait for them to be evicted (32768 tokens of 256
-    // experts, sigmoid, inputs and outputs beyond L2: 11.0 us; two rounds of blocks and plain stores 12.0; one slot per lane for
+    // experts, sigmoid, inputs and outputs beyond L2: 11.1 us; two rounds of blocks and plain stores 12.0; one slot per lane for
     // small k, which leaves more room on an SM, 12.3: the next call's blocks then crowd on the SMs that are done first).
     const long long units = ((long long)p.T + 4 * WARPS - 1) / (4 * WARPS), most = 148 * 64;
     const size_t smem = sizeof(float) * WARPS * 4 * ((p.E + 7) & ~7);

@@ -15,7 +15,10 @@ namespace i8 {
 
 constexpr int THREADS = 256;
 constexpr int ONE_BLOCK = 1024, ONE_BLOCK_ROUTES = 32768;    // of the schedule in one block
-constexpr long long GROUPED_ROWS = 112;                      // rows per expert up to which launch_grouped is the faster one
+// Rows per expert up to which launch_grouped is the faster one.  Grouped against pairs, at 80, 112 and 128 rows: 128 experts of
+// 2048 x 768 185/191, 207/211, 222/227 us; 32 of 2880 x 2880 188/215, 221/243, 244/283; 16 of 4096 x 2048 118/131, 131/140, 140/141;
+// 64 of 1024 x 512 60/67, 76/71, 79/73; at 200 rows the pairs are ahead of all but the third.
+constexpr long long GROUPED_ROWS = 112;
 
 // Rows of h (fp32) -> codes and a scale (which the combine puts on), one per route: route j's row is pos[j].
 template <int TPR, int NV>
