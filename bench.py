@@ -2,8 +2,10 @@
 
     python bench.py [--gpus N] [--steps K] [--warmup W] [--config NAME] [--impl mok|reference]
 
-Prints ONE JSON line.  Default workload: the DeepSeek-V3-like layer (T=32768, H=7168, E=256, k=8, I=2048, one shared
-expert of I=2048; about 23 GB of expert weights resident in HBM), synthetic seeded inputs.  The same line carries
+Prints ONE JSON line of less than 2000 characters on stdout (the metric, its configuration, clocks, roofline and the end-to-end
+number), so that whoever keeps only the end of the output has all of it; the full record, one JSON line as well, goes to stderr
+before it.  Default workload: the DeepSeek-V3-like layer (T=32768, H=7168, E=256, k=8, I=2048, one shared
+expert of I=2048; about 23 GB of expert weights resident in HBM), synthetic seeded inputs.  The full record carries
 `per_config` (the four smaller workloads, each timed the same way) and `sweep` (the default workload at T = 64, 512,
 4096 against the HBM weight-read roofline); `--per-config none` / `--no-sweep` leave them out.
 
@@ -45,6 +47,21 @@ NCU_TRAFFIC = {
     "mixtral_8x7b": {"bytes": 3.553e9, "scale": 1, "source": "profiles/gemm_kernels_other_workloads.md"},
     "gpt_oss_120b": {"bytes": 5.136e9, "scale": 1, "source": "profiles/gemm_kernels_other_workloads.md"},
 }
+
+
+LINE_KEYS = ("metric", "value", "unit", "n_gpus", "steps", "warmup", "ms_per_step", "higher_is_better", "scaling", "vs_baseline",
+             "dtype", "data", "config", "tflops", "gpu_launches", "clocks", "e2e")
+LINE_PARTS = {"roofline": ("bound", "achieved", "peak", "unit", "frac"), "cpu_baseline": ("value", "unit", "cores", "kind")}
+
+
+def emit(record):
+    """The full record on stderr, the line on stdout."""
+    print(json.dumps(record), file=sys.stderr, flush=True)
+    line = {k: record[k] for k in LINE_KEYS if k in record}
+    for name, keys in LINE_PARTS.items():
+        if name in record:
+            line[name] = {k: record[name][k] for k in keys if k in record[name]}
+    print(json.dumps(line), flush=True)
 
 
 def parse():
@@ -778,7 +795,7 @@ def run_ep(args, cfg, rank, local_rank, world):
                     "mode": "per step: pinned host x -> the rank's peer-visible token buffer, the expert-parallel layer, "
                             "out -> pinned host", "result_bits_equal_device_call": same_bits},
         }
-        print(json.dumps(line), flush=True)
+        emit(line)
     dist.barrier()
     dist.destroy_process_group()
 
@@ -1083,7 +1100,7 @@ def main():
         line["per_config"] = per_config
     if sweep:
         line["sweep"] = sweep
-    print(json.dumps(line), flush=True)
+    emit(line)
     if dist is not None:
         dist.destroy_process_group()
 
