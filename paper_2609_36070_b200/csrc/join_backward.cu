@@ -488,6 +488,12 @@ static cudaError_t launch_general(const Params& p, dim3 grid, dim3 block, int sm
 struct Shape {
     int threads, rows, blocks;
 };
+// Whether the usual kernel does a call.  It has no sums of a bias' or a channel gate's gradient (which are wanted of biases that are not there,
+// too: NULL stands for zeros).
+static bool usual_call(const Params& p, Layout layout) {
+    const bool no_sums = p.slot[2] < 0 && p.slot[3] < 0 && p.slot[4] < 0;
+    return layout != ELEMENTS && plain(p) && no_sums && p.d_sum && p.sum && (p.before != MOK_NORM_NONE || p.after != MOK_NORM_NONE);
+}
 // Blocks that stay, one per SM, of as many rows (at most `most`) as its threads are; fewer for few rows.
 static Shape backward_shape(int T, int H, Layout layout, int ld8, int vpt, int most) {
     Shape s;
@@ -513,7 +519,7 @@ static cudaError_t launch_backward_of(Params p, Layout layout, cudaStream_t s, i
     const bool vec = layout != ELEMENTS, shifted = layout == SHIFTED;
     *blocks = shape.blocks;
     const bool before = p.before != MOK_NORM_NONE, after = p.after != MOK_NORM_NONE;
-    const bool usual = VPT == 2 && vec && plain(p) && p.d_sum && p.sum && (before || after);
+    const bool usual = VPT == 2 && usual_call(p, layout);
     const int wide = shape.threads * VPT * 8;       // elements of a row in shared memory
     const dim3 grid(shape.blocks), block(shape.threads, shape.rows);
     const int sums_wide = shifted ? wide : p.H;      // a row of sums
@@ -586,7 +592,7 @@ static cudaError_t launch_rows(const Params& p, Layout layout, cudaStream_t s, i
     // Shifted pieces, beside elements: rms norms of 16392 x 2047 145 against 240 us, 65536 x 505 127 against 201; but a row that only its shift
     // brings to a second warp, 65536 x 511, 240 against 202.
     if (layout == SHIFTED && p.H <= 512 && (p.H + 14) / 8 > 64) layout = ELEMENTS;
-    const bool usual = layout != ELEMENTS && plain(p) && p.d_sum && p.sum && (p.before != MOK_NORM_NONE || p.after != MOK_NORM_NONE);
+    const bool usual = usual_call(p, layout);
     // The general kernel has no shifted form: its vectors would lie in shared memory once for each of a block's rows, which leaves room for
     // fewer of them (16384 x 2047, layer norms, gate and dropout: 695 against 390 us by elements).
     if (!usual && layout == SHIFTED) layout = ELEMENTS;

@@ -331,3 +331,36 @@ def test_rows_that_begin_anywhere(mok, T, H, pad, before, after, gate, shift, dt
     rule = {k: v[:, :H] if torch.is_tensor(v) and v.dim() == 2 and v.shape[1] > 1 else v[:H].clone() if torch.is_tensor(v) and v.dim() == 1 else v
             for k, v in rule.items()}
     check(mok, d, rule, scale=0.5, p=0.0 if gate is None else 0.25, seed=9, offset=1 << 33)
+
+
+@pytest.mark.parametrize("before,after", [("rms", "rms"), ("rms", None), (None, "rms"), ("layer", "rms"), ("layer", "layer")])
+@pytest.mark.parametrize("T,H", [(1, 2047), (5, 264), (40, 1025), (700, 520), (601, 2047), (333, 2880), (300, 505), (200, 8185), (150, 8192)])
+@pytest.mark.parametrize("stream", [BF, FF])
+def test_gradients_of_biases_that_are_not_there(mok, T, H, before, after, stream):
+    """Through the C entry point: a NULL bias stands for zeros, and has a gradient like any other; with every other result, and alone."""
+    import ctypes
+    from paper_2609_36070_b200 import build
+    from test_join_abi import Join, JoinBackward
+    lib = ctypes.CDLL(build.LIB)
+    d, rule = make(T + H, T, H, BF, stream, FF, before, after, None, False)
+    zeros = {n + "_bias": torch.zeros(H, device="cuda") for n, norm in (("before", before), ("after", after)) if norm}
+    want, bound = ref.backward_bounds(d["d_sum"].double(), None if before is None else d["d_normed"].double(), d["x"].double(), d["y"].double(), half(stream),
+                                      half(BF), **wide({**rule, **zeros}))
+    names = ("dx", "dy", "dgate", "d_before_weight", "d_before_bias", "d_after_weight", "d_after_bias")
+    there = [n for n, w in zip(names, want) if w is not None]
+    kinds = {None: 0, "rms": 1, "layer": 2}
+    at = lambda t: None if t is None else t.data_ptr()
+    forward = Join(x=at(d["x"]), y=at(d["y"]), before_weight=at(rule["before_weight"]), after_weight=at(rule["after_weight"]), x_stride=H, y_stride=H, T=T,
+                   H=H, type=0, x_type=2 if stream == FF else 0, vector_type=2, before=kinds[before], after=kinds[after], scale=1.0, eps=1e-6)
+    need = mok.mok_join_bwd_workspace_bytes(T, H)
+    ws = torch.full((need + 512,), 0x5A, device="cuda", dtype=torch.uint8)
+    first = -ws.data_ptr() % 256
+    for wanted in (there, [n for n in there if n.endswith("bias")]):
+        outs = {n: torch.full((T, H) if n in ("dx", "dy") else (H,), float("nan"), device="cuda", dtype={"dx": stream, "dy": BF}.get(n, FF)) for n in wanted}
+        b = JoinBackward(forward=forward, d_sum=at(d["d_sum"]), d_normed=at(d["d_normed"]), d_sum_stride=H, d_normed_stride=H, dx_stride=H, dy_stride=H,
+                         workspace=ws.data_ptr() + first, workspace_bytes=need, stream=torch.cuda.current_stream().cuda_stream,
+                         **{n: at(t) for n, t in outs.items()})
+        assert lib.mok_block_join_backward(ctypes.byref(b)) == 0
+        for n, t in outs.items():
+            near(t, want[names.index(n)], bound[names.index(n)], n)
+        assert (ws[:first] == 0x5A).all() and (ws[first + need:] == 0x5A).all()
