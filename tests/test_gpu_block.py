@@ -136,3 +136,19 @@ def test_command(train):
     done = subprocess.run(cmd, cwd=root, capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, done.stderr[-2000:]
     assert "us per step" in done.stdout
+
+
+@pytest.mark.parametrize("T", [20, 100])
+def test_rows_of_wider_buffers(T):
+    """The layer's input as columns of a wider buffer: the same as in rows of its own, in both layers and in the gradients."""
+    blocks, x, normed = stack(7, T, n=1)
+    wide = torch.full((T, 256 + 40), 3.0, device="cuda", dtype=BF)
+    wide[:, 8:8 + 256] = normed
+    d_x, d_n = (torch.randn(T, 256, generator=gen(s), device="cuda").to(BF) for s in (1, 2))
+    results = []
+    for n in (normed, wide[:, 8:8 + 256]):
+        total, out, saved = blocks[0](x, n, save=True)
+        dx, dn, g = blocks[0].backward(saved, d_x, d_n)
+        results.append([total, out, dx, dn] + [g[k] for k in sorted(g)])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
