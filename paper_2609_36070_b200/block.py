@@ -29,8 +29,15 @@ class Saved:
             setattr(self, name, fields[name])
 
 
+def _check_weight(name, t, shape, dtype, device):
+    if tuple(t.shape) != tuple(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous tensor {list(shape)} of {dtype} on {device}, got shape {list(t.shape)}, strides "
+                         f"{list(t.stride())}, {t.dtype} on {t.device}")
+
+
 class ExpertBlock:
-    """W_router fp32 [E, H], W_gate_up bf16 [E, 2I, H], W_down bf16 [E, H, I], shared [2 I_s, H] and [H, I_s] or None.
+    """W_router fp32 [E, H], W_gate_up bf16 [E, 2I, H], W_down bf16 [E, H, I], shared [2 I_s, H] and [H, I_s] or None.  (The experts may be
+    fp16 where up to 64 tokens are all that the block is called with, forwards.)
 
     after, after_weight, after_bias: the norm of the layer's output; gate, scale, p: how it is added to the residual stream;
     before, before_weight, before_bias: the norm in front of the NEXT block's layer (all of them as in `mok_block_join`)."""
@@ -39,6 +46,18 @@ class ExpertBlock:
                  before_weight=None, before_bias=None, after=None, after_weight=None, after_bias=None, gate=None, scale=1.0, eps=1e-6, p=0.0):
         self.W_router, self.router_bias, self.k = W_router, router_bias, k
         self.experts = (W_gate_up, W_down, W_shared_gate_up, W_shared_down)
+        if W_gate_up.dim() != 3 or W_gate_up.dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"W_gate_up: expected [E, 2I, H] of bfloat16, got shape {list(W_gate_up.shape)} of {W_gate_up.dtype}")
+        if (W_shared_gate_up is None) != (W_shared_down is None):
+            raise ValueError("W_shared_gate_up, W_shared_down: expected both or neither")
+        _, H, I, I_s, E, _ = self.sizes(0)
+        shapes = dict(W_gate_up=(E, 2 * I, H), W_down=(E, H, I), W_shared_gate_up=(2 * I_s, H), W_shared_down=(H, I_s))
+        for (name, shape), t in zip(shapes.items(), self.experts):
+            if t is not None:
+                _check_weight(name, t, shape, W_gate_up.dtype, W_gate_up.device)
+        _check_weight("W_router", W_router, (E, H), torch.float32, W_gate_up.device)
+        if router_bias is not None:
+            _check_weight("router_bias", router_bias, (E,), torch.float32, W_gate_up.device)
         self.rule = dict(before=before, before_weight=before_weight, before_bias=before_bias, after=after, after_weight=after_weight,
                          after_bias=after_bias, gate=gate, scale=scale, eps=eps, p=p)
 
@@ -55,8 +74,18 @@ class ExpertBlock:
             raise mok.MokError(mok.MOK_ERR_SHAPE)
         return torch.empty(max(need, few) + 256, dtype=torch.uint8, device=self.W_router.device)
 
+    def check_input(self, normed, many):
+        """many: for the layer of many tokens or the gradients, which read bf16 whatever they are given."""
+        W = self.experts[0]
+        if normed.dim() != 2 or normed.shape[1] != W.shape[2] or normed.dtype != W.dtype or normed.device != W.device:
+            raise ValueError(f"normed: expected [T, {W.shape[2]}] of {W.dtype} on {W.device}, got shape {list(normed.shape)} of {normed.dtype} "
+                             f"on {normed.device}")
+        if many and W.dtype != torch.bfloat16:
+            raise ValueError(f"more than {mok.MOK_FEW_MAX_TOKENS} tokens, and gradients, are for experts of bfloat16, these are of {W.dtype}")
+
     def layer(self, normed, workspace=None, routes=False):
         """The expert layer's output; with routes also topk_idx and topk_w."""
+        self.check_input(normed, len(normed) > mok.MOK_FEW_MAX_TOKENS)
         if workspace is None:
             workspace = self.workspace(len(normed))
         if len(normed) <= mok.MOK_FEW_MAX_TOKENS:
@@ -77,6 +106,7 @@ class ExpertBlock:
     def backward(self, saved, d_x, d_normed):
         """From the gradients of the block's two outputs (d_x may be None: 0) those of its two inputs and of its weights: (d_x, d_normed,
         {name: gradient}).  A seed tensor has to hold what it held in the forward pass."""
+        self.check_input(saved.normed, True)
         d_sum, d_y, d_gate, *vectors = mok.mok_block_join_backward(d_x, d_normed, saved.sum, saved.y, **self.rule, seed=saved.seed,
                                                                    offset=saved.offset)
         g = mok.mok_moe_backward(saved.normed.contiguous(), *self.experts, saved.topk_idx, saved.topk_w, d_y)

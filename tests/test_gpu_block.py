@@ -152,3 +152,22 @@ def test_rows_of_wider_buffers(T):
         results.append([total, out, dx, dn] + [g[k] for k in sorted(g)])
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("T", [20, 100])
+def test_types_that_the_layer_does_not_take(T):
+    """They are refused for any number of tokens: the layer for many tokens reads bf16 whatever it is given."""
+    from paper_2609_36070_b200.block import ExpertBlock
+    blocks, x, normed = stack(7, T, n=1)
+    b = blocks[0]
+    for bad in (normed.float(), normed.half(), normed[:, :128], normed[0], normed.cpu()):
+        with pytest.raises(ValueError):
+            b(x, bad)
+    half = ExpertBlock(b.W_router, *(w.half() for w in b.experts), k=2, before="rms")
+    if T > 64:
+        with pytest.raises(ValueError):
+            half(x.half(), normed.half())
+    else:
+        _, _, saved = half(x.half(), normed.half(), save=True)
+        with pytest.raises(ValueError):
+            half.backward(saved, None, normed.half())
