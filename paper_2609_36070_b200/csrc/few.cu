@@ -770,7 +770,7 @@ few_kernel(const __grid_constant__ CUtensorMap m_gu, const __grid_constant__ CUt
         }
         asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory");
         const int n1 = ctrl->sh1 - ctrl->sh0 + ctrl->r1 - ctrl->r0, n = n1 + ctrl->v1 - ctrl->v0;
-        bool go = !a.starve;
+        bool go = true;
         for (int i = 0; go && i <= n; ++i) {
             if (i == n1) {
                 go = wait_done(waits, a.signals, 1, G, lane);
@@ -779,7 +779,7 @@ few_kernel(const __grid_constant__ CUtensorMap m_gu, const __grid_constant__ CUt
                     if (c == 0) a.signals->go = 0ull;
                 }
             }
-            if (go && i < n)
+            if (go && i < n && !a.starve)
                 go = load_tokens<X, MT>(a, ctrl, waits, ring, room, unit_of(a, ctrl, i, n1, blocks, rows1, rows2), i < n1, i < n1 ? a.groups1 : a.groups2,
                                         me, turn, lane);
         }
@@ -899,16 +899,17 @@ few_kernel(const __grid_constant__ CUtensorMap m_gu, const __grid_constant__ CUt
         }
         w.finish(rows2);
     }
+    __syncthreads();                                     // no wait of the CTA is under way any more
     if (*(volatile uint32_t*)&ctrl->abort) {             // failure path only: copies in flight land before the CTA leaves
         const unsigned long long t0 = globaltimer();
         while (globaltimer() - t0 < 200000ull) { }
-        // a replay of this call has the same number: it must not find its flags set
+        // a replay of this call has the same number: it must not find its flags set (the token loader clears them behind barrier 2, which it
+        // did not get past if it gave up)
         if (threadIdx.x == 0) {
             a.signals->flag[c] = 0ull;
             if (c == 0) a.signals->go = 0ull;
         }
     }
-    __syncthreads();
 }
 
 // ---------------------------------------------------------------------------------------------------------------- host side
