@@ -637,7 +637,7 @@ typedef struct mok_few_args {
     int32_t score;                           /* MOK_SCORE_* */
     int32_t n_groups, topk_groups, group_top, renormalise;
     float scale;
-    int32_t debug;                           /* MOK_DEBUG_STARVE: nothing is loaded and waits run out after 2 ms (a test hook) */
+    int32_t debug;                           /* MOK_DEBUG_STARVE: no weights are loaded and waits run out after 2 ms (a test hook) */
     void* out;                               /* [T, H] of type, rows out_stride elements apart */
     int32_t* topk_idx;                       /* out: int32 [T, k], or NULL */
     float* topk_w;                           /* out: fp32 [T, k], or NULL */

@@ -105,7 +105,7 @@ struct Args {
     int32_t groups1, groups2;                            // row groups of a unit in the two phases
     int32_t t_tile, t_tiles;                             // ring of the tokens: bytes of eight tokens, how many of them it holds
     double per_cta;                                      // 1 / grid
-    int32_t starve;                                      // test hook: the producer loads nothing
+    int32_t starve;                                      // test hook: no weights are loaded
     unsigned long long number, wait_ns;                  // the call's number
     gate::Params gate;                                   // idx and w: where the routes go
     void* out;
@@ -357,7 +357,8 @@ struct TokenRoom {
     // false: the CTA is giving up
     __device__ __forceinline__ bool take(const TokenRing& ring, int n, const Waits& waits) {
         while (steps == T_STEPS || used + n > ring.tiles) {
-            if (!waits.mbar(oldest.is_empty(), oldest.phase, 6)) return false;
+            // (all lanes alike: after an abort one may still find the step free where another gives up)
+            if (!__all_sync(0xffffffffu, waits.mbar(oldest.is_empty(), oldest.phase, 6))) return false;
             used -= (int)(sizes >> (4 * oldest.slot)) & 15;
             --steps;
             oldest.advance();
@@ -779,7 +780,7 @@ few_kernel(const __grid_constant__ CUtensorMap m_gu, const __grid_constant__ CUt
                     if (c == 0) a.signals->go = 0ull;
                 }
             }
-            if (go && i < n && !a.starve)
+            if (go && i < n)
                 go = load_tokens<X, MT>(a, ctrl, waits, ring, room, unit_of(a, ctrl, i, n1, blocks, rows1, rows2), i < n1, i < n1 ? a.groups1 : a.groups2,
                                         me, turn, lane);
         }
