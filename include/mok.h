@@ -615,7 +615,8 @@ int mok_i8_starve(int wait_limit_us, void* stream);
  * with logits x W_router^T + router_bias (fp32) and from them the ids and weights of mok_gate (its rules, limits and masks; bias
  * takes part in the selection only, router_bias is part of the logits).  x, weights, add and out are of one type, bf16 or fp16; the
  * gated activation is rounded to it between the products, everything else is fp32, and an output is rounded once.  out may be x or
- * add.  Deterministic.  A NaN or infinity reaches the outputs of its own token only (and of all tokens that meet it as a weight).
+ * add.  Deterministic: a token's bits do not depend on the tokens beside it, and are the same in all batches of up to 16 tokens and in all
+ * of more (whose products add up in another order).  A NaN or infinity reaches the outputs of its own token only (and of all tokens that meet it as a weight).
  * Limits: T <= MOK_FEW_MAX_TOKENS; H, I, I_shared multiples of 8 and at most 2^20; E <= 512, k <= 32.
  * The launch is cooperative, one CTA per SM, which wait for one another (bounded: mok_read_status(workspace)); calls that may run at
  * the same time need a workspace each.  The workspace needs no initialisation.

@@ -448,7 +448,9 @@ struct Consumer {
             weights_at[b] = (uint32_t)(block * rows + rg * MT * tile_step) * 128 + chunk;
             tokens_at[b] = (uint32_t)block * 1024 + chunk;
         }
-        constexpr int SETS = TILES * MT <= 2 ? 2 : 1;    // of accumulators, by which a chain of products is shorter
+        // Sets of accumulators, by which a chain of products is shorter.  Not by TILES: the order of a token's sums would depend on how many
+        // others meet its expert.
+        constexpr int SETS = MT == 1 ? 2 : 1;
         float other[MT][TILES][4];
 #pragma unroll
         for (int m = 0; m < MT; ++m)
