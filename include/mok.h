@@ -662,10 +662,11 @@ int mok_moe_few(const mok_few_args* args);
  *               device pointer to {seed, offset} (64 bits each), which a captured call reads on every replay, or NULL
  * y = NULL: sum is x (and need not be written: sum = NULL).  x = NULL: nothing is added to.  sum may be x, and normed y, in place.
  * x and sum are of x_type (that of y, or fp32), y and normed of type, the norms' vectors of vector_type.  Arithmetic is fp32, statistics
- * are two-pass, every output is rounded once (normed is made from the sum before it is rounded).  A row's bits do not depend on the
- * other rows (but on its alignment); a NaN or infinity stays in its row.  H <= MOK_JOIN_MAX_WIDTH; rows may have any stride; 16-byte aligned rows of a
- * multiple of 8 elements are the fast path, next to them (rms norms alone) rows of any width in buffers that lie on 32 bytes, all equally far
- * apart modulo 8 elements.
+ * are two-pass, every output is rounded once (normed is made from the sum before it is rounded).  A row's bits do not depend on what the
+ * other rows hold, but on how many there are, on their alignment and on the options: these choose the code, and with it the order of a row's
+ * sums.  A NaN or infinity stays in its row.  (Squares and their sums are fp32: a norm takes values up to 1e17.)  H <= MOK_JOIN_MAX_WIDTH; rows
+ * may have any stride; 16-byte aligned rows of a multiple of 8 elements are the fast path, next to them (rms norms alone) rows of any width
+ * in buffers that lie on 32 bytes, all equally far apart modulo 8 elements.
  */
 #define MOK_JOIN_MAX_WIDTH 8192
 enum { MOK_NORM_NONE = 0, MOK_NORM_RMS = 1, MOK_NORM_LAYER = 2 };

@@ -364,3 +364,21 @@ def test_gradients_of_biases_that_are_not_there(mok, T, H, before, after, stream
         for n, t in outs.items():
             near(t, want[names.index(n)], bound[names.index(n)], n)
         assert (ws[:first] == 0x5A).all() and (ws[first + need:] == 0x5A).all()
+
+
+@pytest.mark.parametrize("before,after,gate,shift", [("rms", "rms", None, False), ("layer", "layer", "full", True)])
+@pytest.mark.parametrize("H", [520, 2047, 4096])
+def test_numbers_of_rows_where_the_code_changes(mok, H, before, after, gate, shift):
+    """592 rows and one more run in other code: both are held to the bound, and a row's bits stay while only the others' contents change."""
+    d, rule = make(H, 593, H, BF, BF, FF, before, after, gate, shift)
+    for T in (592, 593):
+        part = {k: v[:T] for k, v in d.items()}
+        some = {k: v[:T] if k == "gate" and v is not None else v for k, v in rule.items()}
+        total, normed = check(mok, part, some, scale=0.5)
+        others = torch.ones(T, dtype=torch.bool, device="cuda")
+        others[::7] = False
+        new = {k: torch.where(others[:, None], v.flip(0), v) for k, v in part.items()}
+        if gate:
+            some["gate"] = torch.where(others[:, None], some["gate"].flip(0), some["gate"])
+        again = mok.mok_block_join(new["x"], new["y"], **some, scale=0.5)
+        assert torch.equal(again[0][~others], total[~others]) and torch.equal(again[1][~others], normed[~others])
