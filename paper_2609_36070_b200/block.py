@@ -94,9 +94,9 @@ class ExpertBlock:
         out = mok.mok_moe_forward_ex(normed.contiguous(), self.W_router, self.router_bias, *self.experts, self.k, workspace, stages=routes)
         return (out[0], out[1]["topk_idx"], out[1]["topk_w"]) if routes else out
 
-    def __call__(self, x, normed, workspace=None, seed=0, offset=0, save=False):
-        """(x, normed) for the next block, from this block's; with save also what `backward` needs.  seed, offset: of the dropout (seed may
-        be an int64 tensor [2] of both on the device)."""
+    def __call__(self, x, normed, workspace=None, seed=0, offset=None, save=False):
+        """(x, normed) for the next block, from this block's; with save also what `backward` needs.  seed, offset: of the dropout, integers
+        (None: 0), or seed an int64 tensor [2] of both on the device and no offset."""
         y, idx, w = self.layer(normed, workspace, True) if save else (self.layer(normed, workspace), None, None)
         total, after = mok.mok_block_join(x, y, **self.rule, seed=seed, offset=offset)
         if not save:

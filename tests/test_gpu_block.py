@@ -171,3 +171,29 @@ def test_types_that_the_layer_does_not_take(T):
         _, _, saved = half(x.half(), normed.half(), save=True)
         with pytest.raises(ValueError):
             half.backward(saved, None, normed.half())
+
+
+@pytest.mark.parametrize("T", [10, 70])
+def test_a_seed_on_the_device(T):
+    """Seed and offset in a tensor: the mask of the same integers, other masks on the replays of a captured step, and gradients by the same."""
+    blocks, x, normed = stack(8, T, n=1, p=0.3)
+    b = blocks[0]
+    want = b(x, normed, seed=5, offset=7, save=True)
+    d_x, d_n = (torch.randn(T, 256, generator=gen(s), device="cuda").to(BF) for s in (1, 2))
+    want_back = b.backward(want[2], d_x, d_n)
+    seed = torch.tensor([5, 7], device="cuda")
+    got = b(x, normed, seed=seed, save=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    back = b.backward(got[2], d_x, d_n)
+    assert torch.equal(back[0], want_back[0]) and torch.equal(back[1], want_back[1])
+    ws = b.workspace(T)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = b(x, normed, ws, seed=seed)
+        seed[1] += 1
+    for offset in (7, 8):
+        graph.replay()
+        assert torch.equal(got[0], b(x, normed, seed=5, offset=offset)[0])
+    with pytest.raises(ValueError):
+        b(x, normed, seed=seed, offset=3)
