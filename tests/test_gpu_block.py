@@ -197,3 +197,26 @@ def test_a_seed_on_the_device(T):
         assert torch.equal(got[0], b(x, normed, seed=5, offset=offset)[0])
     with pytest.raises(ValueError):
         b(x, normed, seed=seed, offset=3)
+
+
+@pytest.mark.parametrize("T", [40, 200])
+def test_gradients_of_the_router(T):
+    """From the gradient of the routes' weights, which the layer's own tests hold, to those of the router: fp32 products of up to 256 terms
+    after a softmax, so 1e-5 of the norm; and the input's, with a rounding to bf16 (2^-8 of each element at most)."""
+    from paper_2609_36070_b200 import mok
+    blocks, x, normed = stack(9, T, n=1)
+    b = blocks[0]
+    d_x, d_n = (torch.randn(T, 256, generator=gen(s), device="cuda").to(BF) for s in (1, 2))
+    _, _, saved = b(x, normed, save=True)
+    _, dn, grads = b.backward(saved, d_x, d_n)
+    d_y = mok.mok_block_join_backward(d_x, d_n, saved.sum, saved.y, **b.rule)[1]
+    g = mok.mok_moe_backward(saved.normed, *b.experts, saved.topk_idx, saved.topk_w, d_y)
+    leaves = [t.double().requires_grad_() for t in (b.W_router, b.router_bias, saved.normed)]
+    logits = leaves[2] @ leaves[0].t() + leaves[1]
+    w = torch.softmax(logits.gather(1, saved.topk_idx.long()), -1)
+    assert (w - saved.topk_w).abs().max() < 1e-5
+    want = torch.autograd.grad(w, leaves, g["dw"].double())
+    for name, ref in zip(("W_router", "router_bias"), want):
+        assert (grads[name].double() - ref).norm() <= 1e-5 * ref.norm(), name
+    ref = want[2] + g["dx"].double()
+    assert (dn.double() - ref).norm() <= (2.0 ** -8 + 1e-5) * ref.norm()
