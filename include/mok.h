@@ -401,7 +401,7 @@ size_t mok_mx_workspace_bytes(int T, int H, int I, int I_shared, int E, int k);
  * Outputs: dx = dL/dx through the experts (bf16 [T, H]; the router's own path from x to the logits is not part of
  * the layer's backward), dw = dL/dtopk_w (fp32 [T, k], the router-weight gradient, or NULL), and the weight
  * gradients in bf16 with the shapes of the weights (all four NULL = activation gradients only; otherwise all that
- * belong to present experts must be given).  bf16 mode only; H, I and I_shared must be multiples of 32.
+ * belong to present experts must be given; zeros for T = 0).  bf16 mode only; H, I and I_shared must be multiples of 32.
  * Deterministic like the forward pass: no float atomics, fixed reduction orders.
  */
 typedef struct mok_bwd_args {

@@ -24,6 +24,7 @@
 // dw is accumulated in fp32.  Deterministic: fixed tile order, fixed k order, fixed combine order, no float atomics.
 #include "mok_internal.cuh"
 #include <string.h>
+#include <utility>
 
 namespace mok {
 
@@ -239,6 +240,20 @@ int backward_chain(const mok_bwd_args* a, const BwdLayout& B, const WsLayout& L,
 
 using namespace mok;
 
+// No tokens: the sums over them are 0.
+template <class Args>
+static int zero_weight_gradients(const Args* a, int experts) {
+    const size_t routed = (size_t)experts * a->I * a->H, shared = (size_t)a->I_shared * a->H;
+    const std::pair<void*, size_t> sums[4] = {{a->dW_gate_up, 4 * routed}, {a->dW_down, 2 * routed}, {a->dW_shared_gate_up, 4 * shared},
+                                              {a->dW_shared_down, 2 * shared}};            // bytes: bf16, gate and up rows
+    for (const auto& [to, bytes] : sums)
+        if (to && bytes) {
+            const cudaError_t e = cudaMemsetAsync(to, 0, bytes, reinterpret_cast<cudaStream_t>(a->stream));
+            if (e != cudaSuccess) return cuda_fail(e);
+        }
+    return MOK_OK;
+}
+
 extern "C" {
 
 size_t mok_bwd_workspace_bytes(int T, int H, int I, int I_shared, int E, int k) {
@@ -252,7 +267,7 @@ int mok_moe_backward(const mok_bwd_args* a) {
     if (!bwd_layout(a->T, a->H, a->I, a->I_shared, a->E, a->k, &B)) return MOK_ERR_SHAPE;
     if ((a->I_shared > 0) != (a->W_shared_gate_up != nullptr) || (a->I_shared > 0) != (a->W_shared_down != nullptr))
         return MOK_ERR_SHAPE;
-    if (a->T == 0) return MOK_OK;
+    if (a->T == 0) return zero_weight_gradients(a, a->E);
     if (!a->x || !a->W_gate_up || !a->W_down || !a->topk_idx || !a->topk_w || !a->dout || !a->dx) return MOK_ERR_NULL;
     if (!aligned16(a->x) || !aligned16(a->W_gate_up) || !aligned16(a->W_down) || !aligned16(a->W_shared_gate_up) ||
         !aligned16(a->W_shared_down) || !aligned16(a->dout) || !aligned16(a->dx) || !aligned16(a->dW_gate_up) ||
@@ -546,7 +561,7 @@ int mok_ep_expert_bwd(const mok_ep_bwd_args* a) {
     if (a->config && (a->config->impl != MOK_IMPL_TCGEN05 || a->config->grid < 0 || a->config->precision != MOK_PRECISION_BF16 ||
                       (a->config->cta_group != 0 && a->config->cta_group != 1 && a->config->cta_group != 3)))
         return MOK_ERR_SHAPE;
-    if (a->T_local == 0) return MOK_OK;
+    if (a->T_local == 0) return zero_weight_gradients(a, a->E / a->n_ranks);
     if (!a->idx_all || !a->w_all || !a->W_gate_up || !a->W_down || !a->dxg || !a->pos || !a->dw_routes) return MOK_ERR_NULL;
     if (a->I_shared > 0 && !a->dx_shared) return MOK_ERR_NULL;
     for (int r = 0; r < a->n_ranks; ++r) {

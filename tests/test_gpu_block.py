@@ -220,3 +220,25 @@ def test_gradients_of_the_router(T):
         assert (grads[name].double() - ref).norm() <= 1e-5 * ref.norm(), name
     ref = want[2] + g["dx"].double()
     assert (dn.double() - ref).norm() <= (2.0 ** -8 + 1e-5) * ref.norm()
+
+
+def test_no_rows():
+    """Gradients of an empty batch are zeros, also in memory that held something else."""
+    from paper_2609_36070_b200 import mok
+    blocks, x, normed = stack(10, 1, n=1, p=0.1)
+    b, none = blocks[0], normed[:0]
+    W = b.experts
+    def poison():
+        used = [torch.full(s, float("nan"), device="cuda", dtype=BF) for w in W for s in [w.shape] * 3]
+        del used
+    poison()
+    total, out, saved = b(x[:0], none, save=True)
+    dx, dn, grads = b.backward(saved, x[:0], none)
+    assert total.shape == out.shape == dx.shape == dn.shape == (0, 256)
+    names = {"W_router", "router_bias", "W_gate_up", "W_down", "W_shared_gate_up", "W_shared_down", "gate", "before_weight", "after_weight", "after_bias"}
+    assert set(grads) == names and all((g == 0).all() for g in grads.values())
+    poison()
+    idx, w = torch.empty(1, 0, dtype=torch.int32, device="cuda"), torch.empty(1, 0, device="cuda")
+    ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
+    grads = mok.mok_ep_expert_bwd(0, [0], [0], idx, w, *W, 8, 2, 256, none, idx, w, none, ws)
+    assert len(grads) == 4 and all((g == 0).all() for g in grads.values())
