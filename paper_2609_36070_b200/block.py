@@ -103,6 +103,7 @@ class ExpertBlock:
             return total, after
         return total, after, Saved(normed=normed, y=y, sum=total, topk_idx=idx, topk_w=w, seed=seed, offset=offset)
 
+    @torch.no_grad()
     def backward(self, saved, d_x, d_normed):
         """From the gradients of the block's two outputs (d_x may be None: 0) those of its two inputs and of its weights: (d_x, d_normed,
         {name: gradient}).  A seed tensor has to hold what it held in the forward pass."""

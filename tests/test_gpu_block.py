@@ -242,3 +242,47 @@ def test_no_rows():
     ws = torch.empty(1 << 22, dtype=torch.uint8, device="cuda")
     grads = mok.mok_ep_expert_bwd(0, [0], [0], idx, w, *W, 8, 2, 256, none, idx, w, none, ws)
     assert len(grads) == 4 and all((g == 0).all() for g in grads.values())
+
+
+@pytest.mark.parametrize("T", [10, 100])
+def test_parameters(T):
+    """Weights that require gradients: all of a block is outside of autograd, and its gradients hold no graph."""
+    blocks, x, normed = stack(11, T, n=1)
+    b = blocks[0]
+    want = b.backward(b(x, normed, save=True)[2], x, normed)
+    b.W_router, b.router_bias = torch.nn.Parameter(b.W_router), torch.nn.Parameter(b.router_bias)
+    b.experts = tuple(torch.nn.Parameter(w) for w in b.experts)
+    total, out, saved = b(x, normed, save=True)
+    d_x, d_normed, grads = b.backward(saved, x, normed)
+    assert not any(t.requires_grad for t in (total, out, d_x, d_normed, *grads.values()))
+    assert torch.equal(d_x, want[0]) and torch.equal(d_normed, want[1]) and all(torch.equal(g, want[2][n]) for n, g in grads.items())
+
+
+def test_a_training_step_in_a_graph():
+    """Forwards and backwards of two blocks, captured: other masks on every replay, and the gradients of each."""
+    blocks, x, normed = stack(12, 100, n=2, p=0.2)
+    seed = torch.tensor([3, 0], device="cuda")
+    def step():
+        total, out, saved = x, normed, []
+        for b in blocks:
+            total, out, s = b(total, out, seed=seed, save=True)
+            saved.append(s)
+        d_x, d_n, grads = x, normed, []
+        for b, s in zip(blocks[::-1], saved[::-1]):
+            d_x, d_n, g = b.backward(s, d_x, d_n)
+            grads += g.values()
+        return [total, out, d_x, d_n, *grads]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for offset in (0, 1, 1 << 40):
+        seed[1] = offset
+        graph.replay()
+        for a, b in zip(got, step()):
+            assert torch.equal(a, b)
