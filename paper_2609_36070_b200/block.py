@@ -90,8 +90,9 @@ class ExpertBlock:
             workspace = self.workspace(len(normed))
         if len(normed) <= mok.MOK_FEW_MAX_TOKENS:
             return mok.mok_moe_few(normed, self.W_router, self.router_bias, *self.experts, self.k, workspace, stages=routes)
-        # (mok_moe_forward_ex takes rows one behind the other, mok_moe_few any)
-        out = mok.mok_moe_forward_ex(normed.contiguous(), self.W_router, self.router_bias, *self.experts, self.k, workspace, stages=routes)
+        # (mok_moe_forward_ex takes rows one behind the other, and runs on the current device; mok_moe_few takes any, and finds theirs)
+        with torch.cuda.device(normed.device):
+            out = mok.mok_moe_forward_ex(normed.contiguous(), self.W_router, self.router_bias, *self.experts, self.k, workspace, stages=routes)
         return (out[0], out[1]["topk_idx"], out[1]["topk_w"]) if routes else out
 
     def __call__(self, x, normed, workspace=None, seed=0, offset=None, save=False):
@@ -110,7 +111,8 @@ class ExpertBlock:
         self.check_input(saved.normed, True)
         d_sum, d_y, d_gate, *vectors = mok.mok_block_join_backward(d_x, d_normed, saved.sum, saved.y, **self.rule, seed=saved.seed,
                                                                    offset=saved.offset)
-        g = mok.mok_moe_backward(saved.normed.contiguous(), *self.experts, saved.topk_idx, saved.topk_w, d_y)
+        with torch.cuda.device(saved.normed.device):
+            g = mok.mok_moe_backward(saved.normed.contiguous(), *self.experts, saved.topk_idx, saved.topk_w, d_y)
         logits = saved.normed.float() @ self.W_router.t()
         if self.router_bias is not None:
             logits += self.router_bias

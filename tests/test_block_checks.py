@@ -22,3 +22,39 @@ def test_weights_are_checked():
     for bad in (torch.zeros(4, dtype=torch.bfloat16), torch.zeros(3), torch.zeros(8)[::2]):
         with pytest.raises(ValueError):
             ExpertBlock(*weights(), k=2, router_bias=bad)
+
+
+def test_the_layer_runs_on_its_tensors_device(monkeypatch):
+    """The entry points for many tokens and for gradients launch on the current device, whichever holds the tensors: the block makes it theirs."""
+    from paper_2609_36070_b200 import block, mok
+    current, met = [], []
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            current.append(self.device)
+
+        def __exit__(self, *_):
+            current.pop()
+
+    def forward(x, *_, stages=False, **__):
+        met.append(("forward", list(current)))
+        return x, {"topk_idx": torch.zeros(len(x), 2, dtype=torch.int32), "topk_w": torch.zeros(len(x), 2)}
+
+    def backward(x, *_, **__):
+        met.append(("backward", list(current)))
+        return {n: torch.zeros(1, 64) for n in ("dx", "dw", "dW_gate_up", "dW_down", "dW_shared_gate_up", "dW_shared_down")}
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(mok, "mok_moe_forward_ex", forward)
+    monkeypatch.setattr(mok, "mok_moe_backward", backward)
+    monkeypatch.setattr(mok, "mok_block_join", lambda x, y, **_: (x, y))
+    monkeypatch.setattr(mok, "mok_block_join_backward", lambda d_x, *_, **__: (d_x, d_x, None, None, None, None, None))
+    monkeypatch.setattr(block, "router_gradients", lambda *_: (torch.zeros(4, 64), torch.zeros(1, 64), torch.zeros(1, 4)))
+    b = block.ExpertBlock(*weights(), k=2)
+    x = torch.zeros(65, 64, dtype=torch.bfloat16)
+    _, _, saved = b(x, x, save=True)
+    b.backward(saved, x, x)
+    assert met == [("forward", [x.device]), ("backward", [x.device])]
