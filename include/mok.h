@@ -616,7 +616,8 @@ int mok_i8_starve(int wait_limit_us, void* stream);
  * takes part in the selection only, router_bias is part of the logits).  x, weights, add and out are of one type, bf16 or fp16; the
  * gated activation is rounded to it between the products, everything else is fp32, and an output is rounded once.  out may be x or
  * add.  Deterministic: a token's bits do not depend on the tokens beside it, and are the same in all batches of up to 16 tokens and in all
- * of more (whose products add up in another order).  A NaN or infinity reaches the outputs of its own token only (and of all tokens that meet it as a weight).
+ * of more (whose products add up in another order).  A NaN or infinity reaches the outputs of its own token only (and of all tokens that
+ * meet it as a weight); in fp16 a gated activation beyond 65504 is an infinity.
  * Limits: T <= MOK_FEW_MAX_TOKENS; H, I, I_shared multiples of 8 and at most 2^20; E <= 512, k <= 32.
  * The launch is cooperative, one CTA per SM, which wait for one another (bounded: mok_read_status(workspace)); calls that may run at
  * the same time need a workspace each.  The workspace needs no initialisation.
@@ -658,7 +659,7 @@ int mok_moe_few(const mok_few_args* args);
  *               elements apart) or per element (MOK_JOIN_GATE_FULL, [T, H] of type)
  *     drop    : with probability p an element becomes 0, the others are divided by 1 - p.  Element (t, h) stays if word h % 4 of
  *               Philox4x32-10 (Salmon et al. 2011) of the counter (h / 4, t, low and high word of offset) under the key (low and
- *               high word of seed) is at least p 2^32: nothing is stored, and the gradient finds the same mask again.  seed_at: a
+ *               high word of seed) is at least p 2^32, rounded to an integer: nothing is stored, and the gradient finds the same mask again.  seed_at: a
  *               device pointer to {seed, offset} (64 bits each), which a captured call reads on every replay, or NULL
  * y = NULL: sum is x (and need not be written: sum = NULL).  x = NULL: nothing is added to.  sum may be x, and normed y, in place.
  * x and sum are of x_type (that of y, or fp32), y and normed of type, the norms' vectors of vector_type.  Arithmetic is fp32, statistics
@@ -695,7 +696,8 @@ int mok_block_join(const mok_join_args* args);
 /* The gradients of mok_block_join from those of its outputs (d_sum may be NULL: 0).  `forward` holds the call's arguments with x
  * replaced by the sum that it left (needed if before != MOK_NORM_NONE); its outputs and stream are not used.  Any of the results may
  * be NULL: dx (the gradient of the sum, which is that of x), dy, dgate ([H] fp32, or as the gate), and the norms' vectors' in fp32, which are
- * sums over the rows in a fixed order and need the workspace. */
+ * sums over the rows in a fixed order and need the workspace.  A vector that is NULL has a gradient, too; results of a norm or gate that
+ * there is not are left as they are. */
 typedef struct mok_join_bwd_args {
     mok_join_args forward;
     const void* d_sum;                       /* [T, H] of x_type, or NULL */

@@ -450,7 +450,8 @@ const char FEW_DOC[] =
     "            stream=None)\n"
     "--\n\n"
     "The whole layer for up to 64 tokens x [T, H] (bf16 or fp16) in one launch; routing as in mok_gate, add [T, H] is added to the\n"
-    "output.  Returns out [T, H], or (out, topk_idx, topk_w) with stages.  workspace: from alloc_few_workspace (None: allocated).";
+    "output.  Returns out [T, H], or (out, topk_idx, topk_w) with stages.  workspace: from alloc_few_workspace (None: allocated).\n"
+    "Outside of autograd, like the layer's own calls.";
 PyObject* few(PyObject*, PyObject* const* args, Py_ssize_t n, PyObject* kw) {
     HANDLE_TH_ERRORS
     static const char* const texts[] = {"x", "W_router", "router_bias", "W_gate_up", "W_down", "W_shared_gate_up", "W_shared_down", "k",

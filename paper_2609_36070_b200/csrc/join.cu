@@ -3,7 +3,7 @@
 //   u = norm_after(y);   v = gate .* u;   sum = x + scale * drop(v);   normed = norm_before(sum)
 //   norm(v) = (v - m) r w + b,   r = 1 / sqrt(mean((v - m)^2) + eps),   m = mean(v) (layer norm) or 0 (rms)
 //   drop(v)[t, h] = v[t, h] / (1 - p) where word h % 4 of Philox4x32-10 (Salmon et al. 2011) of counter (h / 4, t, offset) under key
-//                   `seed` is at least p 2^32, else 0: a function of the position, so that no mask is stored
+//                   `seed` is at least p 2^32 (rounded), else 0: a function of the position, so that no mask is stored
 // Backwards, with n = (v - m) r and the gradient g of norm's output, the gradient of v is r (g w - mean(g w) - n mean(g w n)) (the
 // first mean for layer norms only), that of w is sum_t g n and that of b sum_t g.
 //

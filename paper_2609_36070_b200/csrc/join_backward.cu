@@ -7,9 +7,10 @@
 // more rows ahead, and needs no barrier to read them.
 //
 // Measured: rms norms, 32768 x 7168 bf16 (2.8 GB): 558 to 577 us, 0.75 of the copy bandwidth, and 16384 x 2880: 130 us; bound by the
-// chain of a row's two sums at 16 warps per SM (128 registers; more rows at once would spill).  Layer norms with biases, gate and dropout,
-// 8192 x 2880: 178 us for 57.6 of bytes; bound by its instructions, 170 per element at 65 % of the issue slots: the sums a quarter of them,
-// the generator a tenth.
+// chain of a row's two sums at 16 warps per SM (128 registers, of which two norms spill 4 to 40 bytes; more rows at once would spill more).
+// Layer norms with biases, gate and dropout, 8192 x 2880: 178 us for 57.6 of bytes; bound by its instructions, 170 per element at 65 % of the
+// issue slots, of which the row sums are an eighth and the generator a tenth.  The 896 threads that a block of one piece per thread may
+// have leave 72 registers: it spills 44 to 60 bytes, by elements 216 to 232.
 #include "join_common.cuh"
 
 namespace mok {
@@ -122,10 +123,10 @@ join_backward_plain_kernel(const Params p) {
         if (!live[i])
             for (int q = 0; q < p.stages; ++q) {
                 char* to = mine + q * p.stage_bytes;
-                if (BEFORE) store8<true>(reinterpret_cast<S*>(to + p.at_x), at, H, zeros());
-                if (BEFORE) store8<true>(reinterpret_cast<Y*>(to + p.at_dnormed), at, H, zeros());
-                if (AFTER) store8<true>(reinterpret_cast<Y*>(to + p.at_y), at, H, zeros());
-                store8<true>(reinterpret_cast<S*>(to + p.at_dsum), at, H, zeros());
+                if (BEFORE) store8<PIECES>(reinterpret_cast<S*>(to + p.at_x), at, H, zeros());
+                if (BEFORE) store8<PIECES>(reinterpret_cast<Y*>(to + p.at_dnormed), at, H, zeros());
+                if (AFTER) store8<PIECES>(reinterpret_cast<Y*>(to + p.at_y), at, H, zeros());
+                store8<PIECES>(reinterpret_cast<S*>(to + p.at_dsum), at, H, zeros());
             }
     }
     __syncthreads();
@@ -176,17 +177,17 @@ join_backward_plain_kernel(const Params p) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             if (BEFORE) {
-                v[i] = widen(load8<true>(hx, i * step, H));
-                d[i] = widen(load8<true>(hn, i * step, H));
+                v[i] = widen(load8<PIECES>(hx, i * step, H));
+                d[i] = widen(load8<PIECES>(hn, i * step, H));
                 if (M == SHIFTED && !whole[i]) {
                     v[i] = within<M>(v[i], at0 + i * step - shift, H);
                     d[i] = within<M>(d[i], at0 + i * step - shift, H);
                 }
                 a = dot8(v[i], v[i], a);
-                c = dot8(d[i] * widen(load8<true>(wb, i * step, H)), v[i], c);
+                c = dot8(d[i] * widen(load8<PIECES>(wb, i * step, H)), v[i], c);
             }
             if (AFTER) {
-                y[i] = widen(load8<true>(hy, i * step, H));
+                y[i] = widen(load8<PIECES>(hy, i * step, H));
                 if (M == SHIFTED && !whole[i]) y[i] = within<M>(y[i], at0 + i * step - shift, H);
                 b = dot8(y[i], y[i], b);
             }
@@ -211,12 +212,12 @@ join_backward_plain_kernel(const Params p) {
         a = two(0.f);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            F8 direct = widen(load8<true>(hd, i * step, H));
+            F8 direct = widen(load8<PIECES>(hd, i * step, H));
             if (M == SHIFTED && !whole[i]) direct = within<M>(direct, at0 + i * step - shift, H);
             if (BEFORE) {
                 v[i] = v[i] * two(r0);                   // n
                 sum_before[i] = fma8(d[i], v[i], sum_before[i]);
-                d[i] = fma8(fma8(v[i], two(mean), d[i] * widen(load8<true>(wb, i * step, H))), two(r0), direct);
+                d[i] = fma8(fma8(v[i], two(mean), d[i] * widen(load8<PIECES>(wb, i * step, H))), two(r0), direct);
             } else {
                 d[i] = direct;
             }
@@ -225,7 +226,7 @@ join_backward_plain_kernel(const Params p) {
             if (AFTER) {
                 y[i] = y[i] * two(r1);
                 sum_after[i] = fma8(d[i], y[i], sum_after[i]);
-                d[i] = d[i] * widen(load8<true>(wa, i * step, H));
+                d[i] = d[i] * widen(load8<PIECES>(wa, i * step, H));
                 a = dot8(d[i], y[i], a);
             }
         }
@@ -281,11 +282,11 @@ join_backward_kernel(const Params p) {
         if (RING && !live[i])
             for (int q = 0; q < p.stages; ++q) {
                 char* to = mine + q * p.stage_bytes;
-                if (p.at_x >= 0) store8<true>(reinterpret_cast<S*>(to + p.at_x), at, H, zeros());
-                if (p.at_dsum >= 0) store8<true>(reinterpret_cast<S*>(to + p.at_dsum), at, H, zeros());
-                if (p.at_dnormed >= 0) store8<true>(reinterpret_cast<Y*>(to + p.at_dnormed), at, H, zeros());
-                if (p.at_y >= 0) store8<true>(reinterpret_cast<Y*>(to + p.at_y), at, H, zeros());
-                if (p.at_gate >= 0) store8<true>(reinterpret_cast<Y*>(to + p.at_gate), at, H, zeros());
+                if (p.at_x >= 0) store8<PIECES>(reinterpret_cast<S*>(to + p.at_x), at, H, zeros());
+                if (p.at_dsum >= 0) store8<PIECES>(reinterpret_cast<S*>(to + p.at_dsum), at, H, zeros());
+                if (p.at_dnormed >= 0) store8<PIECES>(reinterpret_cast<Y*>(to + p.at_dnormed), at, H, zeros());
+                if (p.at_y >= 0) store8<PIECES>(reinterpret_cast<Y*>(to + p.at_y), at, H, zeros());
+                if (p.at_gate >= 0) store8<PIECES>(reinterpret_cast<Y*>(to + p.at_gate), at, H, zeros());
             }
         for (int a = 0; a < 3; ++a)
             if (live[i] && p.at_acc[a] >= 0) store8<M>(reinterpret_cast<float*>(s_mem + p.at_acc[a]) + threadIdx.y * H, at, H, zeros());
@@ -297,7 +298,7 @@ join_backward_kernel(const Params p) {
         store8<M>(to, at, H, widen(load8<M>(to, at, H)) + v);
     };
     auto vector = [&](int where, const void* from, int at) {
-        return RING ? widen(load8<true>(reinterpret_cast<const float*>(s_mem + where), at, H)) : vector8<M>(from, p.vector_type, at < H ? at : 0, H);
+        return RING ? widen(load8<PIECES>(reinterpret_cast<const float*>(s_mem + where), at, H)) : vector8<M>(from, p.vector_type, at < H ? at : 0, H);
     };
     // one row's pieces of this thread into a stage; a group per row, empty past the last one.  (Addresses are made anew for every row:
     // five pointers to be kept would cost registers that the sums need.)
@@ -338,7 +339,7 @@ join_backward_kernel(const Params p) {
         auto take = [&](int where, const auto* base, long long ld, int i) {
             using E = std::remove_const_t<std::remove_pointer_t<decltype(base)>>;
             const int at = at0 + i * step;
-            if (RING) return widen(load8<true>(reinterpret_cast<const E*>(held + where), at, H));
+            if (RING) return widen(load8<PIECES>(reinterpret_cast<const E*>(held + where), at, H));
             Raw<E> r = Raw<E>();
             if (live[i]) r = load8<M>(base + row * ld, at, H);
             return widen(r);
