@@ -18,7 +18,7 @@
 //                 CTA that completes a slice adds up its tokens' rows in slot order
 //
 // Measured (one call among others, weights beyond L2): 16 tokens of 128 experts of 2048 x 768, k = 8, with 766 MB of weights that are met:
-// 148 us, 5.2 TB/s from beginning to end (floor 119); 64 tokens of 8 experts of 4096 x 14336 (2.8 GB): 540 to 570 us; one token of
+// 148 us, 5.2 TB/s from beginning to end (floor 119); 64 tokens of 8 experts of 4096 x 14336 (2.8 GB): 526 to 583 us by the box; one token of
 // the first layer (75 MB): 37 us, of which 13 pass before the routes are known and 3 in the last slices' sums.
 //
 // The ring runs across the barriers: the shared expert's gate/up rows are on their way before the tokens are routed, and W_down's

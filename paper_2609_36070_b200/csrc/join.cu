@@ -12,7 +12,7 @@
 // consecutive elements (16 bytes of a 16-bit type) to a thread at a time.  All arithmetic is fp32, statistics are two-pass (mean
 // first), and outputs are rounded once: `normed` is made from the sum before it is rounded.
 //
-// Measured: rms norms, 32768 x 7168 bf16 (1.9 GB): 331 to 349 us, 0.82 to 0.87 of the copy bandwidth; 16384 x 2048: 49 (0.83).  Layer norms
+// Measured: rms norms, 32768 x 7168 bf16 (1.9 GB): 331 to 353 us by the box, 0.81 to 0.87 of the copy bandwidth; 16384 x 2048: 49 (0.83).  Layer norms
 // with gate and dropout, 8191 x 2880 fp16: 74 us for 28.8 of bytes; bound by its instructions, 78 per element at 71 % of the issue slots.
 //
 // The other direction: join_backward.cu.

@@ -6,7 +6,7 @@
 // layer norm), so the next rows are on their way meanwhile: each thread copies its own pieces asynchronously into shared memory, two or
 // more rows ahead, and needs no barrier to read them.
 //
-// Measured: rms norms, 32768 x 7168 bf16 (2.8 GB): 558 to 577 us, 0.75 of the copy bandwidth, and 16384 x 2880: 130 us; bound by the
+// Measured: rms norms, 32768 x 7168 bf16 (2.8 GB): 558 to 583 us by the box, 0.75 of the copy bandwidth, and 16384 x 2880: 130 us; bound by the
 // chain of a row's two sums at 16 warps per SM (128 registers, of which two norms spill 4 to 40 bytes; more rows at once would spill more).
 // Layer norms with biases, gate and dropout, 8192 x 2880: 178 us for 57.6 of bytes; bound by its instructions, 170 per element at 65 % of the
 // issue slots, of which the row sums are an eighth and the generator a tenth.  The 896 threads that a block of one piece per thread may
